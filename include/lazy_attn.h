@@ -224,6 +224,82 @@ LAZY_API int lazy_attn_combine(const void* part_o, const float* part_lse, int32_
                                int32_t head_dim, void* out, float* lse, void* stream);
 
 /*
+ * Backward pass of lazy_attn_prefill: gradients of the queries and of the stored keys and values.  The probabilities
+ * are recomputed from q, K and the forward pass's log-sum-exps.  With s_ij the scaled (and biased) score of row i (a
+ * query token and head) and key j, both rotated to their positions,
+ *     P_ij = exp(s_ij - lse_i) (0 where hidden),   delta_i = dout_i . out_i - dlse_i,
+ *     dS_ij = P_ij (dout_i . v_j - delta_i),       dv_j = sum_i P_ij dout_i,
+ *     dq_i = scale R(-p_i) sum_j dS_ij R(p_j) k_j, dk_j = scale sum_i R(-p_j) dS_ij R(p_i) q_i,
+ * where the sums for a stored key run over every request, position and query head that reads it: a chunk that several
+ * requests share receives the sum of their gradients, each turned back from its own position.  Rows that see no key
+ * (lse = -inf) give and receive nothing.
+ *
+ * Which requests read a stored key is worked out once per set of tables, on the host, by lazy_attn_backward_plan:
+ * every 64 stored keys become a tile with the list of its uses, tiles with much work are cut into parts, and the rows
+ * of dq are cut into row tiles and key splits.  Every sum is formed in a fixed order (no atomics): equal calls give
+ * equal bits.
+ */
+typedef struct lazy_backward_info {
+  int32_t batch;         /* what the plan was made for; lazy_attn_prefill_backward checks it against its arguments */
+  int32_t total_q;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t causal;
+  int32_t key_positions;
+  int32_t num_tiles;     /* work items of the key and value gradients */
+  int32_t num_segments;  /* uses of tiles */
+  int32_t num_merges;    /* tiles that were cut into parts */
+  int32_t num_parts;     /* parts of all of them */
+  int32_t num_row_items; /* work items of the query gradient */
+  int32_t num_blocks;    /* blocks of query tokens */
+  int32_t row_slots;     /* most key splits of a request */
+  int32_t row_blocks;    /* 32-row blocks a wave of the query gradient holds (1 or 2) */
+  int32_t reserved;      /* 0 */
+  int64_t plan_bytes;    /* size of the plan */
+} lazy_backward_info_t;
+
+/*
+ * Host planner (CPU only, on HOST copies of the prefill's tables).  Writes the plan (an opaque array for the device,
+ * to be copied there as it is) and *info.  plan_capacity < info->plan_bytes (0 with plan = NULL to ask for the size)
+ * is LAZY_EINVAL; *info is written all the same.  The plan depends on the tables, head counts, head_dim, causal and
+ * key_positions, not on tensors: one plan serves every layer and step that uses the same tables.
+ * LAZY_EDATA: prefix sums that do not start at 0 or decrease, a record or query that breaks the layout contract
+ * (records of length 0 are passed over), or records whose stored keys overlap in a way that gives a key no single
+ * gradient: other strides, a distance that is no whole number of keys, or keys that two records pair with different
+ * values.  Records of one chunk that overlap with the same strides and pairing (other lengths, other first keys) are
+ * fine.  LAZY_EUNSUPPORTED: total_q * G * G >= 2^32.
+ */
+LAZY_API int lazy_attn_backward_plan(const lazy_attn_params_t* params, const int32_t* q_start, const int32_t* q_pos0,
+                                     const lazy_chunk_t* chunks, const int32_t* chunk_start, int32_t batch, void* plan,
+                                     size_t plan_capacity, lazy_backward_info_t* info);
+
+LAZY_API size_t lazy_attn_backward_workspace_size(const lazy_attn_params_t* params, const lazy_backward_info_t* info);
+
+/*
+ * The backward pass.  q .. chunk_start as given to lazy_attn_prefill; out, lse as it wrote them; plan: the device copy
+ * of lazy_attn_backward_plan's array for exactly these tables (16-byte aligned; its contents are trusted), info its
+ * host record.
+ *   dout     [total_q][Hq][D] bf16, gradient of the loss by out
+ *   dlse     [total_q][Hq] fp32, gradient by lse (a loss over merged partial results depends on it), or NULL
+ *   dq       [total_q][Hq][D] bf16, fully overwritten
+ *   dk_pool, dv_pool  bf16 bases laid out like k_pool and v_pool (they may be the same pointer, provided that no
+ *            record's keys are another's values).  Every key of every record is overwritten, with zeros where no query
+ *            sees it; everything else is left as it was.
+ *   workspace  at least lazy_attn_backward_workspace_size(...) bytes, 16-byte aligned.
+ * Gradients are rounded to bf16 once, from fp32 sums; q (rotated, times the scale) and the keys are rounded to bf16
+ * for the matrix cores as in the forward pass, and so are P and dS.  With q_prerotated dq is the gradient of q as
+ * given.  num_splits and cache_hint have no effect.
+ */
+LAZY_API int lazy_attn_prefill_backward(const lazy_attn_params_t* params, const void* q, const int32_t* q_start,
+                                        const int32_t* q_pos0, const void* k_pool, const void* v_pool,
+                                        const lazy_chunk_t* chunks, const int32_t* chunk_start, int32_t batch,
+                                        int32_t total_q, const void* out, const float* lse, const void* dout,
+                                        const float* dlse, const void* plan, const lazy_backward_info_t* info, void* dq,
+                                        void* dk_pool, void* dv_pool, void* workspace, size_t workspace_bytes,
+                                        void* stream);
+
+/*
  * Materialise-then-attend baseline, step 1 (the re-encoding copy that LazyAttention avoids; Block-Attention's
  * rotate-and-copy path described in the appendix "Experiments Details"): for every record i of every request,
  * write R(pos_offset + j) k_j into k_out, request after request, so that each request's rotated keys form one

@@ -36,6 +36,9 @@ SOURCES = [
     ("lazy_attn_validate.cpp", "host"),
     ("lazy_attn_plan.cpp", "host"),
     ("lazy_attn_pool.cpp", "host"),
+    ("lazy_attn_backward.hip", "hip"),
+    ("lazy_attn_backward_api.cpp", "hip"),
+    ("lazy_attn_backward_plan.cpp", "host"),
 ]
 
 

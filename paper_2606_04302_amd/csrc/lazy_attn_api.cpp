@@ -9,34 +9,11 @@
 
 #include "lazy_attn.h"
 #include "lazy_attn_internal.h"
+#include "lazy_attn_params.h"
 
 namespace {
 
-constexpr int kNumCUs = 256;              // MI355X compute units
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-int check_params(const lazy_attn_params_t* p) {
-  if (!p) return LAZY_EINVAL;
-  if (p->num_q_heads <= 0 || p->num_kv_heads <= 0 || p->num_q_heads % p->num_kv_heads != 0) return LAZY_EINVAL;
-  if (p->causal != 0 && p->causal != 1) return LAZY_EINVAL;
-  if (!isfinite(p->softmax_scale) || p->softmax_scale < 0.f) return LAZY_EINVAL;
-  if (p->rope_style != LAZY_ALIBI && !p->inv_freq && !(isfinite(p->rope_base) && p->rope_base > 0.f)) return LAZY_EINVAL;
-  if (p->num_splits < 0) return LAZY_EINVAL;
-  if (p->key_positions != LAZY_KEYS_NOPE && p->key_positions != LAZY_KEYS_LOCAL) return LAZY_EINVAL;
-  if (p->rope_style != LAZY_ROPE_HALF && p->rope_style != LAZY_ROPE_INTERLEAVED && p->rope_style != LAZY_ALIBI)
-    return LAZY_EINVAL;
-  if (p->rope_style == LAZY_ALIBI && p->key_positions != LAZY_KEYS_NOPE) return LAZY_EINVAL;
-  if (p->q_prerotated != 0 && p->q_prerotated != 1) return LAZY_EINVAL;
-  if (p->cache_hint != LAZY_CACHE_DEFAULT && p->cache_hint != LAZY_CACHE_STREAM) return LAZY_EINVAL;
-  if (p->head_dim != 64 && p->head_dim != 128) return LAZY_EUNSUPPORTED;
-  return LAZY_OK;
-}
-
-float scale_log2(const lazy_attn_params_t* p) {
-  const float s = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
-  return s * 1.4426950408889634f;
-}
+using lazy::ceil_div, lazy::check_params, lazy::kNumCUs, lazy::scale_log2;
 
 // 256 packed rows per workgroup (eight waves, one workgroup per CU; head_dim 128 only) once a request has enough
 // rows; otherwise 128 rows (four waves, two workgroups per CU).  Must match the kernel chosen in launch_prefill.

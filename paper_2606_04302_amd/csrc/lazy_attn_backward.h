@@ -1,0 +1,94 @@
+// The backward pass's plan: what the host planner writes and the kernels read (no HIP).
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "lazy_attn.h"
+
+namespace lazy {
+
+constexpr int kGradTileKeys = 64;  // stored keys of one key-gradient tile
+constexpr int kGradRows = 32;      // packed query rows (token * G + head in group) of one step over a tile
+
+// A tile of stored keys (key 0 of KV head 0 at k_off / v_off) or a part of its uses.
+struct GradTile {
+  int64_t k_off, v_off;
+  int32_t kst, vst;
+  int32_t keys;                // 1 .. kGradTileKeys
+  int32_t seg_begin, seg_end;  // its uses (none: the gradient is zero)
+  int32_t part;                // -1: the whole tile; otherwise where its partial sums go
+};
+static_assert(sizeof(GradTile) == 40);
+
+// One use of a tile: query rows row_begin .. row_end - 1 (packed over the batch) of one request, which see the tile's
+// keys key_begin .. key_end - 1, key i at position pos + i.
+struct GradSeg {
+  int32_t row_begin, row_end;
+  int32_t pos_shift;  // a token's position less its index in the batch
+  int32_t pos;
+  int32_t record_pos;  // pos_offset of the record (the rotation of local-position keys)
+  int32_t key_begin, key_end;
+  int32_t full_from;   // rows from this one on see all of the tile's keys (no mask is needed)
+};
+static_assert(sizeof(GradSeg) == 32);
+
+// A tile whose uses were cut into parts: its gradient is the sum of part .. part + parts - 1.
+struct GradMerge {
+  int64_t k_off, v_off;
+  int32_t kst, vst;
+  int32_t keys;
+  int32_t part, parts;
+  int32_t reserved;
+};
+static_assert(sizeof(GradMerge) == 40);
+
+// Query gradient: rows row0 .. of a request against key split `split` of `splits`.
+struct GradRowItem {
+  int32_t request, row0, split, splits;
+};
+
+// Tokens t0 .. t0 + tokens - 1 of one request, whose query gradient comes in `splits` partial sums.
+struct GradBlock {
+  int32_t t0, tokens, pos_shift, splits;
+};
+
+// Where the arrays lie in the plan (all multiples of 8 bytes; the blocks come first so that they are 16-byte aligned).
+struct GradPlanLayout {
+  size_t blocks, rows, tiles, segs, merges, bytes;
+  explicit GradPlanLayout(const lazy_backward_info_t& i) {
+    size_t at = 0;
+    const auto put = [&at](size_t bytes) {
+      const size_t here = at;
+      at += bytes;
+      return here;
+    };
+    blocks = put(sizeof(GradBlock) * (size_t)i.num_blocks);
+    rows = put(sizeof(GradRowItem) * (size_t)i.num_row_items);
+    segs = put(sizeof(GradSeg) * (size_t)i.num_segments);
+    tiles = put(sizeof(GradTile) * (size_t)i.num_tiles);
+    merges = put(sizeof(GradMerge) * (size_t)i.num_merges);
+    bytes = at;
+  }
+};
+
+// Where the backward pass keeps its intermediate results (bytes into the workspace).
+struct GradWorkLayout {
+  size_t q, info, dq, parts, bytes;
+  GradWorkLayout(int hq, int hkv, int d, const lazy_backward_info_t& i) {
+    const size_t rows = (size_t)i.total_q * (size_t)hq;
+    size_t at = 0;
+    const auto put = [&at](size_t bytes) {
+      const size_t here = at;
+      at += (bytes + 255) & ~(size_t)255;
+      return here;
+    };
+    q = put(rows * d * sizeof(uint16_t));                                        // rotated, scaled queries
+    info = put(rows * 2 * sizeof(float));                                        // (-lse log2 e, -delta) of each row
+    dq = put((size_t)i.row_slots * rows * d * sizeof(float));                    // partial query gradients
+    parts = put((size_t)i.num_parts * hkv * 2 * kGradTileKeys * d * sizeof(float));  // partial key, value gradients
+    bytes = at;
+  }
+};
+
+}  // namespace lazy

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "lazy_attn.h"
+#include "lazy_attn_backward.h"
 
 namespace lazy {
 
@@ -72,6 +73,43 @@ struct SharedArgs {
   float scale_log2;
 };
 
+// Arguments of the backward pass's kernels.  rows = total_q * group packed rows a KV head.
+struct GradArgs {
+  const uint16_t* q;           // [total_q][hq][D]
+  const int32_t* q_start;
+  const int32_t* q_pos0;
+  const uint16_t* k_pool;
+  const uint16_t* v_pool;
+  const lazy_chunk_t* chunks;
+  const int32_t* chunk_start;
+  const uint16_t* out;         // [total_q][hq][D]
+  const float* lse;            // [total_q][hq]
+  const uint16_t* dout;        // [total_q][hq][D]
+  const float* dlse;           // [total_q][hq] or null
+  const GradBlock* blocks;     // the plan's arrays
+  const GradRowItem* row_items;
+  const GradSeg* segs;
+  const GradTile* tiles;
+  const GradMerge* merges;
+  uint16_t* dq;                // [total_q][hq][D]
+  uint16_t* dk_pool;
+  uint16_t* dv_pool;
+  uint16_t* ws_q;              // [hkv][rows][D] rotated queries times scale * log2 e, pairs in half-split order
+  float2* ws_info;             // [hkv][rows] (-lse log2 e, -delta)
+  float* ws_dq;                // [row_slots][hkv][rows][D]
+  float* ws_parts;             // [num_parts][hkv][dk, dv][64][D]
+  const float* inv_freq;       // [D/2] or null; ALiBi: [hq] slopes or null
+  int64_t rows;
+  int32_t hq;
+  int32_t hkv;
+  int32_t group;
+  uint32_t group_magic;        // ceil(2^32 / group), 0 for group 1
+  int32_t causal;
+  int32_t rotate_q;            // 0: queries arrive rotated, or nothing is (ALiBi)
+  double rope_log2_base;
+  float scale_log2;
+};
+
 // Packed rows (token, head in group) handled by one prefill workgroup, and keys per decode tile.
 constexpr int kPrefillRowsPerBlock = 128;  // packed rows of a prefill workgroup per row block
 constexpr int kPrefillTileKeys = 64;
@@ -85,6 +123,8 @@ hipError_t launch_decode_shared(const SharedArgs& a, int num_items, int max_slot
 // Device address of the fixed scratch array of lazy_attn_decode_noalloc on `device`, which must be the calling
 // thread's current device; looked up once per device and cached.
 hipError_t noalloc_scratch(int device, void** ptr);
+hipError_t launch_backward(const GradArgs& a, int head_dim, bool local_keys, bool interleaved, bool alibi,
+                           const lazy_backward_info_t& info, hipStream_t stream);
 hipError_t launch_combine(const uint16_t* part_o, const float* part_lse, int splits, int rows, int head_dim,
                           uint16_t* out, float* lse, hipStream_t stream);
 hipError_t launch_materialize(const uint16_t* k_pool, const lazy_chunk_t* chunks, int num_records,

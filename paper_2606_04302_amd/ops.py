@@ -57,6 +57,17 @@ USER_DTYPE = np.dtype([("request", "<i4"), ("pos_offset", "<i4"), ("slot", "<i4"
 assert RANGE_DTYPE.itemsize == 32 and ITEM_DTYPE.itemsize == 24 and USER_DTYPE.itemsize == 16
 SHARED_MAX_RANGES = 64  # LAZY_SHARED_MAX_RANGES
 
+
+
+class BackwardInfo(ctypes.Structure):
+    """lazy_backward_info_t: what a backward plan was made for and how much work it holds."""
+
+    _fields_ = [(n, _c_i32) for n in ("batch", "total_q", "num_q_heads", "num_kv_heads", "head_dim", "causal",
+                                      "key_positions", "num_tiles", "num_segments", "num_merges", "num_parts",
+                                      "num_row_items", "num_blocks", "row_slots", "row_blocks", "reserved")]
+    _fields_ += [("plan_bytes", _c_i64)]
+
+
 _ATTN_PREFILL = [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_i32, _c_i32, _c_i32,
                  _c_i32, _c_p, _c_p, _c_p, _c_sz, _c_p]
 _ATTN_DECODE = [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_i32, _c_i32, _c_p, _c_p,
@@ -71,6 +82,12 @@ SIGNATURES = {
     "lazy_attn_decode_noalloc": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_i32,
                                           _c_i32, _c_p, _c_p, _c_p]),
     "lazy_attn_combine": (_c_i32, [_c_p, _c_p, _c_i32, _c_i32, _c_i32, _c_p, _c_p, _c_p]),
+    "lazy_attn_backward_plan": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_i32, _c_p, _c_sz,
+                                         ctypes.POINTER(BackwardInfo)]),
+    "lazy_attn_backward_workspace_size": (_c_sz, [ctypes.POINTER(LazyAttnParams), ctypes.POINTER(BackwardInfo)]),
+    "lazy_attn_prefill_backward": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p,
+                                            _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_p, _c_p,
+                                            ctypes.POINTER(BackwardInfo), _c_p, _c_p, _c_p, _c_p, _c_sz, _c_p]),
     "lazy_materialize_k": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_i32, _c_i32, _c_i64, _c_p, _c_p,
                                     _c_p]),
     "lazy_attn_validate": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_i32, _c_i64, _c_i64,
@@ -321,6 +338,87 @@ def split_views(workspace, rows: int, head_dim: int):
     po = workspace[: s * rows * head_dim * 2].view(torch.bfloat16).view(s, rows, head_dim)
     pl = workspace[s * rows * head_dim * 2: s * per].view(torch.float32).view(s, rows)
     return po, pl
+
+
+@dataclass
+class BackwardPlan:
+    """Plan of a backward pass: the library's opaque array (host or device) and its host record."""
+
+    data: np.ndarray | torch.Tensor  # uint8
+    info: BackwardInfo
+
+
+def backward_plan(cfg: Config, q_start: np.ndarray, q_pos0: np.ndarray, chunks: np.ndarray,
+                  chunk_start: np.ndarray) -> BackwardPlan:
+    """lazy_attn_backward_plan on host tables (the prefill's, chunks as a CHUNK_DTYPE array)."""
+    _need(chunks.dtype == CHUNK_DTYPE, "chunks must be a CHUNK_DTYPE array")
+    chunks = np.ascontiguousarray(chunks)
+    q_start, q_pos0, chunk_start = (np.ascontiguousarray(t, np.int32) for t in (q_start, q_pos0, chunk_start))
+    batch = chunk_start.size - 1
+    _need(batch >= 0 and q_start.size == batch + 1 and q_pos0.size == batch, "table sizes disagree with the batch")
+    _need(0 <= int(chunk_start[-1]) <= chunks.size, "chunk_start goes past the records")
+    p, info = cfg.c(), BackwardInfo()
+    args = (ctypes.byref(p), q_start.ctypes.data, q_pos0.ctypes.data, chunks.ctypes.data, chunk_start.ctypes.data, batch)
+    code = lib().lazy_attn_backward_plan(*args, None, 0, ctypes.byref(info))
+    if code != LAZY_EINVAL:  # EINVAL: only the size was asked for (or the arguments are bad, then again below)
+        _check(code, "lazy_attn_backward_plan")
+    data = np.zeros(int(info.plan_bytes), np.uint8)
+    _check(lib().lazy_attn_backward_plan(*args, data.ctypes.data, data.size, ctypes.byref(info)),
+           "lazy_attn_backward_plan")
+    return BackwardPlan(data, info)
+
+
+def upload_backward_plan(plan: BackwardPlan, device="cuda:0") -> BackwardPlan:
+    """The plan with its array on the device."""
+    return BackwardPlan(torch.from_numpy(plan.data).to(device), plan.info)
+
+
+def backward_workspace_size(cfg: Config, plan: BackwardPlan) -> int:
+    p = cfg.c()
+    return int(lib().lazy_attn_backward_workspace_size(ctypes.byref(p), ctypes.byref(plan.info)))
+
+
+def prefill_backward(cfg: Config, q, q_start, q_pos0, k_pool, v_pool, chunks, chunk_start, out, lse, dout,
+                     plan: BackwardPlan, dlse=None, dq=None, dk_pool=None, dv_pool=None, workspace=None, stream=None):
+    """lazy_attn_prefill_backward.  Returns (dq, dk_pool, dv_pool).  Gradient pools that are not given are allocated
+    and zeroed (one for both if k_pool and v_pool are the same tensor); given ones keep what no record covers."""
+    for t, name in ((q, "q"), (k_pool, "k_pool"), (v_pool, "v_pool"), (out, "out"), (dout, "dout")):
+        _dev(t, torch.bfloat16, name)
+    for t, name in ((q_start, "q_start"), (q_pos0, "q_pos0"), (chunk_start, "chunk_start")):
+        _dev(t, torch.int32, name)
+    _chunks(chunks)
+    _need(q.dim() == 3 and q.shape[1] == cfg.num_q_heads and q.shape[2] == cfg.head_dim, "q must be [T, Hq, D]")
+    _need(out.shape == q.shape and dout.shape == q.shape, "out and dout must have the shape of q")
+    for t, name in ((lse, "lse"), (dlse, "dlse")):
+        if t is None and name == "dlse":
+            continue
+        _dev(t, torch.float32, name)
+        _need(t.shape == q.shape[:2], f"{name} must be [T, Hq]")
+    batch = q_start.numel() - 1
+    _need(chunk_start.numel() == batch + 1 and q_pos0.numel() == batch, "table sizes disagree with the batch")
+    _need(isinstance(plan.data, torch.Tensor), "the plan must be on the device (upload_backward_plan)")
+    _dev(plan.data, torch.uint8, "plan")
+    _need(plan.data.numel() == plan.info.plan_bytes, "the plan's array does not belong to its record")
+    if dq is None:
+        dq = torch.empty_like(q)
+    if dk_pool is None:
+        dk_pool = torch.zeros_like(k_pool)
+        if dv_pool is None and v_pool.data_ptr() == k_pool.data_ptr() and v_pool.shape == k_pool.shape:
+            dv_pool = dk_pool
+    if dv_pool is None:
+        dv_pool = torch.zeros_like(v_pool)
+    for t, like, name in ((dq, q, "dq"), (dk_pool, k_pool, "dk_pool"), (dv_pool, v_pool, "dv_pool")):
+        _dev(t, torch.bfloat16, name)
+        _need(t.shape == like.shape, f"{name} must have the shape of what it is the gradient of")
+    nbytes = backward_workspace_size(cfg, plan)
+    workspace = _workspace(nbytes, q.device, workspace)
+    p = cfg.c()
+    _check(lib().lazy_attn_prefill_backward(
+        ctypes.byref(p), q.data_ptr(), q_start.data_ptr(), q_pos0.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+        chunks.data_ptr(), chunk_start.data_ptr(), batch, q.shape[0], out.data_ptr(), lse.data_ptr(), dout.data_ptr(),
+        _ptr(dlse), plan.data.data_ptr(), ctypes.byref(plan.info), dq.data_ptr(), dk_pool.data_ptr(),
+        dv_pool.data_ptr(), _ptr(workspace), nbytes, _stream(stream)), "lazy_attn_prefill_backward")
+    return dq, dk_pool, dv_pool
 
 
 def materialize_k(cfg: Config, k_pool, chunks, max_chunk_len: int, total_kv: int, k_out=None, chunks_out=None,
