@@ -300,6 +300,79 @@ LAZY_API int lazy_attn_prefill_backward(const lazy_attn_params_t* params, const 
                                         void* stream);
 
 /*
+ * Eviction from a cache by accumulated attention weight.  Three steps: the weight that queries gave to each key of a
+ * request's table is added up (lazy_attn_prefill_key_weights, lazy_attn_decode_key_weights), the heaviest keys within a
+ * budget are picked (lazy_cache_select), and their K and V are gathered into a record of the request's own
+ * (lazy_cache_compact; the chunk store itself is never changed, other requests may share it).
+ *
+ * Key weights.  Key j of request r (j counts the keys of its table in table order) has its number at
+ * key_start[r] + j of an fp32 array; key_start [batch+1] int32 device, non-decreasing from 0, gives every request room
+ * for key_start[r+1] - key_start[r] keys, which may be more than it has (a growing tail): what lies behind a request's
+ * last key is neither read nor written, and keys without room are passed over.
+ *     weights_j = decay * weights_in_j + sum over the request's query tokens and all query heads of exp(s - lse)
+ * with s the scaled score of the attention entry points (0 for hidden keys and for rows with lse = -inf).  q, q_start,
+ * q_pos0 (q_pos) and lse are what the attention call had and wrote; any rows of a prompt may be given, say its last
+ * ones, as long as q_pos0 is the position of the first of them.
+ *   weights_in  fp32 running sums, or NULL (then decay has no effect); may be the same array as weights
+ *   decay       finite, what the running sums are multiplied by (1: plain accumulation)
+ *   num_keys    size of the weights arrays, key_start[batch] (the prefill form sizes its workspace by it)
+ *   workspace   device scratch of at least ..._workspace_size(...) bytes, 16-byte aligned (may be NULL if 0)
+ * Sums are fp32 in a fixed order: equal calls give equal bits.  num_splits and cache_hint have no effect.
+ */
+LAZY_API int lazy_attn_prefill_key_weights(const lazy_attn_params_t* params, const void* q, const int32_t* q_start,
+                                           const int32_t* q_pos0, const void* k_pool, const lazy_chunk_t* chunks,
+                                           const int32_t* chunk_start, const int32_t* key_start, int32_t batch,
+                                           int32_t total_q, int32_t max_q_len, int32_t max_kv_len, int32_t num_keys,
+                                           const float* lse, const float* weights_in, float decay, float* weights,
+                                           void* workspace, size_t workspace_bytes, void* stream);
+
+LAZY_API size_t lazy_attn_prefill_key_weights_workspace_size(const lazy_attn_params_t* params, int32_t batch,
+                                                             int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
+                                                             int32_t num_keys);
+
+/* One new token per request: q [batch][Hq][D], q_pos [batch], lse [batch][Hq].  Reads K once. */
+LAZY_API int lazy_attn_decode_key_weights(const lazy_attn_params_t* params, const void* q, const int32_t* q_pos,
+                                          const void* k_pool, const lazy_chunk_t* chunks, const int32_t* chunk_start,
+                                          const int32_t* key_start, int32_t batch, int32_t max_kv_len, const float* lse,
+                                          const float* weights_in, float decay, float* weights, void* workspace,
+                                          size_t workspace_bytes, void* stream);
+
+LAZY_API size_t lazy_attn_decode_key_weights_workspace_size(const lazy_attn_params_t* params, int32_t batch,
+                                                            int32_t max_kv_len);
+
+/*
+ * The keys that stay.  Request r has n = key_count[r] keys (NULL: key_start[r+1] - key_start[r]; never more than that)
+ * and keeps b = kept_start[r+1] - kept_start[r] of them, or all n if b > n: its first `sink` and its last `recent` keys
+ * before all others, then by falling weight, NaN last of all, equal ones by rising index.  kept[kept_start[r] ..]
+ * receives their indices j, ascending; entries past n are -1.  max_kv_len bounds the requests' key counts.
+ */
+LAZY_API int lazy_cache_select(const float* weights, const int32_t* key_start, const int32_t* key_count,
+                               const int32_t* kept_start, int32_t batch, int32_t max_kv_len, int32_t sink,
+                               int32_t recent, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
+
+LAZY_API size_t lazy_cache_select_workspace_size(int32_t batch, int32_t max_kv_len);
+
+/*
+ * The kept keys of every request, gathered into one record each: key kept[kept_start[r] + i] becomes key i of the
+ * record dst[r] (device array of [batch] records in k_out / v_out, whose strides are their capacities; len and
+ * pos_offset are not read).  Entries that name no key of the table (-1, or past its end) and entries past the record's
+ * capacity are passed over, their rows left as they were.  Values are copied; keys according to `rotate`:
+ *   0  the new record is used through the same entry points as the old ones: kept keys close up, key i of the record
+ *      sits at dst[r].pos_offset + i.  NoPE (and ALiBi) keys are copied as they are; local-position keys are turned
+ *      from their index in the old record to that in the new one.
+ *   1  keys keep their old positions: they are rotated there, as lazy_materialize_k does, for lazy_plain_attn_prefill
+ *      and lazy_plain_attn_decode.  LAZY_EUNSUPPORTED with LAZY_ALIBI.
+ * max_kept bounds the requests' kept counts.  weights_out (with weights and key_start as above; all three or none)
+ * receives the kept keys' weights at kept_start[r] + i (0 for entries that are passed over).  k_out and v_out may lie
+ * in the pools' own memory (or be the same pointer) as long as no new record overlaps another or what a table reads.
+ */
+LAZY_API int lazy_cache_compact(const lazy_attn_params_t* params, const void* k_pool, const void* v_pool,
+                                const lazy_chunk_t* chunks, const int32_t* chunk_start, int32_t batch,
+                                const int32_t* kept, const int32_t* kept_start, int32_t max_kept,
+                                const lazy_chunk_t* dst, int32_t rotate, void* k_out, void* v_out,
+                                const int32_t* key_start, const float* weights, float* weights_out, void* stream);
+
+/*
  * Materialise-then-attend baseline, step 1 (the re-encoding copy that LazyAttention avoids; Block-Attention's
  * rotate-and-copy path described in the appendix "Experiments Details"): for every record i of every request,
  * write R(pos_offset + j) k_j into k_out, request after request, so that each request's rotated keys form one

@@ -39,6 +39,8 @@ SOURCES = [
     ("lazy_attn_backward.hip", "hip"),
     ("lazy_attn_backward_api.cpp", "hip"),
     ("lazy_attn_backward_plan.cpp", "host"),
+    ("lazy_attn_evict.hip", "hip"),
+    ("lazy_attn_evict_api.cpp", "hip"),
 ]
 
 

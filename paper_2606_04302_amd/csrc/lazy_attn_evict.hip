@@ -1,0 +1,551 @@
+// Eviction by accumulated attention weight for gfx950: key weights of prompts and of single tokens, the selection of the
+// heaviest keys, and the gathering of the kept ones.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "lazy_attn_device.h"
+#include "lazy_attn_internal.h"
+#include "lazy_attn_tiles.h"
+
+namespace lazy {
+namespace {
+
+// A request's 64-key tiles with the index of each tile's first key among the request's keys.
+struct KeyIter : TileIter<kSub> {
+  int base;  // index of the current record's key 0
+  __device__ void start(const lazy_chunk_t* table, int c0, int c1, int split, int splits) {
+    init(table, c0, c1, split, splits);
+    int sum = 0;
+    for (int k = c0 + (threadIdx.x & 63); k < i; k += 64) sum += table[k].len;
+    base = __builtin_amdgcn_readlane(wave_incl_scan(sum), 63);
+  }
+  __device__ void next() {
+    --left;
+    j0 += kSub;
+    while (left > 0 && j0 >= cur.len) {
+      base += cur.len;
+      ++i;
+      j0 = 0;
+      cur = nxt;
+      if (i + 1 < end) nxt = load_rec(recs + i + 1);
+    }
+  }
+  __device__ void skip(int n) {
+    for (int k = 0; k < n && left > 0; ++k) next();
+  }
+};
+
+constexpr int kRowStep = 32;
+constexpr int kPrepTokens = 8;
+
+// Queries rotated, scaled and packed by KV head, and -lse log2 e of each row.
+template <int D, bool IL>
+__global__ __launch_bounds__(256) void prepare_queries(WeightArgs a) {
+  __shared__ float2 cs[kPrepTokens][D / 2];
+  const int first = blockIdx.x * kPrepTokens, tokens = min(kPrepTokens, a.total_q - first);
+  if (a.rotate_q) {
+    for (int e = threadIdx.x; e < tokens * (D / 2); e += 256) {
+      const int t = e % (D / 2), tok = first + e / (D / 2);
+      int lo = 0, hi = a.batch;  // the last request that starts at or before the token (empty ones come before it)
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.q_start[mid] <= tok)
+          lo = mid;
+        else
+          hi = mid;
+      }
+      cs[e / (D / 2)][t] =
+          rope_cs(a.q_pos0[lo] + tok - a.q_start[lo], theta_rev(t, D, a.rope_log2_base, a.inv_freq));
+    }
+    __syncthreads();
+  }
+  constexpr int TPR = D / 16;
+  const int t0 = 8 * (threadIdx.x % TPR);
+  for (int row = threadIdx.x / TPR; row < tokens * a.hq; row += 256 / TPR) {
+    const int tok = row / a.hq, h = row % a.hq;
+    const int64_t src = (int64_t)(first + tok) * a.hq + h;
+    const int64_t dst = (int64_t)(h / a.group) * a.rows + (int64_t)(first + tok) * a.group + h % a.group;
+    u32x4 lo, hi;
+    load_pairs<D, IL>(a.q + src * D, t0, lo, hi);
+    float yl[8], yh[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      yl[e] = element(lo, e);
+      yh[e] = element(hi, e);
+      if (a.rotate_q) rotate_by(element(lo, e), element(hi, e), cs[tok][t0 + e], yl[e], yh[e]);
+      yl[e] *= a.scale_log2;
+      yh[e] *= a.scale_log2;
+    }
+    store_pairs<D, false>(a.ws_q + dst * D, t0, yl, yh);
+    if (t0 == 0) {
+      const float lse = a.lse[src];
+      a.ws_nlse[dst] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
+    }
+  }
+}
+
+// Weights of a prompt: workgroup (key split and row split, KV head, request), four waves with a 64-key tile each, whose
+// rotated keys stay in registers while the rows of the request pass through LDS.  S = Q K^T has a key in every lane and
+// 32 rows in registers and lane halves, so a key's sum never leaves its lane.
+template <int D, int KMI>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void weigh_prompt(WeightArgs a) {
+  constexpr int KM = keys_of(KMI);
+  constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
+  constexpr int C = D / 8;
+  __shared__ uint16_t tq[kRowStep * D] __attribute__((aligned(16)));
+  __shared__ float nlse[kRowStep] __attribute__((aligned(16)));
+  __shared__ int rpos[kRowStep] __attribute__((aligned(16)));
+  __shared__ float rslope[kRowStep] __attribute__((aligned(16)));
+  __shared__ double freq[D / 2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), h2 = lane >> 5;
+  const int r = blockIdx.z, g = blockIdx.y, split = blockIdx.x % a.splits, rs = blockIdx.x / a.splits;
+  const int qs = a.q_start[r], nrows = (a.q_start[r + 1] - qs) * a.group, shift = a.q_pos0[r] - qs;
+  const int steps = (nrows + kRowStep - 1) / kRowStep;
+  const int row_begin = qs * a.group + (int)((int64_t)steps * rs / a.row_splits) * kRowStep;
+  const int row_end = qs * a.group + min(nrows, (int)((int64_t)steps * (rs + 1) / a.row_splits) * kRowStep);
+  const int room = a.key_start[r + 1] - a.key_start[r];
+  if (ROT && tid < D / 2) freq[tid] = theta_rev(tid, D, a.rope_log2_base, a.inv_freq);
+  KeyIter it;
+  it.start(a.chunks, a.chunk_start[r], a.chunk_start[r + 1], split, a.splits);
+  const int rounds = (it.left + 3) / 4;
+  it.skip(wave);
+  __syncthreads();
+  const uint16_t* qbase = a.ws_q + (int64_t)g * a.rows * D;
+  float* part = a.ws_part + (int64_t)(rs * a.hkv + g) * a.num_keys + a.key_start[r];
+  for (int round = 0; round < rounds; ++round) {
+    const bool have = it.left > 0;
+    const int nvalid = have ? min(kSub, it.cur.len - it.j0) : 0, b0 = have ? it.cur.pos + it.j0 : 0;
+    bf16x8 kf[2][D / 16];
+    float acc[2] = {0.f, 0.f};
+    if (have) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int key = 32 * b + (lane & 31);
+        load_keys<D, KM, IL>(k_ptr(a.k_pool, it.cur, g, it.j0 + min(key, nvalid - 1), D), h2,
+                             LOCAL ? it.cur.pos : b0 + key, freq, kf[b]);
+      }
+    }
+    for (int row0 = row_begin; row0 < row_end; row0 += kRowStep) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kRowStep * C / 256; ++i) {
+        const int e = 256 * i + tid, row = e / C, chunk = e % C;
+        *reinterpret_cast<u32x4*>(tq + tile_at<D>(row, chunk)) = *reinterpret_cast<const u32x4*>(
+            qbase + (int64_t)min(row0 + row, row_end - 1) * D + 8 * chunk);
+      }
+      if (tid < kRowStep) {
+        const int src = row0 + tid, tok = token_of(src, a.group_magic);
+        nlse[tid] = src < row_end ? a.ws_nlse[(int64_t)g * a.rows + src] : -INFINITY;
+        rpos[tid] = tok + shift;
+        if (ALIBI) rslope[tid] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
+      }
+      __syncthreads();
+      const int qmin = token_of(row0, a.group_magic) + shift;
+      const int qmax = token_of(min(row0 + kRowStep, row_end) - 1, a.group_magic) + shift;
+      if (!have || (a.causal && b0 > qmax)) continue;
+      f32x16 s[2];
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(nlse + 8 * q4 + 4 * h2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[0][4 * q4 + e] = s[1][4 * q4 + e] = x[e];
+      }
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        const bf16x8 fq = row_operand<D>(tq, lane & 31, k, h2);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq, kf[b][k], s[b], 0, 0, 0);
+      }
+      const bool masked = a.causal && b0 + kSub - 1 > qmin;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int p = b0 + 32 * b + (lane & 31);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
+          if (ALIBI) s[b][i] = fmaf(rslope[row], (float)(p - rpos[row]), s[b][i]);
+          s[b][i] = fast_exp2(s[b][i]);
+          if (masked) s[b][i] = p <= rpos[row] ? s[b][i] : 0.f;
+          acc[b] += s[b][i];
+        }
+      }
+    }
+    if (have) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int key = 32 * b + (lane & 31), at = it.base + it.j0 + key;
+        const float sum = xor32_sum(acc[b]);
+        if (h2 == 0 && key < nvalid && at < room) part[at] = sum;
+      }
+    }
+    it.skip(4);
+  }
+}
+
+// Partial sums of the row splits and KV heads added up in their order.  Keys behind the table's last one are left alone.
+__global__ __launch_bounds__(256) void sum_weights(WeightArgs a) {
+  __shared__ int total[4];
+  const int r = blockIdx.y, tid = threadIdx.x;
+  int n = 0;
+  for (int k = a.chunk_start[r] + tid; k < a.chunk_start[r + 1]; k += 256) n += a.chunks[k].len;
+  n = wave_incl_scan(n);
+  if ((tid & 63) == 63) total[tid >> 6] = n;
+  __syncthreads();
+  n = min(total[0] + total[1] + total[2] + total[3], a.key_start[r + 1] - a.key_start[r]);
+  for (int j = blockIdx.x * 256 + tid; j < n; j += gridDim.x * 256) {
+    const int64_t at = (int64_t)a.key_start[r] + j;
+    float w = 0.f;
+    for (int p = 0; p < a.row_splits * a.hkv; ++p) w += a.ws_part[(int64_t)p * a.num_keys + at];
+    a.weights[at] = a.weights_in ? fmaf(a.decay, a.weights_in[at], w) : w;
+  }
+}
+
+// Weights of one new token per request: workgroup (key split, request), a wave takes 16 keys of each 64-key tile for all
+// heads, so that their angles are formed once and their sums stay in the wave.  Rotated queries lie in LDS, kRowGroups
+// groups of 16 rows (query heads of one KV head) at a time.  S = Q K^T: a key in lane % 16, rows 4 (lane / 16) + 0..3.
+constexpr int kRowGroups = 8;
+template <int D, int KMI>
+__global__ __launch_bounds__(256) void weigh_token(WeightArgs a) {
+  constexpr int KM = keys_of(KMI);
+  constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
+  constexpr int QLD = D + kPad, H = D / 64;
+  __shared__ uint16_t q[kRowGroups * 16 * QLD] __attribute__((aligned(16)));
+  __shared__ float nlse[kRowGroups * 16] __attribute__((aligned(16)));
+  __shared__ float rslope[kRowGroups * 16] __attribute__((aligned(16)));
+  __shared__ double freq[D / 2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, kq = lane >> 4;
+  const int r = blockIdx.y, qpos = a.q_pos0[r], room = a.key_start[r + 1] - a.key_start[r];
+  if (ROT && tid < D / 2) freq[tid] = theta_rev(tid, D, a.rope_log2_base, a.inv_freq);
+  const int per_head = (a.group + 15) / 16, groups = a.hkv * per_head;
+  for (int g0 = 0; g0 < groups; g0 += kRowGroups) {
+    const int ng = min(kRowGroups, groups - g0);
+    __syncthreads();
+    constexpr int TPR = D / 16;
+    for (int e = tid; e < ng * 16 * TPR; e += 256) {
+      const int row = e / TPR, t0 = 8 * (e % TPR), grp = g0 + row / 16, in = (grp % per_head) * 16 + row % 16;
+      const bool ok = in < a.group;
+      const int h = (grp / per_head) * a.group + (ok ? in : 0);
+      u32x4 lo, hi;
+      load_pairs<D, IL>(a.q + ((int64_t)r * a.hq + h) * D, t0, lo, hi);
+      float yl[8], yh[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        yl[k] = element(lo, k);
+        yh[k] = element(hi, k);
+        if (a.rotate_q) rotate_by(element(lo, k), element(hi, k), rope_cs(qpos, freq[t0 + k]), yl[k], yh[k]);
+        yl[k] *= a.scale_log2;
+        yh[k] *= a.scale_log2;
+      }
+      store_pairs<D, false>(q + row * QLD, t0, yl, yh);
+      if (t0 == 0) {
+        const float lse = a.lse[(int64_t)r * a.hq + h];
+        nlse[row] = !ok || lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
+        rslope[row] = ALIBI ? alibi_slope(h, a.hq, a.inv_freq, 1.f) : 0.f;
+      }
+    }
+    __syncthreads();
+    KeyIter it;
+    it.start(a.chunks, a.chunk_start[r], a.chunk_start[r + 1], blockIdx.x, a.splits);
+    for (; it.left > 0; it.next()) {
+      const int key = it.j0 + 16 * wave + col;
+      const bool in = key < it.cur.len;
+      const int p = it.cur.pos + key;
+      float2 cs[H][8];
+      if (ROT) {
+#pragma unroll
+        for (int s = 0; s < H; ++s)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) cs[s][e] = rope_cs(LOCAL ? it.cur.pos : p, freq[32 * s + 8 * kq + e]);
+      }
+      float sum = 0.f;
+      for (int k = 0; k < ng; ++k) {
+        const uint16_t* krow = k_ptr(a.k_pool, it.cur, (g0 + k) / per_head, in ? key : it.j0, D);
+        bf16x8 kf[2 * H];
+#pragma unroll
+        for (int s = 0; s < H; ++s) {
+          u32x4 lo, hi;
+          load_pairs<D, IL>(krow, 32 * s + 8 * kq, lo, hi);
+          if (ROT) {
+            float yl[8], yh[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rotate_by(element(lo, e), element(hi, e), cs[s][e], yl[e], yh[e]);
+            lo = pack8(yl);
+            hi = pack8(yh);
+          }
+          kf[s] = as_bf16x8(lo);
+          kf[s + H] = as_bf16x8(hi);
+        }
+        f32x4 s4 = *reinterpret_cast<const f32x4*>(nlse + 16 * k + 4 * kq);
+#pragma unroll
+        for (int s = 0; s < 2 * H; ++s)
+          s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              as_bf16x8(*reinterpret_cast<const u32x4*>(q + (16 * k + col) * QLD + 32 * s + 8 * kq)), kf[s], s4, 0, 0,
+              0);
+        if (ALIBI) {
+          const f32x4 sl = *reinterpret_cast<const f32x4*>(rslope + 16 * k + 4 * kq);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s4[e] = fmaf(sl[e], (float)(p - qpos), s4[e]);
+        }
+        sum += (fast_exp2(s4[0]) + fast_exp2(s4[1])) + (fast_exp2(s4[2]) + fast_exp2(s4[3]));
+      }
+      sum += __shfl_xor(sum, 16, 64);
+      sum += __shfl_xor(sum, 32, 64);
+      if (a.causal && p > qpos) sum = 0.f;
+      const int at = it.base + key;
+      if (kq == 0 && in && at < room) {
+        float* w = a.weights + a.key_start[r] + at;
+        if (g0 > 0)
+          *w += sum;
+        else
+          *w = a.weights_in ? fmaf(a.decay, a.weights_in[a.key_start[r] + at], sum) : sum;
+      }
+    }
+  }
+}
+
+// Selection: a radix select of the b-th largest score and an ordered compaction, one workgroup a request.
+// Scores as integers in their order: NaN lowest, -0 like 0, protected keys above all.
+constexpr int kSelectThreads = 1024;
+__device__ __forceinline__ uint32_t score_of(float w, int j, int n, int sink, int recent) {
+  if (j < sink || j >= n - recent) return 0xffffffffu;
+  if (w != w) return 0;
+  const uint32_t u = __float_as_uint(w + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__global__ __launch_bounds__(kSelectThreads) void select_keys(const float* weights, const int32_t* key_start,
+                                                              const int32_t* key_count, const int32_t* kept_start,
+                                                              int sink, int recent, int32_t* kept) {
+  constexpr int kWaves = kSelectThreads / 64;
+  __shared__ int hist[256];
+  __shared__ uint32_t prefix_s;
+  __shared__ int need_s;
+  __shared__ int above[kWaves], equal[kWaves];
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int k0 = key_start[r], room = key_start[r + 1] - k0;
+  const int n = key_count ? max(0, min(key_count[r], room)) : room;
+  const int o0 = kept_start[r], b = kept_start[r + 1] - o0;
+  const float* w = weights + k0;
+  if (b >= n) {
+    for (int i = tid; i < b; i += kSelectThreads) kept[o0 + i] = i < n ? i : -1;
+    return;
+  }
+  if (b <= 0) return;
+  // The b-th largest score, eight bits at a time: `prefix` its bits so far, `need` its rank among the scores with them.
+  uint32_t prefix = 0;
+  int need = b;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+    for (int j = tid; j < n; j += kSelectThreads) {
+      const uint32_t s = score_of(w[j], j, n, sink, recent);
+      if (shift == 24 || s >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[s >> shift & 255], 1);
+    }
+    __syncthreads();
+    if (tid < 64) {  // lane l holds digits 255 - 4 l .. 252 - 4 l, so the scan counts from the largest
+      int c[4], sum = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += c[e] = hist[255 - 4 * tid - e];
+      int before = wave_incl_scan(sum) - sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (before < need && need <= before + c[e]) {
+          prefix_s = prefix | (uint32_t)(255 - 4 * tid - e) << shift;
+          need_s = need - before;
+        }
+        before += c[e];
+      }
+    }
+    __syncthreads();
+    prefix = prefix_s;
+    need = need_s;
+  }
+  // Every wave counts, then writes, the keys of a contiguous part: all above the threshold, and the first `need` equal
+  // to it.
+  const int per = ((n + kWaves - 1) / kWaves + 63) & ~63, j0 = min(n, wave * per), j1 = min(n, j0 + per);
+  int na = 0, ne = 0;
+  for (int j = j0 + lane; j - lane < j1; j += 64) {
+    const uint32_t s = j < j1 ? score_of(w[j], j, n, sink, recent) : 0;
+    na += __builtin_popcountll(__ballot(j < j1 && s > prefix));
+    ne += __builtin_popcountll(__ballot(j < j1 && s == prefix));
+  }
+  if (lane == 0) {
+    above[wave] = na;
+    equal[wave] = ne;
+  }
+  __syncthreads();
+  na = ne = 0;
+  for (int k = 0; k < wave; ++k) {
+    na += above[k];
+    ne += equal[k];
+  }
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  for (int j = j0 + lane; j - lane < j1; j += 64) {
+    const uint32_t s = j < j1 ? score_of(w[j], j, n, sink, recent) : 0;
+    const uint64_t ma = __ballot(j < j1 && s > prefix), me = __ballot(j < j1 && s == prefix);
+    const int ra = na + __builtin_popcountll(ma & below), re = ne + __builtin_popcountll(me & below);
+    if ((ma >> lane & 1) || ((me >> lane & 1) && re < need)) kept[o0 + ra + min(re, need)] = j;
+    na += __builtin_popcountll(ma);
+    ne += __builtin_popcountll(me);
+  }
+}
+
+// Gather of kept keys: workgroup (64 kept keys, KV head, request).  The records that hold them are found by prefix sums
+// over the request's table, 256 records at a time.
+constexpr int kGather = 64;
+template <int D, int TURN, bool LOCAL, bool IL>
+__global__ __launch_bounds__(256) void gather_keys(CompactArgs a) {
+  __shared__ int ends[256], wsum[4];
+  __shared__ int64_t ksrc[kGather], vsrc[kGather];
+  __shared__ int turn[kGather];
+  __shared__ double freq[D / 2];
+  const int r = blockIdx.z, g = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int o0 = a.kept_start[r], count = a.kept_start[r + 1] - o0, i0 = blockIdx.x * kGather;
+  if (i0 >= count) return;
+  const int i = i0 + tid;  // threads 0 .. 63: one kept key each
+  int want = tid < kGather && i < count ? a.kept[o0 + i] : -1;
+  const int asked = want;
+  if (tid < kGather) ksrc[tid] = -1;
+  if (TURN && tid < D / 2) freq[tid] = theta_rev(tid, D, a.rope_log2_base, a.inv_freq);
+  const lazy_chunk_t dst = a.dst[r];
+  int base = 0;
+  for (int c0 = a.chunk_start[r]; c0 < a.chunk_start[r + 1]; c0 += 256) {
+    const int nrec = min(256, a.chunk_start[r + 1] - c0);
+    const int incl = wave_incl_scan(tid < nrec ? a.chunks[c0 + tid].len : 0);
+    if (lane == 63) wsum[wave] = incl;
+    __syncthreads();
+    int before = base;
+    for (int w = 0; w < wave; ++w) before += wsum[w];
+    ends[tid] = before + incl;
+    base += wsum[0] + wsum[1] + wsum[2] + wsum[3];
+    __syncthreads();
+    if (want >= 0 && want < base) {
+      int lo = 0, hi = nrec - 1;  // the first record that ends past the key
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (ends[mid] > want)
+          hi = mid;
+        else
+          lo = mid + 1;
+      }
+      const lazy_chunk_t c = a.chunks[c0 + lo];
+      const int j = want - (ends[lo] - c.len);
+      ksrc[tid] = c.k_offset + ((int64_t)g * c.k_stride + j) * D;
+      vsrc[tid] = c.v_offset + ((int64_t)g * c.v_stride + j) * D;
+      turn[tid] = TURN == 2 ? i - j : LOCAL ? c.pos_offset : c.pos_offset + j;
+      want = -1;
+    }
+  }
+  __syncthreads();
+  if (a.weights_out && g == 0 && tid < kGather && i < count)
+    a.weights_out[o0 + i] = ksrc[tid] >= 0 ? a.weights[(int64_t)a.key_start[r] + asked] : 0.f;
+  constexpr int TPR = D / 16;
+  const int t0 = 8 * (tid % TPR);
+  for (int row = tid / TPR; row < kGather; row += 256 / TPR) {
+    const int at = i0 + row;
+    if (at >= count || ksrc[row] < 0 || at >= dst.k_stride || at >= dst.v_stride) continue;
+    const uint16_t* ks = a.k_pool + ksrc[row];
+    const uint16_t* vs = a.v_pool + vsrc[row];
+    uint16_t* kd = a.k_out + dst.k_offset + ((int64_t)g * dst.k_stride + at) * D;
+    uint16_t* vd = a.v_out + dst.v_offset + ((int64_t)g * dst.v_stride + at) * D;
+    if (TURN) {
+      u32x4 lo, hi;
+      load_pairs<D, IL>(ks, t0, lo, hi);
+      float yl[8], yh[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        rotate_by(element(lo, e), element(hi, e), rope_cs(turn[row], freq[t0 + e]), yl[e], yh[e]);
+      store_pairs<D, IL>(kd, t0, yl, yh);
+    } else {
+      reinterpret_cast<u32x4*>(kd + 2 * t0)[0] = reinterpret_cast<const u32x4*>(ks + 2 * t0)[0];
+      reinterpret_cast<u32x4*>(kd + 2 * t0)[1] = reinterpret_cast<const u32x4*>(ks + 2 * t0)[1];
+    }
+    reinterpret_cast<u32x4*>(vd + 2 * t0)[0] = reinterpret_cast<const u32x4*>(vs + 2 * t0)[0];
+    reinterpret_cast<u32x4*>(vd + 2 * t0)[1] = reinterpret_cast<const u32x4*>(vs + 2 * t0)[1];
+  }
+}
+
+template <int D, int KMI>
+hipError_t prompt_mode(const WeightArgs& a, int max_kv_len, hipStream_t s) {
+  if (a.total_q > 0)
+    prepare_queries<D, interleaved_of(KMI)><<<(a.total_q + kPrepTokens - 1) / kPrepTokens, 256, 0, s>>>(a);
+  weigh_prompt<D, KMI><<<dim3(a.splits * a.row_splits, a.hkv, a.batch), 256, 0, s>>>(a);
+  sum_weights<<<dim3((max_kv_len + 255) / 256, a.batch), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <int D, int KMI>
+hipError_t token_mode(const WeightArgs& a, hipStream_t s) {
+  weigh_token<D, KMI><<<dim3(a.splits, a.batch), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int D, int TURN>
+void compact_mode(const CompactArgs& a, dim3 grid, bool local_keys, bool interleaved, hipStream_t s) {
+  if (local_keys) {
+    if (interleaved)
+      gather_keys<D, TURN, true, true><<<grid, 256, 0, s>>>(a);
+    else
+      gather_keys<D, TURN, true, false><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (interleaved)
+      gather_keys<D, TURN, false, true><<<grid, 256, 0, s>>>(a);
+    else
+      gather_keys<D, TURN, false, false><<<grid, 256, 0, s>>>(a);
+  }
+}
+
+}  // namespace
+
+#define LAZY_KEY_MODES(CALL)                                              \
+  if (alibi) return CALL(kKeysAlibi);                                     \
+  if (local_keys) {                                                       \
+    if (interleaved) return CALL(kKeysLocal | kInterleaved);              \
+    return CALL(kKeysLocal);                                              \
+  }                                                                       \
+  if (interleaved) return CALL(kKeysNope | kInterleaved);                 \
+  return CALL(kKeysNope);
+
+hipError_t launch_prefill_weights(const WeightArgs& a, int head_dim, bool local_keys, bool interleaved, bool alibi,
+                                  int max_kv_len, hipStream_t s) {
+#define CALL(KM) (head_dim == 64 ? prompt_mode<64, KM>(a, max_kv_len, s) : prompt_mode<128, KM>(a, max_kv_len, s))
+  LAZY_KEY_MODES(CALL)
+#undef CALL
+}
+
+hipError_t launch_decode_weights(const WeightArgs& a, int head_dim, bool local_keys, bool interleaved, bool alibi,
+                                 hipStream_t s) {
+#define CALL(KM) (head_dim == 64 ? token_mode<64, KM>(a, s) : token_mode<128, KM>(a, s))
+  LAZY_KEY_MODES(CALL)
+#undef CALL
+}
+
+hipError_t launch_select(const float* weights, const int32_t* key_start, const int32_t* key_count,
+                         const int32_t* kept_start, int batch, int sink, int recent, int32_t* kept, hipStream_t s) {
+  select_keys<<<batch, kSelectThreads, 0, s>>>(weights, key_start, key_count, kept_start, sink, recent, kept);
+  return hipGetLastError();
+}
+
+hipError_t launch_compact(const CompactArgs& a, int head_dim, int batch, int max_kept, int turn, bool local_keys,
+                          bool interleaved, hipStream_t s) {
+  const dim3 grid((max_kept + kGather - 1) / kGather, a.hkv, batch);
+  if (turn == 0) {
+    if (head_dim == 64)
+      gather_keys<64, 0, false, false><<<grid, 256, 0, s>>>(a);
+    else
+      gather_keys<128, 0, false, false><<<grid, 256, 0, s>>>(a);
+  } else if (turn == 1) {
+    if (head_dim == 64)
+      compact_mode<64, 1>(a, grid, local_keys, interleaved, s);
+    else
+      compact_mode<128, 1>(a, grid, local_keys, interleaved, s);
+  } else {
+    if (head_dim == 64)
+      compact_mode<64, 2>(a, grid, true, interleaved, s);
+    else
+      compact_mode<128, 2>(a, grid, true, interleaved, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace lazy

@@ -110,6 +110,57 @@ struct GradArgs {
   float scale_log2;
 };
 
+// Arguments of the key-weight kernels (prompt rows packed by KV head as for the backward pass).
+struct WeightArgs {
+  const uint16_t* q;          // [total_q][hq][D]
+  const int32_t* q_start;     // decode: null
+  const int32_t* q_pos0;
+  const uint16_t* k_pool;
+  const lazy_chunk_t* chunks;
+  const int32_t* chunk_start;
+  const int32_t* key_start;
+  const float* lse;           // [total_q][hq]
+  const float* weights_in;    // or null
+  float* weights;
+  uint16_t* ws_q;             // [hkv][rows][D] rotated queries times scale * log2 e
+  float* ws_nlse;             // [hkv][rows] -lse log2 e
+  float* ws_part;             // [row_splits * hkv][num_keys] partial sums
+  const float* inv_freq;
+  int64_t rows;
+  int32_t total_q;
+  int32_t batch;
+  int32_t hq;
+  int32_t hkv;
+  int32_t group;
+  uint32_t group_magic;
+  int32_t causal;
+  int32_t rotate_q;
+  int32_t splits;             // key splits of a request
+  int32_t row_splits;
+  int32_t num_keys;
+  float decay;
+  double rope_log2_base;
+  float scale_log2;
+};
+
+struct CompactArgs {
+  const uint16_t* k_pool;
+  const uint16_t* v_pool;
+  const lazy_chunk_t* chunks;
+  const int32_t* chunk_start;
+  const int32_t* kept;
+  const int32_t* kept_start;
+  const lazy_chunk_t* dst;
+  uint16_t* k_out;
+  uint16_t* v_out;
+  const int32_t* key_start;   // the last three together or null
+  const float* weights;
+  float* weights_out;
+  const float* inv_freq;
+  int32_t hkv;
+  double rope_log2_base;
+};
+
 // Packed rows (token, head in group) handled by one prefill workgroup, and keys per decode tile.
 constexpr int kPrefillRowsPerBlock = 128;  // packed rows of a prefill workgroup per row block
 constexpr int kPrefillTileKeys = 64;
@@ -125,6 +176,15 @@ hipError_t launch_decode_shared(const SharedArgs& a, int num_items, int max_slot
 hipError_t noalloc_scratch(int device, void** ptr);
 hipError_t launch_backward(const GradArgs& a, int head_dim, bool local_keys, bool interleaved, bool alibi,
                            const lazy_backward_info_t& info, hipStream_t stream);
+hipError_t launch_prefill_weights(const WeightArgs& a, int head_dim, bool local_keys, bool interleaved, bool alibi,
+                                  int max_kv_len, hipStream_t stream);
+hipError_t launch_decode_weights(const WeightArgs& a, int head_dim, bool local_keys, bool interleaved, bool alibi,
+                                 hipStream_t stream);
+hipError_t launch_select(const float* weights, const int32_t* key_start, const int32_t* key_count,
+                         const int32_t* kept_start, int batch, int sink, int recent, int32_t* kept, hipStream_t stream);
+// turn: 0 keys are copied, 1 rotated to their positions, 2 turned from their old local index to the new one.
+hipError_t launch_compact(const CompactArgs& a, int head_dim, int batch, int max_kept, int turn, bool local_keys,
+                          bool interleaved, hipStream_t stream);
 hipError_t launch_combine(const uint16_t* part_o, const float* part_lse, int splits, int rows, int head_dim,
                           uint16_t* out, float* lse, hipStream_t stream);
 hipError_t launch_materialize(const uint16_t* k_pool, const lazy_chunk_t* chunks, int num_records,

@@ -1,0 +1,93 @@
+// Device code of the kernels that recompute attention probabilities (backward pass, key weights): unpadded tiles in LDS
+// and matrix operands with the head dimension in half-split order.
+#pragma once
+
+#include "lazy_attn_device.h"
+
+namespace lazy {
+namespace {
+
+// Tiles in LDS: rows of D bf16, unpadded (a row of 64 or 32 banks), whose 16-byte chunks are permuted: chunk c of row r
+// lies at place c ^ swizzle(r).  Two kinds of reads are conflict free then: rows by 16 lanes of consecutive rows (one
+// chunk each: swizzle takes as many values as there are chunks over the rows that share banks) and transposing reads,
+// whose passes cover four chunks 4 b .. 4 b + 3 of four consecutive rows (rows that share banks differ in the bits of
+// swizzle that select b).
+template <int D>
+__device__ __forceinline__ int swizzle(int r) {
+  return D == 128 ? ((r & 3) << 2 | (r >> 2 & 3)) : ((r >> 1 & 1) << 2 | (r >> 2 & 3));
+}
+template <int D>
+__device__ __forceinline__ int tile_at(int row, int chunk) {
+  return row * D + 8 * (chunk ^ swizzle<D>(row));
+}
+// Operand of row `row`, elements 16 s + 8 h2 .. + 7.
+template <int D>
+__device__ __forceinline__ bf16x8 row_operand(const uint16_t* tile, int row, int s, int h2) {
+  return as_bf16x8(*reinterpret_cast<const u32x4*>(tile + tile_at<D>(row, 2 * s + h2)));
+}
+// Transposed operand: element column 32 db + lane % 32 of rows row0 + {0..3, 8..11} + 4 (lane / 32): the rows that
+// registers 8 k .. 8 k + 7 of a 32x32 product's accumulator hold for this lane half (row0 = 16 k).
+template <int D>
+__device__ __forceinline__ bf16x8 column_operand(const uint16_t* tile, int row0, int db, int lane) {
+  const int i = lane & 15, grp = lane >> 4;
+  const int row = row0 + 4 * (grp >> 1) + (i >> 2), chunk = 4 * db + 2 * (grp & 1) + ((i & 3) >> 1), half = 4 * (i & 1);
+  const u32x2 lo = tr_read(tile + tile_at<D>(row, chunk) + half);
+  const u32x2 hi = tr_read(tile + tile_at<D>(row + 8, chunk) + half);
+  return as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
+}
+
+// Packed row -> token: row / G by multiplication (total_q * G * G < 2^32, checked by the planner).
+__device__ __forceinline__ int token_of(int row, uint32_t magic) { return magic ? (int)__umulhi(row, magic) : row; }
+
+// Eight pairs t0 .. t0 + 7 of a vector in global memory: first elements lo, second elements hi.
+template <int D, bool IL>
+__device__ __forceinline__ void load_pairs(const uint16_t* v, int t0, u32x4& lo, u32x4& hi) {
+  if (IL) {
+    const u32x4* src = reinterpret_cast<const u32x4*>(v + 2 * t0);
+    const u32x4 a = src[0], b = src[1];
+    deinterleave8(a, b, lo, hi);
+  } else {
+    lo = *reinterpret_cast<const u32x4*>(v + t0);
+    hi = *reinterpret_cast<const u32x4*>(v + D / 2 + t0);
+  }
+}
+__device__ __forceinline__ float element(const u32x4& v, int e) { return (e & 1) ? bf_hi(v[e >> 1]) : bf_lo(v[e >> 1]); }
+__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
+  return u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+}
+template <int D, bool IL>
+__device__ __forceinline__ void store_pairs(uint16_t* v, int t0, const float (&lo)[8], const float (&hi)[8]) {
+  if (IL) {
+    const float a[8] = {lo[0], hi[0], lo[1], hi[1], lo[2], hi[2], lo[3], hi[3]};
+    const float b[8] = {lo[4], hi[4], lo[5], hi[5], lo[6], hi[6], lo[7], hi[7]};
+    reinterpret_cast<u32x4*>(v + 2 * t0)[0] = pack8(a);
+    reinterpret_cast<u32x4*>(v + 2 * t0)[1] = pack8(b);
+  } else {
+    *reinterpret_cast<u32x4*>(v + t0) = pack8(lo);
+    *reinterpret_cast<u32x4*>(v + D / 2 + t0) = pack8(hi);
+  }
+}
+
+// Rotates the raw key operands of a 32-key block to their positions.  Lane: key lane % 32 of the block, elements
+// 16 s + 8 h2 .. + 7 of operand s; its pairs lie in operand s + D / 32.
+template <int D, int KM, bool IL>
+__device__ __forceinline__ void load_keys(const uint16_t* krow, int h2, int p, const double* freq, bf16x8 (&kf)[D / 16]) {
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    const int t0 = 16 * s + 8 * h2;
+    u32x4 lo, hi;
+    load_pairs<D, IL>(krow, t0, lo, hi);
+    if (KM == kKeysNope || KM == kKeysLocal) {
+      float yl[8], yh[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) rotate_by(element(lo, e), element(hi, e), rope_cs(p, freq[t0 + e]), yl[e], yh[e]);
+      lo = pack8(yl);
+      hi = pack8(yh);
+    }
+    kf[s] = as_bf16x8(lo);
+    kf[s + D / 32] = as_bf16x8(hi);
+  }
+}
+
+}  // namespace
+}  // namespace lazy

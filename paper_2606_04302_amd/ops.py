@@ -88,6 +88,18 @@ SIGNATURES = {
     "lazy_attn_prefill_backward": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p,
                                             _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_p, _c_p,
                                             ctypes.POINTER(BackwardInfo), _c_p, _c_p, _c_p, _c_p, _c_sz, _c_p]),
+    "lazy_attn_prefill_key_weights": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_p, _c_p,
+                                               _c_p, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_p, _c_f32, _c_p,
+                                               _c_p, _c_sz, _c_p]),
+    "lazy_attn_prefill_key_weights_workspace_size": (_c_sz, [ctypes.POINTER(LazyAttnParams), _c_i32, _c_i32, _c_i32,
+                                                             _c_i32, _c_i32]),
+    "lazy_attn_decode_key_weights": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_p, _c_p,
+                                              _c_i32, _c_i32, _c_p, _c_p, _c_f32, _c_p, _c_p, _c_sz, _c_p]),
+    "lazy_attn_decode_key_weights_workspace_size": (_c_sz, [ctypes.POINTER(LazyAttnParams), _c_i32, _c_i32]),
+    "lazy_cache_select": (_c_i32, [_c_p, _c_p, _c_p, _c_p, _c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_p, _c_sz, _c_p]),
+    "lazy_cache_select_workspace_size": (_c_sz, [_c_i32, _c_i32]),
+    "lazy_cache_compact": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_i32, _c_p, _c_p, _c_i32,
+                                    _c_p, _c_i32, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p]),
     "lazy_materialize_k": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_i32, _c_i32, _c_i64, _c_p, _c_p,
                                     _c_p]),
     "lazy_attn_validate": (_c_i32, [ctypes.POINTER(LazyAttnParams), _c_p, _c_p, _c_p, _c_p, _c_i32, _c_i64, _c_i64,
@@ -419,6 +431,123 @@ def prefill_backward(cfg: Config, q, q_start, q_pos0, k_pool, v_pool, chunks, ch
         _ptr(dlse), plan.data.data_ptr(), ctypes.byref(plan.info), dq.data_ptr(), dk_pool.data_ptr(),
         dv_pool.data_ptr(), _ptr(workspace), nbytes, _stream(stream)), "lazy_attn_prefill_backward")
     return dq, dk_pool, dv_pool
+
+
+def prefill_key_weights_workspace_size(cfg: Config, batch: int, total_q: int, max_q_len: int, max_kv_len: int,
+                                       num_keys: int) -> int:
+    p = cfg.c()
+    return int(lib().lazy_attn_prefill_key_weights_workspace_size(ctypes.byref(p), batch, total_q, max_q_len,
+                                                                  max_kv_len, num_keys))
+
+
+def decode_key_weights_workspace_size(cfg: Config, batch: int, max_kv_len: int) -> int:
+    p = cfg.c()
+    return int(lib().lazy_attn_decode_key_weights_workspace_size(ctypes.byref(p), batch, max_kv_len))
+
+
+def _weight_args(cfg, q, q_pos, k_pool, chunks, chunk_start, key_start, batch, lse, weights, weights_in):
+    _dev(q, torch.bfloat16, "q")
+    _dev(k_pool, torch.bfloat16, "k_pool")
+    for t, name in ((q_pos, "query positions"), (chunk_start, "chunk_start"), (key_start, "key_start")):
+        _dev(t, torch.int32, name)
+    _chunks(chunks)
+    _need(q.dim() == 3 and q.shape[1] == cfg.num_q_heads and q.shape[2] == cfg.head_dim, "q must be [T, Hq, D]")
+    _need(chunk_start.numel() == batch + 1 and key_start.numel() == batch + 1 and q_pos.numel() == batch,
+          "table sizes disagree with the batch")
+    _dev(lse, torch.float32, "lse")
+    _need(lse.shape == q.shape[:2], "lse must be [T, Hq]")
+    _dev(weights, torch.float32, "weights")
+    _need(weights.dim() == 1, "weights must be one-dimensional")
+    if weights_in is not None:
+        _dev(weights_in, torch.float32, "weights_in")
+        _need(weights_in.shape == weights.shape, "weights_in must have the shape of weights")
+
+
+def prefill_key_weights(cfg: Config, q, q_start, q_pos0, k_pool, chunks, chunk_start, key_start, max_q_len: int,
+                        max_kv_len: int, lse, weights, weights_in=None, decay: float = 1.0, workspace=None,
+                        stream=None):
+    """lazy_attn_prefill_key_weights: the attention weight that a prompt's rows gave to each key of their tables, into
+    ``weights`` [key_start[-1]] fp32 (plus decay * weights_in).  Returns weights."""
+    batch = q_start.numel() - 1
+    _dev(q_start, torch.int32, "q_start")
+    _weight_args(cfg, q, q_pos0, k_pool, chunks, chunk_start, key_start, batch, lse, weights, weights_in)
+    nbytes = prefill_key_weights_workspace_size(cfg, batch, q.shape[0], max_q_len, max_kv_len, weights.numel())
+    workspace = _workspace(nbytes, q.device, workspace)
+    p = cfg.c()
+    _check(lib().lazy_attn_prefill_key_weights(
+        ctypes.byref(p), q.data_ptr(), q_start.data_ptr(), q_pos0.data_ptr(), k_pool.data_ptr(), chunks.data_ptr(),
+        chunk_start.data_ptr(), key_start.data_ptr(), batch, q.shape[0], max_q_len, max_kv_len, weights.numel(),
+        lse.data_ptr(), _ptr(weights_in), float(decay), weights.data_ptr(), _ptr(workspace), nbytes, _stream(stream)),
+        "lazy_attn_prefill_key_weights")
+    return weights
+
+
+def decode_key_weights(cfg: Config, q, q_pos, k_pool, chunks, chunk_start, key_start, max_kv_len: int, lse, weights,
+                       weights_in=None, decay: float = 1.0, workspace=None, stream=None):
+    """lazy_attn_decode_key_weights: the weights that one new token per request gives, as prefill_key_weights."""
+    batch = q.shape[0]
+    _weight_args(cfg, q, q_pos, k_pool, chunks, chunk_start, key_start, batch, lse, weights, weights_in)
+    nbytes = decode_key_weights_workspace_size(cfg, batch, max_kv_len)
+    workspace = _workspace(nbytes, q.device, workspace)
+    p = cfg.c()
+    _check(lib().lazy_attn_decode_key_weights(
+        ctypes.byref(p), q.data_ptr(), q_pos.data_ptr(), k_pool.data_ptr(), chunks.data_ptr(), chunk_start.data_ptr(),
+        key_start.data_ptr(), batch, max_kv_len, lse.data_ptr(), _ptr(weights_in), float(decay), weights.data_ptr(),
+        _ptr(workspace), nbytes, _stream(stream)), "lazy_attn_decode_key_weights")
+    return weights
+
+
+def cache_select_workspace_size(batch: int, max_kv_len: int) -> int:
+    return int(lib().lazy_cache_select_workspace_size(batch, max_kv_len))
+
+
+def cache_select(weights, key_start, kept_start, max_kv_len: int, kept, sink: int = 0, recent: int = 0, key_count=None,
+                 workspace=None, stream=None):
+    """lazy_cache_select: indices of the kept_start[r+1] - kept_start[r] heaviest keys of every request, ascending,
+    into ``kept`` [kept_start[-1]] int32; the first ``sink`` and last ``recent`` keys come before all others.
+    Returns kept."""
+    _dev(weights, torch.float32, "weights")
+    _dev(key_start, torch.int32, "key_start")
+    _dev(kept_start, torch.int32, "kept_start")
+    _dev(kept, torch.int32, "kept")
+    batch = key_start.numel() - 1
+    _need(kept_start.numel() == batch + 1, "table sizes disagree with the batch")
+    if key_count is not None:
+        _dev(key_count, torch.int32, "key_count")
+        _need(key_count.numel() == batch, "table sizes disagree with the batch")
+    nbytes = cache_select_workspace_size(batch, max_kv_len)
+    workspace = _workspace(nbytes, weights.device, workspace)
+    _check(lib().lazy_cache_select(weights.data_ptr(), key_start.data_ptr(), _ptr(key_count), kept_start.data_ptr(),
+                                   batch, max_kv_len, sink, recent, kept.data_ptr(), _ptr(workspace), nbytes,
+                                   _stream(stream)), "lazy_cache_select")
+    return kept
+
+
+def cache_compact(cfg: Config, k_pool, v_pool, chunks, chunk_start, kept, kept_start, max_kept: int, dst, k_out, v_out,
+                  rotate: bool = False, key_start=None, weights=None, weights_out=None, stream=None):
+    """lazy_cache_compact: the kept keys of every request gathered into its record of ``dst`` (device records in k_out
+    / v_out); with weights, their weights into weights_out.  Returns (k_out, v_out)."""
+    for t, name in ((k_pool, "k_pool"), (v_pool, "v_pool"), (k_out, "k_out"), (v_out, "v_out")):
+        _dev(t, torch.bfloat16, name)
+    for t, name in ((chunk_start, "chunk_start"), (kept, "kept"), (kept_start, "kept_start")):
+        _dev(t, torch.int32, name)
+    _chunks(chunks)
+    _chunks(dst)
+    batch = chunk_start.numel() - 1
+    _need(kept_start.numel() == batch + 1 and dst.numel() == 32 * batch, "table sizes disagree with the batch")
+    if key_start is not None:
+        _dev(key_start, torch.int32, "key_start")
+        _need(key_start.numel() == batch + 1, "table sizes disagree with the batch")
+    for t, name in ((weights, "weights"), (weights_out, "weights_out")):
+        if t is not None:
+            _dev(t, torch.float32, name)
+    _need(weights_out is None or weights_out.numel() >= kept.numel(), "weights_out must have an entry a kept key")
+    p = cfg.c()
+    _check(lib().lazy_cache_compact(
+        ctypes.byref(p), k_pool.data_ptr(), v_pool.data_ptr(), chunks.data_ptr(), chunk_start.data_ptr(), batch,
+        kept.data_ptr(), kept_start.data_ptr(), max_kept, dst.data_ptr(), int(bool(rotate)), k_out.data_ptr(),
+        v_out.data_ptr(), _ptr(key_start), _ptr(weights), _ptr(weights_out), _stream(stream)), "lazy_cache_compact")
+    return k_out, v_out
 
 
 def materialize_k(cfg: Config, k_pool, chunks, max_chunk_len: int, total_kv: int, k_out=None, chunks_out=None,
