@@ -254,7 +254,7 @@ typedef struct lazy_backward_info {
   int32_t num_row_items; /* work items of the query gradient */
   int32_t num_blocks;    /* blocks of query tokens */
   int32_t row_slots;     /* most key splits of a request */
-  int32_t row_blocks;    /* 32-row blocks a wave of the query gradient holds (1 or 2) */
+  int32_t row_blocks;    /* 128-row blocks of a workgroup of the query gradient (1 or 2) */
   int32_t reserved;      /* 0 */
   int64_t plan_bytes;    /* size of the plan */
 } lazy_backward_info_t;

@@ -8,40 +8,49 @@
 
 namespace lazy {
 
-constexpr int kGradTileKeys = 64;  // stored keys of one key-gradient tile
+constexpr int kGradTileKeys = 64;  // stored keys of half a key-gradient tile
+constexpr int kGradHalves = 2;     // halves of a tile: 64 keys each, wherever they lie
 constexpr int kGradRows = 32;      // packed query rows (token * G + head in group) of one step over a tile
 
-// A tile of stored keys (key 0 of KV head 0 at k_off / v_off) or a part of its uses.
-struct GradTile {
+// Up to 64 stored keys (key 0 of KV head 0 at k_off / v_off).
+struct GradHalf {
   int64_t k_off, v_off;
   int32_t kst, vst;
-  int32_t keys;                // 1 .. kGradTileKeys
-  int32_t seg_begin, seg_end;  // its uses (none: the gradient is zero)
-  int32_t part;                // -1: the whole tile; otherwise where its partial sums go
+  int32_t keys;  // 0: none
+  int32_t reserved;
 };
-static_assert(sizeof(GradTile) == 40);
+static_assert(sizeof(GradHalf) == 32);
 
-// One use of a tile: query rows row_begin .. row_end - 1 (packed over the batch) of one request, which see the tile's
-// keys key_begin .. key_end - 1, key i at position pos + i.
+// Two halves that the same requests read, or a part of their uses.
+struct GradTile {
+  GradHalf half[kGradHalves];
+  int32_t seg_begin, seg_end;  // the uses (none: the gradient is zero)
+  int32_t part;                // -1: the whole tile; otherwise where its partial sums go
+  int32_t reserved;
+};
+static_assert(sizeof(GradTile) == 80);
+
+// One use of a tile: query rows row_begin .. row_end - 1 (packed over the batch) of one request.  They see the keys
+// key_begin .. key_end - 1 of each half, key i at position pos + i.
 struct GradSeg {
   int32_t row_begin, row_end;
   int32_t pos_shift;  // a token's position less its index in the batch
-  int32_t pos;
-  int32_t record_pos;  // pos_offset of the record (the rotation of local-position keys)
-  int32_t key_begin, key_end;
-  int32_t full_from;   // rows from this one on see all of the tile's keys (no mask is needed)
+  int32_t full_from;  // rows from this one on see all of the tile's keys (no mask is needed)
+  struct Half {
+    int32_t pos;
+    int32_t record_pos;  // pos_offset of the record (the rotation of local-position keys)
+    int32_t key_begin, key_end;
+  } half[kGradHalves];
 };
-static_assert(sizeof(GradSeg) == 32);
+static_assert(sizeof(GradSeg) == 48);
 
 // A tile whose uses were cut into parts: its gradient is the sum of part .. part + parts - 1.
 struct GradMerge {
-  int64_t k_off, v_off;
-  int32_t kst, vst;
-  int32_t keys;
+  GradHalf half[kGradHalves];
   int32_t part, parts;
-  int32_t reserved;
+  int32_t reserved[2];
 };
-static_assert(sizeof(GradMerge) == 40);
+static_assert(sizeof(GradMerge) == 80);
 
 // Query gradient: rows row0 .. of a request against key split `split` of `splits`.
 struct GradRowItem {
@@ -74,7 +83,7 @@ struct GradPlanLayout {
 
 // Where the backward pass keeps its intermediate results (bytes into the workspace).
 struct GradWorkLayout {
-  size_t q, info, dq, parts, bytes;
+  size_t q, dout, info, angles, dq, parts, bytes;
   GradWorkLayout(int hq, int hkv, int d, const lazy_backward_info_t& i) {
     const size_t rows = (size_t)i.total_q * (size_t)hq;
     size_t at = 0;
@@ -84,9 +93,12 @@ struct GradWorkLayout {
       return here;
     };
     q = put(rows * d * sizeof(uint16_t));                                        // rotated, scaled queries
-    info = put(rows * 2 * sizeof(float));                                        // (-lse log2 e, -delta) of each row
+    dout = put(rows * d * sizeof(uint16_t));                                     // packed like the queries
+    info = put((rows + kGradRows) * 2 * sizeof(float));                          // (-lse log2 e, -delta) of each row
+    angles = put((size_t)kGradTileKeys * d * sizeof(float));                     // rotations of positions 0 .. 63
     dq = put((size_t)i.row_slots * rows * d * sizeof(float));                    // partial query gradients
-    parts = put((size_t)i.num_parts * hkv * 2 * kGradTileKeys * d * sizeof(float));  // partial key, value gradients
+    // partial key and value gradients
+    parts = put((size_t)i.num_parts * hkv * 2 * kGradHalves * kGradTileKeys * d * sizeof(float));
     bytes = at;
   }
 };

@@ -59,6 +59,7 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const u32x4 x = *reinterpret_cast<const u32x4*>(a.dout + src * D + 2 * t0 + 8 * k);
+      *reinterpret_cast<u32x4*>(a.ws_do + dst * D + 2 * t0 + 8 * k) = x;
       const u32x4 y = *reinterpret_cast<const u32x4*>(a.out + src * D + 2 * t0 + 8 * k);
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum = fmaf(element(x, e), element(y, e), sum);
@@ -74,217 +75,314 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
   }
 }
 
-// Key and value gradients.  A workgroup is one wave and owns the 64 keys of a tile: K (rotated) and V stay in registers
-// as the right-hand operands of S = Q K^T and dP = dO V^T, whose accumulators have a key in every lane and 32 query
-// rows in registers and lane halves; P and dS leave them as the right-hand operands of dV^T += dO^T P and
-// dK^T += Q^T dS without any exchange between lanes.  Q and dO come through LDS, 32 rows at a time, read by rows for
-// the first two products and transposed for the last two.  -lse and -delta are the accumulators' initial values.
-// dK is kept in the rotated frame of the use at hand and turned on when the next use has another position.
+// Angles of the first kGradTileKeys positions, which every tile's keys add to the position of their key 0.
+template <int D>
+__global__ __launch_bounds__(256) void angle_rows(GradArgs a) {
+  const int e = blockIdx.x * 256 + threadIdx.x, t = e % (D / 2);
+  reinterpret_cast<float2*>(a.ws_angles)[e] = rope_cs(e / (D / 2), theta_rev(t, D, a.rope_log2_base, a.inv_freq));
+}
+
+// Rows of 16-byte chunks copied to a tile in LDS without passing through registers: lane l of a wave writes the 16 bytes
+// at 16 l from a uniform base, so the tile's permutation of chunks is made by the lanes' source addresses.
+__device__ __forceinline__ void copy_async(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
+                                   (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
+}
+// Every copy and LDS access so far has ended; nothing moves across.
+__device__ __forceinline__ void wait_copies() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Key and value gradients.  A workgroup owns a tile of two 64-key halves, each of its four waves 32 keys: K (rotated) stays
+// in registers and V in LDS, as the right-hand operands of S = Q K^T and dP = dO V^T, whose accumulators have a key in
+// every lane and 32 query rows in registers and lane halves; P and dS leave them as the right-hand operands of
+// dV^T += dO^T P and dK^T += Q^T dS without any exchange between lanes.  Q and dO come through LDS, 32 rows at a time,
+// read by rows for the first two products and transposed for the last two; the next 32 are copied to the other buffer
+// during the products.  -lse and -delta are the accumulators' initial values.  dK is kept in the rotated frame of the use
+// at hand and turned on when the next use has another position.
 template <int D, int KMI>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(1, 1))) void grad_kv(GradArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kv(GradArgs a) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
-  constexpr int C = D / 8;
-  __shared__ uint16_t tq[kGradRows * D] __attribute__((aligned(16)));
-  __shared__ uint16_t td[kGradRows * D] __attribute__((aligned(16)));
-  __shared__ float nlse[kGradRows] __attribute__((aligned(16)));
-  __shared__ float ndelta[kGradRows] __attribute__((aligned(16)));
-  __shared__ int rpos[kGradRows] __attribute__((aligned(16)));
-  __shared__ float rslope[kGradRows] __attribute__((aligned(16)));
-  __shared__ double freq[D / 2];
-  __shared__ float2 turn[D / 2] __attribute__((aligned(16)));
-  const int lane = threadIdx.x, h2 = lane >> 5, g = blockIdx.x % a.hkv;
-  const GradTile t = a.tiles[blockIdx.x / a.hkv];
-  if (ROT && lane < D / 2) freq[lane] = theta_rev(lane, D, a.rope_log2_base, a.inv_freq);
-  __syncthreads();
+  constexpr int C = D / 8;  // chunks of a row
+  constexpr int COPIES = kGradRows * C / 256;
+  // Two buffers as variables of their own: the compiler then knows that copies to one do not touch reads of the other.
+  __shared__ uint16_t tq0[kGradRows * D] __attribute__((aligned(16)));
+  __shared__ uint16_t td0[kGradRows * D] __attribute__((aligned(16)));
+  __shared__ float2 in0[kGradRows] __attribute__((aligned(16)));
+  __shared__ uint16_t tq1[kGradRows * D] __attribute__((aligned(16)));
+  __shared__ uint16_t td1[kGradRows * D] __attribute__((aligned(16)));
+  __shared__ float2 in1[kGradRows] __attribute__((aligned(16)));
+  __shared__ uint16_t tv[4][32 * D] __attribute__((aligned(16)));  // a wave's V operands, then its results
+  __shared__ int rpos_all[4][kGradRows] __attribute__((aligned(16)));
+  __shared__ float rslope_all[4][kGradRows] __attribute__((aligned(16)));
+  __shared__ float2 turn_all[4][D / 2] __attribute__((aligned(16)));
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h2 = lane >> 5, g = blockIdx.x % a.hkv;
+  const int hf = wave >> 1, k32 = 32 * (wave & 1), key = k32 + (lane & 31);
+  const GradTile* const tile = a.tiles + blockIdx.x / a.hkv;
+  const GradHalf t = tile->half[hf];
+  const int seg_begin = tile->seg_begin, seg_end = tile->seg_end, part = tile->part;
+  const bool active = k32 < t.keys;  // a wave without keys only helps to copy
+  int* const rpos = rpos_all[wave];
+  float* const rslope = rslope_all[wave];
+  float2* const turn = turn_all[wave];
+  const double rev = ROT ? theta_rev(lane % (D / 2), D, a.rope_log2_base, a.inv_freq) : 0.0;
+  const float2* angles = reinterpret_cast<const float2*>(a.ws_angles);
+  const int own_key = min(key, t.keys - 1);  // lanes past the last key repeat it; their columns are not stored
 
-  bf16x8 kf[2][D / 16], vf[2][D / 16];
-  f32x16 dk[2][D / 32], dv[2][D / 32];
-  int key[2];
+  bf16x8 kf[D / 16];
+  f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    key[b] = 32 * b + (lane & 31);
-    const uint16_t* v = a.v_pool + t.v_off + ((int64_t)g * t.vst + min(key[b], t.keys - 1)) * D;
+  for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = f32x16{};
+  const uint16_t* krow = a.k_pool + t.k_off + ((int64_t)g * t.kst + own_key) * D;
+  if (active) {
+    const uint16_t* v = a.v_pool + t.v_off + ((int64_t)g * t.vst + own_key) * D + 8 * h2;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) vf[b][s] = as_bf16x8(*reinterpret_cast<const u32x4*>(v + 16 * s + 8 * h2));
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) dk[b][db] = dv[b][db] = f32x16{};
+    for (int s = 0; s < D / 16; ++s) copy_async(v + 16 * s, tv[wave] + 512 * s);
   }
   const uint16_t* qbase = a.ws_q + (int64_t)g * a.rows * D;
+  const uint16_t* dbase = a.ws_do + (int64_t)g * a.rows * D;
   const float2* ibase = a.ws_info + (int64_t)g * a.rows;
-  const int head0 = g * a.group;
-  int frame = 0;  // position by which dk is rotated (NoPE: that of the tile's key 0)
-  for (int si = t.seg_begin; si < t.seg_end; ++si) {
-    const GradSeg seg = a.segs[si];
-    const int here = LOCAL ? seg.record_pos : seg.pos;
+  int frame = 0;  // position by which dk is rotated (NoPE: that of the half's key 0)
+  bool first = true;
+
+  const auto fetch = [&](int si, int row0, uint16_t* tq, uint16_t* td, float2* in) {
+    const int most = a.segs[si].row_end - 1 - row0;  // rows past the use's end repeat its last one
+    const uint16_t* q = qbase + (int64_t)row0 * D;
+    const uint16_t* d = dbase + (int64_t)row0 * D;
+    const int e0 = again(threadIdx.x);
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-      load_keys<D, KM, IL>(a.k_pool + t.k_off + ((int64_t)g * t.kst + min(key[b], t.keys - 1)) * D, h2,
-                           LOCAL ? here : here + key[b], freq, kf[b]);
-    if (ROT && si > t.seg_begin && here != frame) {
-      __syncthreads();
-      if (lane < D / 2) turn[lane] = rope_cs(here - frame, freq[lane]);
-      __syncthreads();
-#pragma unroll
-      for (int db = 0; db < D / 64; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float2 cs = turn[32 * db + 8 * (i >> 2) + 4 * h2 + (i & 3)];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const float x1 = dk[b][db][i], x2 = dk[b][db + D / 64][i];
-            float y1, y2;
-            rotate_by(x1, x2, cs, y1, y2);
-            dk[b][db][i] = y1;
-            dk[b][db + D / 64][i] = y2;
-          }
-        }
+    for (int i = 0; i < COPIES; ++i) {
+      const int row = (256 * i + e0) / C, chunk = ((256 * i + e0) % C) ^ swizzle<D>(row);
+      const int off = min(row, most) * D + 8 * chunk;
+      copy_async(q + off, tq + 2048 * i + 512 * wave);
+      copy_async(d + off, td + 2048 * i + 512 * wave);
     }
-    frame = here;
+    if (e0 < kGradRows / 2) copy_async(ibase + row0 + 2 * e0, in);  // two rows a lane
+  };
 
-    for (int row0 = seg.row_begin; row0 < seg.row_end; row0 += kGradRows) {
-      __syncthreads();
+  const auto compute = [&](int si, int row0, const uint16_t* tq, const uint16_t* td, const float2* in) {
+    const GradSeg& seg = a.segs[si];
+    const int rows = min(kGradRows, seg.row_end - row0), pos = seg.half[hf].pos;
+    if (row0 == seg.row_begin) {  // a new use: its keys, and dk turned on to its frame
+      const int l = again(lane);
+      const int here = LOCAL ? seg.half[hf].record_pos : pos;
+      if (ROT) {
+        if (!first && here != frame) {
+          if (l < D / 2) turn[l] = rope_cs(here - frame, rev);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-      for (int i = 0; i < kGradRows * C / 64; ++i) {
-        const int e = 64 * i + lane, row = e / C, chunk = e % C;
-        const int src = min(row0 + row, seg.row_end - 1);
-        const int tok = token_of(src, a.group_magic);
-        *reinterpret_cast<u32x4*>(tq + tile_at<D>(row, chunk)) =
-            *reinterpret_cast<const u32x4*>(qbase + (int64_t)src * D + 8 * chunk);
-        *reinterpret_cast<u32x4*>(td + tile_at<D>(row, chunk)) = *reinterpret_cast<const u32x4*>(
-            a.dout + ((int64_t)tok * (a.hq - a.group) + src + head0) * D + 8 * chunk);
-      }
-      if (lane < kGradRows) {
-        const int src = row0 + lane;
-        const int tok = token_of(src, a.group_magic);
-        const float2 in = src < seg.row_end ? ibase[src] : make_float2(-INFINITY, 0.f);
-        nlse[lane] = in.x;
-        ndelta[lane] = in.y;
-        rpos[lane] = tok + seg.pos_shift;
-        if (ALIBI) rslope[lane] = alibi_slope(head0 + src - tok * a.group, a.hq, a.inv_freq, 1.f);
-      }
-      __syncthreads();
-
-      f32x16 s[2], dp[2];
+          for (int db = 0; db < D / 64; ++db)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(nlse + 8 * q4 + 4 * h2);
-        const f32x4 y = *reinterpret_cast<const f32x4*>(ndelta + 8 * q4 + 4 * h2);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[0][4 * q4 + e] = s[1][4 * q4 + e] = x[e];
-          dp[0][4 * q4 + e] = dp[1][4 * q4 + e] = y[e];
+            for (int i = 0; i < 16; ++i) {
+              const float x1 = dk[db][i], x2 = dk[db + D / 64][i];
+              float y1, y2;
+              rotate_by(x1, x2, turn[32 * db + 8 * (i >> 2) + 4 * h2 + (i & 3)], y1, y2);
+              dk[db][i] = y1;
+              dk[db + D / 64][i] = y2;
+              if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
+        if (l < D / 2) turn[l] = rope_cs(here, rev);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        const bf16x8 fq = row_operand<D>(tq, lane & 31, k, h2), fd = row_operand<D>(td, lane & 31, k, h2);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq, kf[b][k], s[b], 0, 0, 0);
-          dp[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd, vf[b][k], dp[b], 0, 0, 0);
-        }
-      }
-      const bool masked = row0 < seg.full_from;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if (ALIBI) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
-            s[b][i] = fmaf(rslope[row], (float)(seg.pos + key[b] - rpos[row]), s[b][i]);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[b][i] = fast_exp2(s[b][i]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) dp[b][i] *= s[b][i];
-        if (masked) {
-          const bool used = key[b] >= seg.key_begin && key[b] < seg.key_end;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
-            const bool ok = used && (!a.causal || seg.pos + key[b] <= rpos[row]);
-            s[b][i] = ok ? s[b][i] : 0.f;
-            dp[b][i] = ok ? dp[b][i] : 0.f;
-          }
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        bf16x8 pf[2], sf[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          float x[8], y[8];
+      for (int s = 0; s < D / 32; ++s) {
+        const int t0 = 16 * s + 8 * (l >> 5);
+        u32x4 lo, hi;
+        load_pairs<D, IL>(krow, t0, lo, hi);
+        if (ROT) {
+          float yl[8], yh[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            x[e] = s[b][8 * k + e];
-            y[e] = dp[b][8 * k + e];
+            if (LOCAL)
+              rotate_by(element(lo, e), element(hi, e), turn[t0 + e], yl[e], yh[e]);
+            else
+              rotate_pair(element(lo, e), element(hi, e), turn[t0 + e], angles[(k32 + (l & 31)) * (D / 2) + t0 + e],
+                          yl[e], yh[e]);
           }
-          pf[b] = as_bf16x8(pack8(x));
-          sf[b] = as_bf16x8(pack8(y));
+          lo = pack8(yl);
+          hi = pack8(yh);
         }
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) {
-          const bf16x8 fd = column_operand<D>(td, 16 * k, db, lane), fq = column_operand<D>(tq, 16 * k, db, lane);
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            dv[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd, pf[b], dv[b][db], 0, 0, 0);
-            dk[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq, sf[b], dk[b][db], 0, 0, 0);
-          }
-        }
+        kf[s] = as_bf16x8(lo);
+        kf[s + D / 32] = as_bf16x8(hi);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      frame = here;
+      first = false;
     }
-  }
+    const bool masked = row0 < seg.full_from || rows < kGradRows;
+    if (ALIBI || masked) {
+      if (lane < kGradRows) {
+        const int src = row0 + lane, tok = token_of(src, a.group_magic);
+        rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + seg.pos_shift : INT32_MAX;
+        if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
 
-  // q carries scale * log2 e, dk wants scale: a factor of ln 2.  Turned back to the frame in which the key is stored.
+    const TileOperands<D> op(again(lane));
+    f32x16 s, dp;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+    for (int q2 = 0; q2 < 8; ++q2) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(in + 8 * (q2 >> 1) + 4 * h2 + 2 * (q2 & 1));
+      s[2 * q2] = x[0];
+      dp[2 * q2] = x[1];
+      s[2 * q2 + 1] = x[2];
+      dp[2 * q2 + 1] = x[3];
+    }
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int db = 0; db < D / 64; ++db)
+    for (int k = 0; k < D / 16; ++k) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(tq, 0, k), kf[k], s, 0, 0, 0);
+      const bf16x8 fv = as_bf16x8(*reinterpret_cast<const u32x4*>(tv[wave] + 512 * k + 8 * lane));
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(td, 0, k), fv, dp, 0, 0, 0);
+      if (k & 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    if (ALIBI) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float x1 = dk[b][db][i] * kLn2, x2 = dk[b][db + D / 64][i] * kLn2;
-        if (ROT) {
-          const int pair = 32 * db + 8 * (i >> 2) + 4 * h2 + (i & 3);
-          rotate_by(x1, x2, rope_cs(-(LOCAL ? frame : frame + key[b]), freq[pair]), x1, x2);
-        }
-        dk[b][db][i] = x1;
-        dk[b][db + D / 64][i] = x2;
+        const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
+        s[i] = fmaf(rslope[row], (float)(pos + key - rpos[row]), s[i]);
       }
-    if (t.part >= 0) {
-      float* out = a.ws_parts + (((int64_t)t.part * a.hkv + g) * 2 * kGradTileKeys + key[b]) * D;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const int col = 32 * db + 8 * q4 + 4 * h2;
-          *reinterpret_cast<f32x4*>(out + col) =
-              f32x4{dk[b][db][4 * q4], dk[b][db][4 * q4 + 1], dk[b][db][4 * q4 + 2], dk[b][db][4 * q4 + 3]};
-          *reinterpret_cast<f32x4*>(out + kGradTileKeys * D + col) =
-              f32x4{dv[b][db][4 * q4], dv[b][db][4 * q4 + 1], dv[b][db][4 * q4 + 2], dv[b][db][4 * q4 + 3]};
-        }
-    } else if (key[b] < t.keys) {
-      uint16_t* ko = a.dk_pool + t.k_off + ((int64_t)g * t.kst + key[b]) * D;
-      uint16_t* vo = a.dv_pool + t.v_off + ((int64_t)g * t.vst + key[b]) * D;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const int col = 32 * db + 8 * q4 + 4 * h2;
-          *reinterpret_cast<u32x2*>(vo + col) = u32x2{pack2(dv[b][db][4 * q4], dv[b][db][4 * q4 + 1]),
-                                                      pack2(dv[b][db][4 * q4 + 2], dv[b][db][4 * q4 + 3])};
-          if (!IL) {
-            *reinterpret_cast<u32x2*>(ko + col) = u32x2{pack2(dk[b][db][4 * q4], dk[b][db][4 * q4 + 1]),
-                                                        pack2(dk[b][db][4 * q4 + 2], dk[b][db][4 * q4 + 3])};
-          } else if (db < D / 64) {
-            u32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = pack2(dk[b][db][4 * q4 + e], dk[b][db + D / 64][4 * q4 + e]);
-            *reinterpret_cast<u32x4*>(ko + 2 * col) = w;
-          }
-        }
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = fast_exp2(s[i]);
+    if (masked) {
+      const bool used = key >= seg.half[hf].key_begin && key < seg.half[hf].key_end;
+      const int p = a.causal ? pos + key : 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
+        const bool ok = used && p <= rpos[row];
+        s[i] = ok ? s[i] : 0.f;
+        dp[i] = ok ? dp[i] : 0.f;
+      }
+    }
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float x[8], y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = s[8 * k + e];
+        y[e] = dp[8 * k + e] * x[e];
+      }
+      const bf16x8 pf = as_bf16x8(pack8(x)), sf = as_bf16x8(pack8(y));
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.column(td, 16 * k, db), pf, dv[db], 0, 0, 0);
+        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.column(tq, 16 * k, db), sf, dk[db], 0, 0, 0);
+        if (db & 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+  const auto advance = [&](int& si, int& row0) {  // to the next step; false at the end
+    row0 += kGradRows;
+    if (row0 < a.segs[si].row_end) return true;
+    if (++si >= seg_end) return false;
+    row0 = a.segs[si].row_begin;
+    return true;
+  };
+
+  if (seg_begin < seg_end) {
+    int si = seg_begin, row0 = a.segs[seg_begin].row_begin;
+    fetch(si, row0, tq0, td0, in0);
+    while (true) {
+      int nsi = si, nrow0 = row0;
+      bool more = advance(nsi, nrow0);
+      wait_copies();
+      __syncthreads();
+      if (more) fetch(nsi, nrow0, tq1, td1, in1);
+      if (active) compute(si, row0, tq0, td0, in0);
+      if (!more) break;
+      si = nsi;
+      row0 = nrow0;
+      more = advance(nsi, nrow0);
+      wait_copies();
+      __syncthreads();
+      if (more) fetch(nsi, nrow0, tq0, td0, in0);
+      if (active) compute(si, row0, tq1, td1, in1);
+      if (!more) break;
+      si = nsi;
+      row0 = nrow0;
+    }
+  }
+  wait_copies();
+  if (!active) return;
+
+  // q carries scale * log2 e, dk wants scale: a factor of ln 2.  Turned back to the frame in which the key is stored.
+  if (ROT && lane < D / 2) turn[lane] = rope_cs(-frame, rev);
+  wait_copies();
+#pragma unroll
+  for (int db = 0; db < D / 64; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float x1 = dk[db][i] * kLn2, x2 = dk[db + D / 64][i] * kLn2;
+      if (ROT) {
+        const int pair = 32 * db + 8 * (i >> 2) + 4 * h2 + (i & 3);
+        float2 cs = make_float2(1.f, 0.f);
+        if (!LOCAL) {
+          cs = angles[key * (D / 2) + pair];
+          cs.y = -cs.y;
+        }
+        rotate_pair(x1, x2, turn[pair], cs, x1, x2);
+      }
+      dk[db][i] = x1;
+      dk[db + D / 64][i] = x2;
+      if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  if (part >= 0) {
+    float* out = a.ws_parts + ((((int64_t)part * a.hkv + g) * kGradHalves + hf) * 2 * kGradTileKeys + key) * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int col = 32 * db + 8 * q4 + 4 * h2;
+        *reinterpret_cast<f32x4*>(out + col) =
+            f32x4{dk[db][4 * q4], dk[db][4 * q4 + 1], dk[db][4 * q4 + 2], dk[db][4 * q4 + 3]};
+        *reinterpret_cast<f32x4*>(out + kGradTileKeys * D + col) =
+            f32x4{dv[db][4 * q4], dv[db][4 * q4 + 1], dv[db][4 * q4 + 2], dv[db][4 * q4 + 3]};
+      }
+    return;
+  }
+  // Through LDS, so that whole rows are written: a lane has neighbouring elements of one key, four at a time.
+  uint16_t* const stage = tv[wave];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int col = 32 * db + 8 * q4 + 4 * h2;
+        const f32x16& x = which ? dk[db] : dv[db];
+        if (!IL || !which) {
+          *reinterpret_cast<u32x2*>(stage + tile_at<D>(lane & 31, col / 8) + col % 8) =
+              u32x2{pack2(x[4 * q4], x[4 * q4 + 1]), pack2(x[4 * q4 + 2], x[4 * q4 + 3])};
+        } else if (db < D / 64) {
+          u32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = pack2(dk[db][4 * q4 + e], dk[db + D / 64][4 * q4 + e]);
+          *reinterpret_cast<u32x4*>(stage + tile_at<D>(lane & 31, col / 4)) = w;
+        }
+      }
+    wait_copies();
+    uint16_t* out = which ? a.dk_pool + t.k_off + ((int64_t)g * t.kst + k32) * D
+                          : a.dv_pool + t.v_off + ((int64_t)g * t.vst + k32) * D;
+#pragma unroll
+    for (int i = 0; i < 32 * C / 64; ++i) {
+      const int row = (64 * i + lane) / C, chunk = (64 * i + lane) % C;
+      if (k32 + row < t.keys)
+        *reinterpret_cast<u32x4*>(out + row * D + 8 * chunk) =
+            *reinterpret_cast<const u32x4*>(stage + tile_at<D>(row, chunk));
+    }
+    wait_copies();
   }
 }
 
@@ -292,16 +390,17 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(1, 1))) void
 template <int D, bool IL>
 __global__ __launch_bounds__(256) void merge_tiles(GradArgs a) {
   const int g = blockIdx.x % a.hkv;
-  const GradMerge m = a.merges[blockIdx.x / a.hkv];
+  const GradMerge* const m = a.merges + blockIdx.x / a.hkv;
   constexpr int TPR = D / 16;
   const int t0 = 8 * (threadIdx.x % TPR);
-  for (int row = threadIdx.x / TPR; row < 2 * kGradTileKeys; row += 256 / TPR) {
-    const bool values = row >= kGradTileKeys;
+  for (int row = threadIdx.x / TPR; row < 2 * kGradHalves * kGradTileKeys; row += 256 / TPR) {
+    const bool values = row / kGradTileKeys % 2;
     const int key = row % kGradTileKeys;
-    if (key >= m.keys) continue;
+    const GradHalf h = m->half[row / (2 * kGradTileKeys)];
+    if (key >= h.keys) continue;
     float lo[8] = {}, hi[8] = {};
-    for (int p = m.part; p < m.part + m.parts; ++p) {
-      const float* src = a.ws_parts + (((int64_t)p * a.hkv + g) * 2 * kGradTileKeys + row) * D + t0;
+    for (int p = m->part; p < m->part + m->parts; ++p) {
+      const float* src = a.ws_parts + (((int64_t)p * a.hkv + g) * 2 * kGradHalves * kGradTileKeys + row) * D + t0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         lo[e] += src[e];
@@ -309,161 +408,252 @@ __global__ __launch_bounds__(256) void merge_tiles(GradArgs a) {
       }
     }
     if (values)
-      store_pairs<D, false>(a.dv_pool + m.v_off + ((int64_t)g * m.vst + key) * D, t0, lo, hi);
+      store_pairs<D, false>(a.dv_pool + h.v_off + ((int64_t)g * h.vst + key) * D, t0, lo, hi);
     else
-      store_pairs<D, IL>(a.dk_pool + m.k_off + ((int64_t)g * m.kst + key) * D, t0, lo, hi);
+      store_pairs<D, IL>(a.dk_pool + h.k_off + ((int64_t)g * h.kst + key) * D, t0, lo, hi);
   }
 }
 
-// Query gradient of 128 RB packed rows over the 64-key tiles of one key split: four waves of RB blocks of 32 rows, Q
-// and dO in registers.  S^T = K Q^T and dP^T = V dO^T have a query row in every lane; dS^T leaves them as the right-hand
-// operand of dQ^T += K^T dS^T.  K (rotated) and V pass through LDS, K read by rows and transposed.
-template <int D, int KMI, int RB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) void grad_q(GradArgs a) {
-  constexpr int KM = keys_of(KMI);
-  constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
-  constexpr int PP = D / 8;  // pairs of a key row that one of its four loader threads rotates
-  __shared__ uint16_t tk[kSub * D] __attribute__((aligned(16)));
-  __shared__ uint16_t tv[kSub * D] __attribute__((aligned(16)));
-  __shared__ double freq[D / 2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h2 = lane >> 5, g = blockIdx.x % a.hkv;
+// Loads a 64-key tile of K and V for a workgroup of NT threads, NT / 64 a key row, rotates the keys and writes both to
+// LDS (unpadded tiles, pairs in half-split order).
+template <int D, int KMI, int NT, bool REGS>
+struct TileLoader {
+  using S = TileLayout<D>;
+  static constexpr int KM = keys_of(KMI);
+  static constexpr bool ROT = KM == kKeysNope || KM == kKeysLocal, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
+  static constexpr int TPR = NT / kSub, PP = D / (2 * TPR), NV = PP / 8, VC = kSub * (D / 8) / NT;
+  static_assert(PP % 8 == 0 && VC * TPR == D / 8);
+  u32x4 ka[NV], kb[NV], vr[VC];  // raw pairs: first and second halves (interleaved: 16 elements as stored)
+  float2 cdr[REGS && KM == kKeysNope ? PP : 1];
+  int row, part;
+  __device__ void init(int t) {
+    row = t / TPR;
+    part = t % TPR;
+  }
+  __device__ void constants(const float* csd) {
+    if (KM == kKeysNope && REGS) {
+#pragma unroll
+      for (int e = 0; e < PP; ++e)
+        cdr[e] = *reinterpret_cast<const float2*>(csd + (row & (kAngleRows - 1)) * S::CSD_LD + cs_idx<D>(part * PP + e));
+    }
+  }
+  // Rows past the record's end repeat its last key; their products are masked.
+  __device__ void fetch(const uint16_t* k, const uint16_t* v, int nvalid) {
+    const int r = min(row, nvalid - 1);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int t0 = part * PP + 8 * i;
+      const uint16_t* src = k + r * D;
+      ka[i] = *reinterpret_cast<const u32x4*>(src + (IL ? 2 * t0 : t0));
+      kb[i] = *reinterpret_cast<const u32x4*>(src + (IL ? 2 * t0 + 8 : D / 2 + t0));
+    }
+#pragma unroll
+    for (int i = 0; i < VC; ++i) vr[i] = *reinterpret_cast<const u32x4*>(v + r * D + 8 * (part + TPR * i));
+  }
+  __device__ void store(uint16_t* tk, uint16_t* tv, const float* cb2, const float* csd) {
+    const float* cb = cb2 + (row / kAngleRows) * S::CSW;
+    const float* cd = csd + (row & (kAngleRows - 1)) * S::CSD_LD;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int t0 = part * PP + 8 * i;
+      u32x4 lo = ka[i], hi = kb[i];
+      if (IL) deinterleave8(ka[i], kb[i], lo, hi);
+      if (ROT) {
+        float yl[8], yh[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int ci = cs_idx<D>(t0 + e);
+          if (LOCAL) {
+            rotate_by(element(lo, e), element(hi, e), *reinterpret_cast<const float2*>(cb + ci), yl[e], yh[e]);
+          } else {
+            const float2 c = REGS ? cdr[8 * i + e] : *reinterpret_cast<const float2*>(cd + ci);
+            rotate_pair(element(lo, e), element(hi, e), *reinterpret_cast<const float2*>(cb + ci), c, yl[e], yh[e]);
+          }
+        }
+        lo = pack8(yl);
+        hi = pack8(yh);
+      }
+      *reinterpret_cast<u32x4*>(tk + tile_at<D>(row, t0 / 8)) = lo;
+      *reinterpret_cast<u32x4*>(tk + tile_at<D>(row, D / 16 + t0 / 8)) = hi;
+    }
+#pragma unroll
+    for (int i = 0; i < VC; ++i) *reinterpret_cast<u32x4*>(tv + tile_at<D>(row, part + TPR * i)) = vr[i];
+  }
+};
+
+template <int D, int NBUF>
+struct GradQSmem {
+  using S = TileLayout<D>;
+  uint16_t k[NBUF][kSub * D] __attribute__((aligned(16)));
+  uint16_t v[NBUF][kSub * D] __attribute__((aligned(16)));
+  float csd[kAngleRows * S::CSD_LD] __attribute__((aligned(16)));
+  float csb[2][2][S::CSW] __attribute__((aligned(16)));
+  double freq[D / 2];
+};
+
+// dS of one 64-key tile for a wave's 32 query rows, and its product: S^T = K Q^T and dP^T = V dO^T have a query row in
+// every lane; dS^T leaves them as the right-hand operand of dQ^T += K^T dS^T.
+template <int D, bool ALIBI>
+__device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv, int lane, const bf16x8 (&qf)[D / 16],
+                                          const bf16x8 (&df)[D / 16], f32x16 (&dq)[D / 32], float nl, float nd,
+                                          float slope, int qpos, int b0, int nvalid, int qmin, int causal) {
+  const int h2 = lane >> 5;
+  const bool masked = nvalid < kSub || (causal && b0 + kSub - 1 > qmin);
+  const TileOperands<D> op(again(lane));
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    f32x16 s, dp;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = nl;
+      dp[i] = nd;
+    }
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(tk, 32 * kb, k), qf[k], s, 0, 0, 0);
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(tv, 32 * kb, k), df[k], dp, 0, 0, 0);
+      if (k & 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    if (ALIBI) {
+      const float base = slope * (float)(b0 + 32 * kb + 4 * h2 - qpos);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = fmaf(slope, (float)(8 * (i >> 2) + (i & 3)), s[i] + base);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dp[i] *= fast_exp2(s[i]);
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int kk = 32 * kb + 8 * (i >> 2) + 4 * h2 + (i & 3);
+        dp[i] = kk < nvalid && (!causal || b0 + kk <= qpos) ? dp[i] : 0.f;
+      }
+    }
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = dp[8 * k + e];
+      const bf16x8 sf = as_bf16x8(pack8(y));
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.column(tk, 32 * kb + 16 * k, db), sf, dq[db], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  }
+}
+
+// Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q and dO in
+// registers; K (rotated) and V pass through LDS, K read by rows and transposed.
+template <int D, int KMI, int NW, int NBUF>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_q(GradArgs a) {
+  constexpr int KM = keys_of(KMI), NT = NW * 64;
+  constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal;
+  using S = TileLayout<D>;
+  __shared__ GradQSmem<D, NBUF> sm;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), h2 = lane >> 5, g = blockIdx.x % a.hkv;
   const GradRowItem item = a.row_items[blockIdx.x / a.hkv];
   const int r = item.request;
   const int qs = a.q_start[r], nrows = (a.q_start[r + 1] - qs) * a.group, shift = a.q_pos0[r] - qs;
-  if (ROT && tid < D / 2) freq[tid] = theta_rev(tid, D, a.rope_log2_base, a.inv_freq);
-
-  bf16x8 qf[RB][D / 16], df[RB][D / 16];
-  float nl[RB], nd[RB], slope[RB];
-  int row[RB], qpos[RB];
-  f32x16 dq[RB][D / 32];
+  const int pr = item.row0 + 32 * wave + (lane & 31);
+  const int src = qs * a.group + min(pr, nrows - 1), tok = token_of(src, a.group_magic), qpos = tok + shift;
+  const uint16_t* qrow = a.ws_q + ((int64_t)g * a.rows + src) * D;
+  const uint16_t* drow = a.ws_do + ((int64_t)g * a.rows + src) * D;
+  bf16x8 qf[D / 16], df[D / 16];
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int pr = item.row0 + 32 * (RB * wave + rb) + (lane & 31);
-    row[rb] = pr < nrows ? qs * a.group + pr : -1;
-    const int src = qs * a.group + min(pr, nrows - 1);
-    const int tok = token_of(src, a.group_magic);
-    qpos[rb] = tok + shift;
-    const uint16_t* qrow = a.ws_q + ((int64_t)g * a.rows + src) * D;
-    const uint16_t* drow = a.dout + ((int64_t)tok * (a.hq - a.group) + src + g * a.group) * D;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      qf[rb][s] = as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + 16 * s + 8 * h2));
-      df[rb][s] = as_bf16x8(*reinterpret_cast<const u32x4*>(drow + 16 * s + 8 * h2));
-    }
-    const float2 in = a.ws_info[(int64_t)g * a.rows + src];
-    nl[rb] = pr < nrows ? in.x : -INFINITY;
-    nd[rb] = in.y;
-    slope[rb] = ALIBI ? alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f) : 0.f;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) dq[rb][db] = f32x16{};
+  for (int s = 0; s < D / 16; ++s) {
+    qf[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + 16 * s + 8 * h2));
+    df[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(drow + 16 * s + 8 * h2));
   }
-  const int first_tok = token_of(item.row0, a.group_magic);
-  const int last_tok = token_of(min(item.row0 + 128 * RB, nrows) - 1, a.group_magic);
-  const int qmin = uniform(qs + first_tok + shift), qmax = uniform(qs + last_tok + shift);
+  const float2 in = a.ws_info[(int64_t)g * a.rows + src];
+  const float nl = pr < nrows ? in.x : -INFINITY, nd = in.y;
+  const float slope = ALIBI ? alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f) : 0.f;
+  f32x16 dq[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) dq[db] = f32x16{};
+  const int qmin = uniform(token_of(qs * a.group + item.row0, a.group_magic) + shift);
+  const int qmax = uniform(token_of(qs * a.group + min(item.row0 + 32 * NW, nrows) - 1, a.group_magic) + shift);
 
+  if (ROT) {
+    const double rev = theta_rev(tid % (D / 2), D, a.rope_log2_base, a.inv_freq);
+    if (tid < D / 2) sm.freq[tid] = rev;
+    for (int e = tid; e < kAngleRows * (D / 2); e += NT)
+      *reinterpret_cast<float2*>(sm.csd + e / (D / 2) * S::CSD_LD + cs_idx<D>(e % (D / 2))) = rope_cs(e / (D / 2), rev);
+  }
+  __syncthreads();
+  TileLoader<D, KMI, NT, NW == 8> ld;
+  ld.init(tid);
+  ld.constants(sm.csd);
   TileIter<kSub> it;
   it.init(a.chunks, a.chunk_start[r], a.chunk_start[r + 1], item.split, item.splits);
-  const int krow = tid >> 2, part = tid & 3;
-  while (it.seek(a.causal, qmax)) {
+  bool have = it.seek(a.causal, qmax);
+  const auto fetch = [&](const TileIter<kSub>& t) {
+    ld.fetch(k_ptr(a.k_pool, t.cur, g, t.j0, D), v_ptr(a.v_pool, t.cur, g, t.j0, D), min(kSub, t.cur.len - t.j0));
+  };
+  const auto base = [&](float* to, const TileIter<kSub>& t) {
+    if (ROT) prefill_base<D, LOCAL>(to, sm.freq, tid, t.cur.pos + (LOCAL ? 0 : t.j0));
+  };
+  if (have) fetch(it);
+  // Eight waves: as in the prefill kernel the upper four store the next tile at the start of a tile's products and the
+  // lower four at the end, so that the two waves of a SIMD are in different phases.
+  const bool early = NBUF == 2 && NW == 8 && wave >= NW / 2;
+  TileIter<kSub> ahead = it;
+  bool have_ahead = false;
+  if (have && NBUF == 2) {
+    base(sm.csb[0][0], it);
+    ahead.step();
+    have_ahead = ahead.seek(a.causal, qmax);
+    if (have_ahead) base(sm.csb[1][0], ahead);
+    __syncthreads();
+    ld.store(sm.k[0], sm.v[0], sm.csb[0][0], sm.csd);
+    if (early && have_ahead) fetch(ahead);
+    __syncthreads();
+  }
+  int parity = 0;
+  while (have) {
     const int nvalid = min(kSub, it.cur.len - it.j0), b0 = it.cur.pos + it.j0;
-    __syncthreads();
-    {
-      const int kr = min(krow, nvalid - 1);
-      const uint16_t* ks = k_ptr(a.k_pool, it.cur, g, it.j0 + kr, D);
-      const uint16_t* vs = v_ptr(a.v_pool, it.cur, g, it.j0 + kr, D);
-#pragma unroll
-      for (int v = 0; v < PP / 8; ++v) {
-        const int t0 = part * PP + 8 * v;
-        u32x4 lo, hi;
-        load_pairs<D, IL>(ks, t0, lo, hi);
-        if (ROT) {
-          float yl[8], yh[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            rotate_by(element(lo, e), element(hi, e), rope_cs(LOCAL ? it.cur.pos : b0 + krow, freq[t0 + e]), yl[e],
-                      yh[e]);
-          lo = pack8(yl);
-          hi = pack8(yh);
-        }
-        *reinterpret_cast<u32x4*>(tk + tile_at<D>(krow, t0 / 8)) = lo;
-        *reinterpret_cast<u32x4*>(tk + tile_at<D>(krow, D / 16 + t0 / 8)) = hi;
-      }
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-        *reinterpret_cast<u32x4*>(tv + tile_at<D>(krow, part * (D / 32) + i)) =
-            *reinterpret_cast<const u32x4*>(vs + 8 * (part * (D / 32) + i));
-    }
-    __syncthreads();
-    const bool masked = nvalid < kSub || (a.causal && b0 + kSub - 1 > qmin);
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      f32x16 s[RB], dp[RB];
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[rb][i] = nl[rb];
-          dp[rb][i] = nd[rb];
-        }
-#pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        const bf16x8 fk = row_operand<D>(tk, 32 * kb + (lane & 31), k, h2);
-        const bf16x8 fv = row_operand<D>(tv, 32 * kb + (lane & 31), k, h2);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          s[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, qf[rb][k], s[rb], 0, 0, 0);
-          dp[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, df[rb][k], dp[rb], 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int kk = 32 * kb + 8 * (i >> 2) + 4 * h2 + (i & 3);
-          if (ALIBI) s[rb][i] = fmaf(slope[rb], (float)(b0 + kk - qpos[rb]), s[rb][i]);
-          dp[rb][i] *= fast_exp2(s[rb][i]);
-        }
-        if (masked) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int kk = 32 * kb + 8 * (i >> 2) + 4 * h2 + (i & 3);
-            const bool ok = kk < nvalid && (!a.causal || b0 + kk <= qpos[rb]);
-            dp[rb][i] = ok ? dp[rb][i] : 0.f;
-          }
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        bf16x8 sf[RB];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = dp[rb][8 * k + e];
-          sf[rb] = as_bf16x8(pack8(y));
-        }
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) {
-          const bf16x8 fk = column_operand<D>(tk, 32 * kb + 16 * k, db, lane);
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
-            dq[rb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, sf[rb], dq[rb][db], 0, 0, 0);
-        }
+    int buf = 0;
+    bool have_next;
+    if (NBUF == 1) {
+      base(sm.csb[0][0], it);
+      it.step();
+      have_next = it.seek(a.causal, qmax);
+      __syncthreads();
+      ld.store(sm.k[0], sm.v[0], sm.csb[0][0], sm.csd);
+      __syncthreads();
+      if (have_next) fetch(it);
+    } else {
+      buf = parity;
+      it = ahead;
+      have_next = have_ahead;
+      if (early && have_next) ld.store(sm.k[parity ^ 1], sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
+      if (have_next) {
+        if (!early) fetch(it);
+        ahead.step();
+        have_ahead = ahead.seek(a.causal, qmax);
+        if (early && have_ahead) fetch(ahead);
       }
     }
-    it.step();
+    grad_tile<D, ALIBI>(sm.k[buf], sm.v[buf], lane, qf, df, dq, nl, nd, slope, qpos, b0, nvalid, qmin, a.causal);
+    if (NBUF == 2) {
+      if (have_ahead) base(sm.csb[parity][0], ahead);
+      if (!early && have_next) ld.store(sm.k[parity ^ 1], sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
+      __syncthreads();
+      parity ^= 1;
+    }
+    have = have_next;
   }
+  if (pr >= nrows) return;
+  float* out = a.ws_dq + (((int64_t)item.split * a.hkv + g) * a.rows + src) * D;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    if (row[rb] < 0) continue;
-    float* out = a.ws_dq + (((int64_t)item.split * a.hkv + g) * a.rows + row[rb]) * D;
+  for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-        *reinterpret_cast<f32x4*>(out + 32 * db + 8 * q4 + 4 * h2) =
-            f32x4{dq[rb][db][4 * q4], dq[rb][db][4 * q4 + 1], dq[rb][db][4 * q4 + 2], dq[rb][db][4 * q4 + 3]};
-  }
+    for (int q4 = 0; q4 < 4; ++q4)
+      *reinterpret_cast<f32x4*>(out + 32 * db + 8 * q4 + 4 * h2) =
+          f32x4{dq[db][4 * q4], dq[db][4 * q4 + 1], dq[db][4 * q4 + 2], dq[db][4 * q4 + 3]};
 }
 
 // Partial query gradients summed in the order of the splits, turned back from the rows' positions, scaled, rounded.
@@ -507,13 +697,18 @@ template <int D, int KMI>
 hipError_t launch(const GradArgs& a, const lazy_backward_info_t& i, hipStream_t stream) {
   constexpr bool IL = interleaved_of(KMI);
   if (i.num_blocks) prepare_rows<D, IL><<<i.num_blocks, 256, 0, stream>>>(a);
-  if (i.num_tiles) grad_kv<D, KMI><<<i.num_tiles * a.hkv, 64, 0, stream>>>(a);
+  if (i.num_tiles) angle_rows<D><<<kGradTileKeys * (D / 2) / 256, 256, 0, stream>>>(a);
+  if (i.num_tiles) grad_kv<D, KMI><<<i.num_tiles * a.hkv, 256, 0, stream>>>(a);
   if (i.num_merges) merge_tiles<D, IL><<<i.num_merges * a.hkv, 256, 0, stream>>>(a);
   if (i.num_row_items) {
-    if (i.row_blocks == 2)
-      grad_q<D, KMI, 2><<<i.num_row_items * a.hkv, 256, 0, stream>>>(a);
-    else
-      grad_q<D, KMI, 1><<<i.num_row_items * a.hkv, 256, 0, stream>>>(a);
+    if constexpr (D == 128) {
+      if (i.row_blocks == 2)
+        grad_q<D, KMI, 8, 2><<<i.num_row_items * a.hkv, 512, 0, stream>>>(a);
+      else
+        grad_q<D, KMI, 4, 1><<<i.num_row_items * a.hkv, 256, 0, stream>>>(a);
+    } else {
+      grad_q<D, KMI, 4, 2><<<i.num_row_items * a.hkv, 256, 0, stream>>>(a);
+    }
     finish_rows<D, IL><<<i.num_blocks, 256, 0, stream>>>(a);
   }
   return hipGetLastError();

@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <map>
 #include <new>
 #include <tuple>
 #include <vector>
@@ -14,7 +15,7 @@
 
 namespace {
 
-using lazy::GradBlock, lazy::GradMerge, lazy::GradRowItem, lazy::GradSeg, lazy::GradTile;
+using lazy::GradBlock, lazy::GradHalf, lazy::GradMerge, lazy::GradRowItem, lazy::GradSeg, lazy::GradTile;
 using lazy::kGradRows, lazy::kGradTileKeys;
 
 // One use of a record by a request.
@@ -90,54 +91,91 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
   }
   if (blocks_overlap(slabs, hkv, d, false) || blocks_overlap(slabs, hkv, d, true)) return LAZY_EDATA;
 
-  // Tiles and their uses.
+  // 64-key halves and their uses.
+  struct Use64 {
+    int32_t request, row_begin, full_from;
+    GradSeg::Half half;
+  };
+  struct Half {
+    GradHalf h;
+    std::vector<Use64> uses;
+  };
+  std::vector<Half> halves;
+  for (Slab& s : slabs) {
+    std::sort(s.uses.begin(), s.uses.end(), [](const Use& a, const Use& b) { return a.record < b.record; });
+    const size_t first = halves.size();
+    for (int64_t k = 0; k < s.keys; k += kGradTileKeys)
+      halves.push_back({{s.k_off + k * d, s.v_off + k * d, s.kst, s.vst,
+                         (int32_t)std::min<int64_t>(kGradTileKeys, s.keys - k), 0},
+                        {}});
+    for (const Use& u : s.uses) {
+      const lazy_chunk_t& c = chunks[u.record];
+      const int32_t r = u.request, qs = q_start[r], n = q_start[r + 1] - qs;
+      const int64_t begin = (c.k_offset - s.k_off) / d, end = begin + c.len;
+      for (int64_t k = begin / kGradTileKeys * kGradTileKeys; k < end; k += kGradTileKeys) {
+        Half& t = halves[first + k / kGradTileKeys];
+        Use64 g = {};
+        g.request = r;
+        g.half.key_begin = (int32_t)std::max<int64_t>(0, begin - k);
+        g.half.key_end = (int32_t)std::min<int64_t>(t.h.keys, end - k);
+        g.half.pos = (int32_t)(c.pos_offset + k - begin);
+        g.half.record_pos = c.pos_offset;
+        int32_t tb = 0, tf = 0;  // first token that sees a key, and all of them
+        if (p->causal && n > 0) {
+          tb = (int32_t)std::min<int64_t>(n, std::max<int64_t>(0, (int64_t)g.half.pos + g.half.key_begin - q_pos0[r]));
+          tf = (int32_t)std::min<int64_t>(n, std::max<int64_t>(0, (int64_t)g.half.pos + g.half.key_end - 1 - q_pos0[r]));
+        }
+        if (tb >= n) continue;
+        g.row_begin = (qs + tb) * G;
+        g.full_from = g.half.key_begin == 0 && g.half.key_end == t.h.keys ? (qs + tf) * G : (qs + n) * G;
+        t.uses.push_back(g);
+      }
+    }
+  }
+
+  // Tiles: two halves that the same requests read, in the order in which they come (the next 64 keys of a chunk, or the
+  // next block of a paged one); a half that finds no partner stays alone.
   struct Tile {
     GradTile t;
     std::vector<GradSeg> segs;
     int64_t steps = 0;
   };
   std::vector<Tile> tiles;
-  int64_t total_steps = 0;
-  for (Slab& s : slabs) {
-    std::sort(s.uses.begin(), s.uses.end(), [](const Use& a, const Use& b) { return a.record < b.record; });
-    const size_t first = tiles.size();
-    for (int64_t k = 0; k < s.keys; k += kGradTileKeys) {
-      Tile t;
-      t.t = {s.k_off + k * d, s.v_off + k * d, s.kst, s.vst, (int32_t)std::min<int64_t>(kGradTileKeys, s.keys - k),
-             0, 0, -1};
-      tiles.push_back(std::move(t));
+  std::map<std::vector<int32_t>, size_t> open;  // requests of the uses -> a tile with one half
+  std::vector<int32_t> who;
+  for (const Half& h : halves) {
+    who.clear();
+    for (const Use64& u : h.uses) who.push_back(u.request);
+    const auto found = open.find(who);
+    const int at = found == open.end() ? 0 : 1;
+    if (at == 0) {
+      open.emplace(who, tiles.size());
+      tiles.emplace_back();
+      tiles.back().t.part = -1;
+      tiles.back().segs.resize(h.uses.size());
     }
-    for (const Use& u : s.uses) {
-      const lazy_chunk_t& c = chunks[u.record];
-      const int32_t r = u.request, qs = q_start[r], n = q_start[r + 1] - qs;
-      const int64_t begin = (c.k_offset - s.k_off) / d, end = begin + c.len;
-      for (int64_t k = begin / kGradTileKeys * kGradTileKeys; k < end; k += kGradTileKeys) {
-        Tile& t = tiles[first + k / kGradTileKeys];
-        GradSeg g = {};
-        g.key_begin = (int32_t)std::max<int64_t>(0, begin - k);
-        g.key_end = (int32_t)std::min<int64_t>(t.t.keys, end - k);
-        g.pos = (int32_t)(c.pos_offset + k - begin);
-        g.record_pos = c.pos_offset;
-        g.pos_shift = (n > 0 ? q_pos0[r] : 0) - qs;
-        int32_t tb = 0, tf = 0;  // first token that sees a key, and all of them
-        if (p->causal && n > 0) {
-          tb = (int32_t)std::min<int64_t>(n, std::max<int64_t>(0, (int64_t)g.pos + g.key_begin - q_pos0[r]));
-          tf = (int32_t)std::min<int64_t>(n, std::max<int64_t>(0, (int64_t)g.pos + g.key_end - 1 - q_pos0[r]));
-        }
-        if (tb >= n) continue;
-        g.row_begin = (qs + tb) * G;
-        g.row_end = (qs + n) * G;
-        g.full_from = g.key_begin == 0 && g.key_end == t.t.keys ? (qs + tf) * G : g.row_end;
-        t.segs.push_back(g);
-        t.steps += steps_of(g);
-      }
+    Tile& t = at == 0 ? tiles.back() : tiles[found->second];
+    if (at == 1) open.erase(found);
+    t.t.half[at] = h.h;
+    for (size_t i = 0; i < h.uses.size(); ++i) {
+      const Use64& u = h.uses[i];
+      GradSeg& s = t.segs[i];
+      const int32_t r = u.request;
+      s.row_begin = at == 0 ? u.row_begin : std::min(s.row_begin, u.row_begin);
+      s.full_from = at == 0 ? u.full_from : std::max(s.full_from, u.full_from);
+      s.row_end = q_start[r + 1] * G;
+      s.pos_shift = q_pos0[r] - q_start[r];
+      s.half[at] = u.half;
     }
   }
+  int64_t total_steps = 0;
+  for (Tile& t : tiles)
+    for (const GradSeg& s : t.segs) t.steps += steps_of(s);
   for (const Tile& t : tiles) total_steps += t.steps;
 
-  // Parts: no work item should take much longer than a SIMD's share of the whole (one workgroup of one wave is one
-  // SIMD's worth of registers), nor so little that its loads and its final sums dominate.
-  const int64_t limit = std::max<int64_t>(8, lazy::ceil_div(total_steps * hkv, 2 * 4 * lazy::kNumCUs));
+  // Parts: no work item should take much longer than half of a workgroup's share of the whole (a CU holds two), nor so
+  // little that its loads and its final sums dominate.
+  const int64_t limit = std::max<int64_t>(8, lazy::ceil_div(total_steps * hkv, 2 * 2 * lazy::kNumCUs));
   std::vector<GradTile> out_tiles;
   std::vector<GradSeg> out_segs;
   std::vector<GradMerge> merges;
@@ -146,7 +184,7 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
   for (Tile& t : tiles) {
     const int64_t parts = std::max<int64_t>(1, lazy::ceil_div(t.steps, limit + limit / 2));
     if (parts > 1)
-      merges.push_back({t.t.k_off, t.t.v_off, t.t.kst, t.t.vst, t.t.keys, num_parts, (int32_t)parts, 0});
+      merges.push_back({{t.t.half[0], t.t.half[1]}, num_parts, (int32_t)parts, {0, 0}});
     size_t at = 0;
     int64_t done = 0;
     for (int64_t part = 0; part < parts; ++part) {
@@ -175,7 +213,7 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
   for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
   std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return cost[a] > cost[b]; });
 
-  // Query gradient: 64 rows a wave (128: one block of 32) where requests fill such tiles.
+  // Query gradient: 256 rows a workgroup (eight waves; head_dim 128 only) where requests fill such tiles, else 128.
   int64_t rows1 = 0, rows2 = 0;
   std::vector<int64_t> key_tiles(batch);
   for (int r = 0; r < batch; ++r) {
@@ -185,7 +223,7 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
     for (int i = chunk_start[r]; i < chunk_start[r + 1]; ++i)
       key_tiles[r] += lazy::ceil_div(chunks[i].len, kGradTileKeys);
   }
-  const int row_blocks = 4 * rows2 <= 5 * rows1 ? 2 : 1, bm = 128 * row_blocks;
+  const int row_blocks = d == 128 && 4 * rows2 <= 5 * rows1 ? 2 : 1, bm = 128 * row_blocks;
   int64_t work = 0;
   for (int r = 0; r < batch; ++r)
     work += lazy::ceil_div((int64_t)(q_start[r + 1] - q_start[r]) * G, bm) * key_tiles[r] * hkv;

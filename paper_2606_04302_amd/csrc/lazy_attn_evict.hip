@@ -144,6 +144,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       const int qmin = token_of(row0, a.group_magic) + shift;
       const int qmax = token_of(min(row0 + kRowStep, row_end) - 1, a.group_magic) + shift;
       if (!have || (a.causal && b0 > qmax)) continue;
+      const TileOperands<D> op(lane);
       f32x16 s[2];
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4) {
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       }
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
-        const bf16x8 fq = row_operand<D>(tq, lane & 31, k, h2);
+        const bf16x8 fq = op.row(tq, 0, k);
 #pragma unroll
         for (int b = 0; b < 2; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq, kf[b][k], s[b], 0, 0, 0);
       }

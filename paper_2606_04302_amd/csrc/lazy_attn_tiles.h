@@ -20,21 +20,35 @@ template <int D>
 __device__ __forceinline__ int tile_at(int row, int chunk) {
   return row * D + 8 * (chunk ^ swizzle<D>(row));
 }
-// Operand of row `row`, elements 16 s + 8 h2 .. + 7.
-template <int D>
-__device__ __forceinline__ bf16x8 row_operand(const uint16_t* tile, int row, int s, int h2) {
-  return as_bf16x8(*reinterpret_cast<const u32x4*>(tile + tile_at<D>(row, 2 * s + h2)));
+// x, in a way that the compiler does not see through: what is computed from it is computed where it stands, not kept in
+// registers across a loop.
+__device__ __forceinline__ int again(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
-// Transposed operand: element column 32 db + lane % 32 of rows row0 + {0..3, 8..11} + 4 (lane / 32): the rows that
-// registers 8 k .. 8 k + 7 of a 32x32 product's accumulator hold for this lane half (row0 = 16 k).
+
+// A lane's operands of 32x32x16 products from a tile.  row: elements 16 k + 8 (lane / 32) .. + 7 of row row0 + lane % 32.
+// column: transposed, element column 32 db + lane % 32 of rows row0 + {0..3, 8..11} + 4 (lane / 32), the rows that
+// registers 8 j .. 8 j + 7 of an accumulator hold for this lane half (row0 a multiple of 16; row's of 32).  Steps only
+// flip bits of the chunk index, so every address is one exclusive or away from two.
 template <int D>
-__device__ __forceinline__ bf16x8 column_operand(const uint16_t* tile, int row0, int db, int lane) {
-  const int i = lane & 15, grp = lane >> 4;
-  const int row = row0 + 4 * (grp >> 1) + (i >> 2), chunk = 4 * db + 2 * (grp & 1) + ((i & 3) >> 1), half = 4 * (i & 1);
-  const u32x2 lo = tr_read(tile + tile_at<D>(row, chunk) + half);
-  const u32x2 hi = tr_read(tile + tile_at<D>(row + 8, chunk) + half);
-  return as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
-}
+struct TileOperands {
+  int ra, ca;
+  __device__ explicit TileOperands(int lane) {
+    const int i = lane & 15;
+    ra = 2 * tile_at<D>(lane & 31, lane >> 5);
+    ca = 2 * (tile_at<D>(4 * (lane >> 5) + (i >> 2), 2 * (lane >> 4 & 1) + ((i & 3) >> 1)) + 4 * (i & 1));
+  }
+  __device__ __forceinline__ bf16x8 row(const uint16_t* tile, int row0, int k) const {
+    return as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(tile) + 2 * D * row0 + (ra ^ 32 * k)));
+  }
+  __device__ __forceinline__ bf16x8 column(const uint16_t* tile, int row0, int db) const {
+    const char* at = reinterpret_cast<const char*>(tile) + 2 * D * row0;
+    const u32x2 lo = tr_read(reinterpret_cast<const uint16_t*>(at + (ca ^ 64 * db)));
+    const u32x2 hi = tr_read(reinterpret_cast<const uint16_t*>(at + 16 * D + (ca ^ 32 ^ 64 * db)));
+    return as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
+  }
+};
 
 // Packed row -> token: row / G by multiplication (total_q * G * G < 2^32, checked by the planner).
 __device__ __forceinline__ int token_of(int row, uint32_t magic) { return magic ? (int)__umulhi(row, magic) : row; }

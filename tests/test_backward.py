@@ -21,12 +21,12 @@ from paper_2606_04302_amd import workloads as W
 
 REL = 0.017
 
-TILE = np.dtype([("k_off", "<i8"), ("v_off", "<i8"), ("kst", "<i4"), ("vst", "<i4"), ("keys", "<i4"),
-                 ("seg_begin", "<i4"), ("seg_end", "<i4"), ("part", "<i4")])
-SEG = np.dtype([(n, "<i4") for n in ("row_begin", "row_end", "pos_shift", "pos", "record_pos", "key_begin", "key_end",
-                                     "full_from")])
-MERGE = np.dtype([("k_off", "<i8"), ("v_off", "<i8"), ("kst", "<i4"), ("vst", "<i4"), ("keys", "<i4"),
-                  ("part", "<i4"), ("parts", "<i4"), ("reserved", "<i4")])
+HALF = np.dtype([("k_off", "<i8"), ("v_off", "<i8"), ("kst", "<i4"), ("vst", "<i4"), ("keys", "<i4"),
+                 ("reserved", "<i4")])
+TILE = np.dtype([("half", HALF, 2), ("seg_begin", "<i4"), ("seg_end", "<i4"), ("part", "<i4"), ("reserved", "<i4")])
+SEG_HALF = np.dtype([(n, "<i4") for n in ("pos", "record_pos", "key_begin", "key_end")])
+SEG = np.dtype([(n, "<i4") for n in ("row_begin", "row_end", "pos_shift", "full_from")] + [("half", SEG_HALF, 2)])
+MERGE = np.dtype([("half", HALF, 2), ("part", "<i4"), ("parts", "<i4"), ("reserved", "<i4", 2)])
 ROW = np.dtype([(n, "<i4") for n in ("request", "row0", "split", "splits")])
 BLOCK = np.dtype([(n, "<i4") for n in ("t0", "tokens", "pos_shift", "splits")])
 
@@ -81,23 +81,27 @@ def shared(seed, hq, hkv, d, lens, q_lens, reqs=3, causal=True, gap=0, twice=Fal
 # CPU: planner
 # ---------------------------------------------------------------------------------------------------------------
 def covered(w, plan, G):
-    """{(token, k element offset of head 0): times} over the plan's tiles and segments, with positions checked."""
+    """{(token, k element offset of head 0, position): rows} over the plan's tiles and segments."""
     _, _, segs, tiles, _ = arrays(plan)
     pos_of = w.q_positions()
     seen = {}
     for t in tiles:
         for s in segs[t["seg_begin"]:t["seg_end"]]:
-            assert 0 <= s["row_begin"] < s["row_end"] <= w.total_q * G and 0 <= s["key_begin"] < s["key_end"] <= t["keys"]
-            for tok in range(int(s["row_begin"]) // G, -(-int(s["row_end"]) // G)):
-                # rows of a token may be divided between parts: count rows
-                rows = min(int(s["row_end"]), (tok + 1) * G) - max(int(s["row_begin"]), tok * G)
-                assert pos_of[tok] == tok + int(s["pos_shift"])
-                for key in range(int(s["key_begin"]), int(s["key_end"])):
-                    if not w.causal or int(s["pos"]) + key <= pos_of[tok]:
-                        at = (tok, int(t["k_off"]) + key * w.head_dim, int(s["pos"]) + key)
-                        seen[at] = seen.get(at, 0) + rows
-                    else:
-                        assert int(s["row_begin"]) < int(s["full_from"])
+            assert 0 <= s["row_begin"] < s["row_end"] <= w.total_q * G
+            for h, sh in zip(t["half"], s["half"]):
+                assert 0 <= sh["key_begin"] <= sh["key_end"] <= h["keys"]
+                for tok in range(int(s["row_begin"]) // G, -(-int(s["row_end"]) // G)):
+                    # rows of a token may be divided between parts: count rows
+                    rows = min(int(s["row_end"]), (tok + 1) * G) - max(int(s["row_begin"]), tok * G)
+                    assert pos_of[tok] == tok + int(s["pos_shift"])
+                    full = tok * G >= s["full_from"]
+                    assert not full or (sh["key_begin"] == 0 and sh["key_end"] == h["keys"])
+                    for key in range(int(sh["key_begin"]), int(sh["key_end"])):
+                        if not w.causal or int(sh["pos"]) + key <= pos_of[tok]:
+                            at = (tok, int(h["k_off"]) + key * w.head_dim, int(sh["pos"]) + key)
+                            seen[at] = seen.get(at, 0) + rows
+                        else:
+                            assert not full
     return seen
 
 
@@ -137,8 +141,9 @@ def test_plan_covers_every_visible_pair_once(name):
     # Every stored key belongs to one tile (or to the parts of one), and parts are numbered without a gap.
     keys = {}
     for t in tiles:
-        for k in range(int(t["keys"])):
-            keys.setdefault(int(t["k_off"]) + k * w.head_dim, []).append(int(t["part"]))
+        for h in t["half"]:
+            for k in range(int(h["keys"])):
+                keys.setdefault(int(h["k_off"]) + k * w.head_dim, []).append(int(t["part"]))
     for c in w.chunks:
         for j in range(int(c["len"])):
             parts = keys[int(c["k_offset"]) + j * w.head_dim]
