@@ -305,90 +305,293 @@ __global__ __launch_bounds__(256) void weigh_token(WeightArgs a) {
   }
 }
 
-// Selection: a radix select of the b-th largest score and an ordered compaction, one workgroup a request.
-// Scores as integers in their order: NaN lowest, -0 like 0, protected keys above all.
-constexpr int kSelectThreads = 1024;
-__device__ __forceinline__ uint32_t score_of(float w, int j, int n, int sink, int recent) {
-  if (j < sink || j >= n - recent) return 0xffffffffu;
-  if (w != w) return 0;
+// Selection: a radix select of the b-th largest score, 11, 11 and 10 bits at a time, and an ordered compaction.  Scores
+// are compared as integers in their order: NaN lowest, -0 like 0, protected keys above all.
+//
+// A workgroup of 1024 threads holds up to 35840 scores in LDS, so that a request of so many keys is read once and selected
+// in one launch (select_request).  Longer requests are cut into slices of 16384 keys, one workgroup each: select_slices
+// counts one digit a launch, leaving every slice's counts in the workspace, and the next launch (and the writing one)
+// adds them up; nothing has to be cleared and no workgroup waits for another.
+//
+// One workgroup's passes are bound by its CU's vector instructions (64 lanes a clock: 33068 keys times one instruction is
+// 0.2 us) and by LDS atomics on the same address (weights of a few octaves share their top bits).  So every pass does the
+// least for a score: no bounds (the tail is filled up with the lowest score, which is never picked before a key), the
+// first digit counted while the scores arrive, protected keys marked afterwards, passes that few scores concern skip
+// whole waves, and every bin has two counters, one for every other lane (one counter: 3.5 us more).
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kBins = 2048;
+constexpr int kSlice = 16384, kMostResident = 35840;
+__device__ __forceinline__ uint32_t score_of(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  return w != w ? 0 : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint32_t with_digit(uint32_t prefix, int digit, int pass) {
+  return prefix | (uint32_t)digit << (pass == 0 ? 21 : pass == 1 ? 10 : 0);
 }
 
-__global__ __launch_bounds__(kSelectThreads) void select_keys(const float* weights, const int32_t* key_start,
-                                                              const int32_t* key_count, const int32_t* kept_start,
-                                                              int sink, int recent, int32_t* kept) {
-  constexpr int kWaves = kSelectThreads / 64;
-  __shared__ int hist[256];
-  __shared__ uint32_t prefix_s;
-  __shared__ int need_s;
-  __shared__ int above[kWaves], equal[kWaves];
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int k0 = key_start[r], room = key_start[r + 1] - k0;
-  const int n = key_count ? max(0, min(key_count[r], room)) : room;
-  const int o0 = kept_start[r], b = kept_start[r + 1] - o0;
-  const float* w = weights + k0;
-  if (b >= n) {
-    for (int i = tid; i < b; i += kSelectThreads) kept[o0 + i] = i < n ? i : -1;
-    return;
-  }
-  if (b <= 0) return;
-  // The b-th largest score, eight bits at a time: `prefix` its bits so far, `need` its rank among the scores with them.
-  uint32_t prefix = 0;
-  int need = b;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    for (int j = tid; j < n; j += kSelectThreads) {
-      const uint32_t s = score_of(w[j], j, n, sink, recent);
-      if (shift == 24 || s >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[s >> shift & 255], 1);
-    }
-    __syncthreads();
-    if (tid < 64) {  // lane l holds digits 255 - 4 l .. 252 - 4 l, so the scan counts from the largest
-      int c[4], sum = 0;
+template <int CAP>
+struct SelectSmem {
+  uint32_t score[CAP] __attribute__((aligned(16)));
+  int hist[2 * kBins] __attribute__((aligned(16)));  // two counters a digit
+  int wave_sum[2 * kSelectWaves] __attribute__((aligned(8)));
+  int digit, need;
+};
+
+constexpr int kBatch = 4;  // scores a thread has in flight
+template <int CAP>
+__device__ __forceinline__ void clear_counts(SelectSmem<CAP>& sm) {
+  reinterpret_cast<u32x4*>(sm.hist)[threadIdx.x] = u32x4{0, 0, 0, 0};
+  static_assert(2 * kBins == 4 * kSelectThreads);
+  __syncthreads();
+}
+
+// Scores of keys j0 .. j0 + count - 1 (count <= CAP) of a request of n, filled up to a multiple of the workgroup's
+// threads, and with COUNT their first digits.
+template <bool COUNT, int CAP>
+__device__ __forceinline__ int load_scores(SelectSmem<CAP>& sm, const float* w, int j0, int count, int n, int sink,
+                                           int recent) {
+  static_assert(CAP % kSelectThreads == 0);
+  constexpr int U = 8;
+  const int tid = threadIdx.x, filled = (count + kSelectThreads - 1) & ~(kSelectThreads - 1);
+  if (COUNT) clear_counts(sm);
+  for (int base = 0; base < filled; base += U * kSelectThreads) {
+    float x[U];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += c[e] = hist[255 - 4 * tid - e];
-      int before = wave_incl_scan(sum) - sum;
+    for (int u = 0; u < U; ++u) x[u] = w[j0 + min(base + u * kSelectThreads + tid, count - 1)];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (before < need && need <= before + c[e]) {
-          prefix_s = prefix | (uint32_t)(255 - 4 * tid - e) << shift;
-          need_s = need - before;
-        }
-        before += c[e];
-      }
+    for (int u = 0; u < U; ++u) {
+      if (base + u * kSelectThreads >= filled) break;
+      const int i = base + u * kSelectThreads + tid;
+      uint32_t s = score_of(x[u]);
+      if (base + (u + 1) * kSelectThreads > count && i >= count) s = 0;
+      sm.score[i] = s;
+      if (COUNT) atomicAdd(&sm.hist[2 * (s >> 21) + (tid & 1)], 1);
     }
-    __syncthreads();
-    prefix = prefix_s;
-    need = need_s;
-  }
-  // Every wave counts, then writes, the keys of a contiguous part: all above the threshold, and the first `need` equal
-  // to it.
-  const int per = ((n + kWaves - 1) / kWaves + 63) & ~63, j0 = min(n, wave * per), j1 = min(n, j0 + per);
-  int na = 0, ne = 0;
-  for (int j = j0 + lane; j - lane < j1; j += 64) {
-    const uint32_t s = j < j1 ? score_of(w[j], j, n, sink, recent) : 0;
-    na += __builtin_popcountll(__ballot(j < j1 && s > prefix));
-    ne += __builtin_popcountll(__ballot(j < j1 && s == prefix));
-  }
-  if (lane == 0) {
-    above[wave] = na;
-    equal[wave] = ne;
   }
   __syncthreads();
-  na = ne = 0;
-  for (int k = 0; k < wave; ++k) {
-    na += above[k];
-    ne += equal[k];
+  const auto protect = [&](int i) {
+    if (COUNT) {
+      atomicAdd(&sm.hist[2 * (sm.score[i] >> 21) + (tid & 1)], -1);
+      atomicAdd(&sm.hist[2 * (kBins - 1) + (tid & 1)], 1);
+    }
+    sm.score[i] = 0xffffffffu;
+  };
+  const int head = min(max(0, sink - j0), count), tail = max(head, n - recent - j0);
+  for (int i = tid; i < head; i += kSelectThreads) protect(i);
+  for (int i = tail + tid; i < count; i += kSelectThreads) protect(i);
+  __syncthreads();
+  return filled;
+}
+
+// Counts the digits of pass 1 or 2.
+template <int CAP>
+__device__ __forceinline__ void count_digits(SelectSmem<CAP>& sm, int filled, uint32_t prefix, int pass) {
+  const int tid = threadIdx.x, shift = pass == 1 ? 10 : 0;
+  const uint32_t width = pass == 1 ? 1u << 21 : 1u << 10;
+  clear_counts(sm);
+  for (int base = 0; base < filled; base += kBatch * kSelectThreads) {
+    uint32_t s[kBatch];
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e)
+      s[e] = sm.score[min(base + e * kSelectThreads, filled - kSelectThreads) + tid] - prefix;
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e)
+      if (base + e * kSelectThreads < filled && s[e] < width) atomicAdd(&sm.hist[2 * (s[e] >> shift) + (tid & 1)], 1);
   }
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-  for (int j = j0 + lane; j - lane < j1; j += 64) {
-    const uint32_t s = j < j1 ? score_of(w[j], j, n, sink, recent) : 0;
-    const uint64_t ma = __ballot(j < j1 && s > prefix), me = __ballot(j < j1 && s == prefix);
-    const int ra = na + __builtin_popcountll(ma & below), re = ne + __builtin_popcountll(me & below);
-    if ((ma >> lane & 1) || ((me >> lane & 1) && re < need)) kept[o0 + ra + min(re, need)] = j;
-    na += __builtin_popcountll(ma);
-    ne += __builtin_popcountll(me);
+  __syncthreads();
+}
+// This thread's two bins, from the largest digit down.
+template <int CAP>
+__device__ __forceinline__ int2 own_bins(const SelectSmem<CAP>& sm, int pair) {
+  const u32x4 x = reinterpret_cast<const u32x4*>(sm.hist)[pair];
+  return make_int2((int)(x[0] + x[1]), (int)(x[2] + x[3]));
+}
+
+// The digit in which the need-th largest score lies and its rank among those with that digit.  count: this thread's bins
+// 2047 - 2 tid and 2046 - 2 tid.
+template <int CAP>
+__device__ __forceinline__ void find_digit(SelectSmem<CAP>& sm, const int (&count)[2], int need) {
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const int sum = count[0] + count[1], incl = wave_incl_scan(sum);
+  if ((tid & 63) == 63) sm.wave_sum[wave] = incl;
+  __syncthreads();
+  int before = incl - sum;
+  for (int w = 0; w < wave; ++w) before += sm.wave_sum[w];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    if (before < need && need <= before + count[e]) {
+      sm.digit = kBins - 1 - 2 * tid - e;
+      sm.need = need - before;
+    }
+    before += count[e];
+  }
+  __syncthreads();
+}
+
+// Writes the indices of the scores above the threshold and of the first `need` equal to it, in order; `above` and
+// `equal` of either come before this workgroup's.  Every wave counts, then writes, a part of its own.
+template <int CAP>
+__device__ __forceinline__ void write_kept(SelectSmem<CAP>& sm, int j0, int filled, uint32_t threshold, int need,
+                                           int above, int equal, int32_t* out) {
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int per = filled / kSelectWaves;  // a multiple of 64
+  const uint32_t* const mine = sm.score + wave * per + lane;
+  int na = 0, ne = 0;
+  for (int i = 0; i < per; i += 64 * kBatch) {
+    uint32_t s[kBatch];
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) s[e] = mine[min(i + 64 * e, per - 64)];
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) {
+      if (i + 64 * e >= per) break;
+      na += __builtin_popcountll(__ballot(s[e] > threshold));
+      ne += __builtin_popcountll(__ballot(s[e] == threshold));
+    }
+  }
+  if (lane == 0) *reinterpret_cast<int2*>(&sm.wave_sum[2 * wave]) = make_int2(na, ne);
+  __syncthreads();
+  na = above;
+  ne = equal;
+  for (int w = 0; w < wave; ++w) {
+    na += sm.wave_sum[2 * w];
+    ne += sm.wave_sum[2 * w + 1];
+  }
+  const int first = j0 + wave * per + lane;
+  const auto before = [](uint64_t m) {  // lanes below this one in a mask
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+  };
+  for (int i = 0; i < per; i += 64 * kBatch) {
+    uint32_t s[kBatch];
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) s[e] = mine[min(i + 64 * e, per - 64)];
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) {
+      if (i + 64 * e >= per) break;
+      const uint64_t ma = __ballot(s[e] > threshold), me = __ballot(s[e] == threshold);
+      if (me) {  // rare
+        const int re = ne + before(me);
+        if (s[e] > threshold || (s[e] == threshold && re < need)) out[na + before(ma) + min(re, need)] = first + i + 64 * e;
+      } else if (s[e] > threshold) {
+        out[na + min(ne, need) + before(ma)] = first + i + 64 * e;
+      }
+      na += __builtin_popcountll(ma);
+      ne += __builtin_popcountll(me);
+    }
+  }
+}
+
+struct SelectArgs {
+  const float* weights;
+  const int32_t* key_start;
+  const int32_t* key_count;
+  const int32_t* kept_start;
+  int32_t* kept;
+  int32_t* ws;  // [batch][slices] of SliceWork (long requests)
+  int sink, recent, slices;
+};
+// A slice's counts of each pass's digits.
+struct SliceWork {
+  int hist[3][kBins];
+};
+
+__device__ __forceinline__ bool trivial_selection(const SelectArgs& a, int n, int b, int o0) {
+  if (b >= n) {
+    for (int i = blockIdx.x * kSelectThreads + threadIdx.x; i < b; i += gridDim.x * kSelectThreads)
+      a.kept[o0 + i] = i < n ? i : -1;
+    return true;
+  }
+  return b <= 0;
+}
+
+template <int CAP>
+__global__ __launch_bounds__(kSelectThreads) void select_request(SelectArgs a) {
+  __shared__ SelectSmem<CAP> sm;
+  const int r = blockIdx.y, tid = threadIdx.x;
+  const int k0 = a.key_start[r], room = a.key_start[r + 1] - k0;
+  const int n = min(a.key_count ? max(0, min(a.key_count[r], room)) : room, CAP);
+  const int o0 = a.kept_start[r], b = a.kept_start[r + 1] - o0;
+  if (trivial_selection(a, n, b, o0)) return;
+  const int filled = load_scores<true>(sm, a.weights + k0, 0, n, n, a.sink, a.recent);
+  uint32_t prefix = 0;
+  int need = b;
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    if (pass > 0) count_digits(sm, filled, prefix, pass);
+    const int2 x = own_bins(sm, kSelectThreads - 1 - tid);
+    const int c[2] = {x.y, x.x};
+    find_digit(sm, c, need);
+    prefix = with_digit(prefix, sm.digit, pass);
+    need = sm.need;
+    __syncthreads();
+  }
+  write_kept(sm, 0, filled, prefix, need, 0, 0, a.kept + o0);
+}
+
+// Launch `pass` of a long request's selection: 0 to 2 count a digit, 3 writes.
+template <int PASS>
+__global__ __launch_bounds__(kSelectThreads) void select_slices(SelectArgs a) {
+  __shared__ SelectSmem<kSlice> sm;
+  __shared__ int before_s[2];
+  const int r = blockIdx.y, w = blockIdx.x, tid = threadIdx.x;
+  const int k0 = a.key_start[r], room = a.key_start[r + 1] - k0;
+  const int n = min(a.key_count ? max(0, min(a.key_count[r], room)) : room, a.slices * kSlice);
+  const int o0 = a.kept_start[r], b = a.kept_start[r + 1] - o0;
+  if (b >= n || b <= 0) {
+    if (PASS == 3) trivial_selection(a, n, b, o0);
+    return;
+  }
+  SliceWork* const all = reinterpret_cast<SliceWork*>(a.ws) + (int64_t)r * a.slices;
+  const int used = (n + kSlice - 1) / kSlice;
+  if (w >= used) return;
+  const int j0 = w * kSlice, count = min(kSlice, n - j0);
+  const int filled = load_scores<PASS == 0>(sm, a.weights + k0, j0, count, n, a.sink, a.recent);
+  if (tid < 2) before_s[tid] = 0;
+  // The digits counted so far, from every slice's counts.
+  uint32_t prefix = 0;
+  int need = b;
+#pragma unroll
+  for (int pass = 0; pass < PASS; ++pass) {
+    int c[2] = {0, 0};
+    const int b1 = kBins - 1 - 2 * tid;
+    for (int v0 = 0; v0 < used; v0 += 8) {
+      int2 x[8];
+#pragma unroll
+      for (int v = 0; v < 8; ++v)
+        x[v] = *reinterpret_cast<const int2*>(&all[min(v0 + v, used - 1)].hist[pass][b1 - 1]);
+#pragma unroll
+      for (int v = 0; v < 8; ++v) {
+        c[0] += v0 + v < used ? x[v].y : 0;
+        c[1] += v0 + v < used ? x[v].x : 0;
+      }
+    }
+    find_digit(sm, c, need);
+    const int digit = sm.digit;
+    prefix = with_digit(prefix, digit, pass);
+    need = sm.need;
+    if (PASS == 3) {  // scores of earlier slices above the threshold, and equal to it
+      int above = 0;
+      for (int v0 = 0; v0 < w; v0 += 8) {
+        int2 x[8];
+#pragma unroll
+        for (int v = 0; v < 8; ++v)
+          x[v] = *reinterpret_cast<const int2*>(&all[min(v0 + v, w - 1)].hist[pass][b1 - 1]);
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+          if (v0 + v >= w) continue;
+          above += (b1 > digit ? x[v].y : 0) + (b1 - 1 > digit ? x[v].x : 0);
+          if (pass == 2 && (b1 == digit || b1 - 1 == digit)) atomicAdd(&before_s[1], b1 == digit ? x[v].y : x[v].x);
+        }
+      }
+      above = wave_incl_scan(above);
+      if ((tid & 63) == 63 && above) atomicAdd(&before_s[0], above);
+    }
+    __syncthreads();
+  }
+  if (PASS < 3) {
+    if (PASS > 0) count_digits(sm, filled, prefix, PASS);
+    *reinterpret_cast<int2*>(&all[w].hist[PASS][2 * tid]) = own_bins(sm, tid);
+  } else {
+    write_kept(sm, j0, filled, prefix, need, before_s[0], before_s[1], a.kept + o0);
   }
 }
 
@@ -521,9 +724,28 @@ hipError_t launch_decode_weights(const WeightArgs& a, int head_dim, bool local_k
 #undef CALL
 }
 
+size_t select_workspace(int batch, int max_kv_len) {
+  return max_kv_len <= kMostResident ? 0 : sizeof(SliceWork) * (size_t)batch * ((max_kv_len + kSlice - 1) / kSlice);
+}
+
+// The least instance that holds the longest request: LDS decides how many workgroups share a CU.
 hipError_t launch_select(const float* weights, const int32_t* key_start, const int32_t* key_count,
-                         const int32_t* kept_start, int batch, int sink, int recent, int32_t* kept, hipStream_t s) {
-  select_keys<<<batch, kSelectThreads, 0, s>>>(weights, key_start, key_count, kept_start, sink, recent, kept);
+                         const int32_t* kept_start, int batch, int max_kv_len, int sink, int recent, int32_t* kept,
+                         void* workspace, hipStream_t s) {
+  SelectArgs a = {weights, key_start, key_count, kept_start, kept, static_cast<int32_t*>(workspace), sink, recent, 0};
+  const dim3 one(1, batch);
+  if (max_kv_len <= kSlice) {
+    select_request<kSlice><<<one, kSelectThreads, 0, s>>>(a);
+  } else if (max_kv_len <= kMostResident) {
+    select_request<kMostResident><<<one, kSelectThreads, 0, s>>>(a);
+  } else {
+    a.slices = (max_kv_len + kSlice - 1) / kSlice;
+    const dim3 grid(a.slices, batch);
+    select_slices<0><<<grid, kSelectThreads, 0, s>>>(a);
+    select_slices<1><<<grid, kSelectThreads, 0, s>>>(a);
+    select_slices<2><<<grid, kSelectThreads, 0, s>>>(a);
+    select_slices<3><<<grid, kSelectThreads, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -142,16 +142,21 @@ int lazy_attn_decode_key_weights(const lazy_attn_params_t* p, const void* q, con
                                             static_cast<hipStream_t>(stream)));
 }
 
-size_t lazy_cache_select_workspace_size(int32_t, int32_t) { return 0; }
+size_t lazy_cache_select_workspace_size(int32_t batch, int32_t max_kv_len) {
+  return batch <= 0 || max_kv_len <= 0 ? 0 : lazy::select_workspace(batch, max_kv_len);
+}
 
 int lazy_cache_select(const float* weights, const int32_t* key_start, const int32_t* key_count,
                       const int32_t* kept_start, int32_t batch, int32_t max_kv_len, int32_t sink, int32_t recent,
-                      int32_t* kept, void*, size_t, void* stream) {
+                      int32_t* kept, void* workspace, size_t workspace_bytes, void* stream) {
   if (batch < 0 || max_kv_len < 0 || sink < 0 || recent < 0) return LAZY_EINVAL;
   if (batch == 0) return LAZY_OK;
   if (!key_start || !kept_start || !kept || (max_kv_len > 0 && !weights)) return LAZY_EINVAL;
-  return status(lazy::launch_select(weights, key_start, key_count, kept_start, batch, sink, recent, kept,
-                                    static_cast<hipStream_t>(stream)));
+  if (batch > 65535) return LAZY_EUNSUPPORTED;
+  const size_t need = lazy::select_workspace(batch, max_kv_len);
+  if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15u))) return LAZY_EWORKSPACE;
+  return status(lazy::launch_select(weights, key_start, key_count, kept_start, batch, max_kv_len, sink, recent, kept,
+                                    workspace, static_cast<hipStream_t>(stream)));
 }
 
 int lazy_cache_compact(const lazy_attn_params_t* p, const void* k_pool, const void* v_pool, const lazy_chunk_t* chunks,

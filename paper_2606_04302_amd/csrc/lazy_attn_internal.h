@@ -183,7 +183,9 @@ hipError_t launch_prefill_weights(const WeightArgs& a, int head_dim, bool local_
 hipError_t launch_decode_weights(const WeightArgs& a, int head_dim, bool local_keys, bool interleaved, bool alibi,
                                  hipStream_t stream);
 hipError_t launch_select(const float* weights, const int32_t* key_start, const int32_t* key_count,
-                         const int32_t* kept_start, int batch, int sink, int recent, int32_t* kept, hipStream_t stream);
+                         const int32_t* kept_start, int batch, int max_kv_len, int sink, int recent, int32_t* kept,
+                         void* workspace, hipStream_t stream);
+size_t select_workspace(int batch, int max_kv_len);
 // turn: 0 keys are copied, 1 rotated to their positions, 2 turned from their old local index to the new one.
 hipError_t launch_compact(const CompactArgs& a, int head_dim, int batch, int max_kept, int turn, bool local_keys,
                           bool interleaved, hipStream_t stream);
