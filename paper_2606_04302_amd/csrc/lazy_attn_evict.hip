@@ -202,54 +202,222 @@ __global__ __launch_bounds__(256) void sum_weights(WeightArgs a) {
   }
 }
 
-// Weights of one new token per request: workgroup (key split, request), a wave takes 16 keys of each 64-key tile for all
-// heads, so that their angles are formed once and their sums stay in the wave.  Rotated queries lie in LDS, kRowGroups
-// groups of 16 rows (query heads of one KV head) at a time.  S = Q K^T: a key in lane % 16, rows 4 (lane / 16) + 0..3.
-constexpr int kRowGroups = 8;
-template <int D, int KMI>
-__global__ __launch_bounds__(256) void weigh_token(WeightArgs a) {
+// Weights of one new token per request.  S = Q K^T with 16x16x32 products: a key in lane % 16, query heads
+// 4 (lane / 16) + 0..3 of a group of 16 in its registers, so a key's sum over a group stays in four lanes.  Rotated
+// queries lie in LDS, kTokenRows rows at a time.
+//   HS = 1: workgroup (key split, request); a wave takes 16 keys of each 64-key tile for all KV heads, whose angles it
+//     forms once.
+//   HS = 4: workgroup (16 keys of every tile of a key split, request); its waves share the KV heads and add up their sums
+//     through LDS.  For batches whose tiles alone would leave CUs without work: a wave then waits for a quarter of the
+//     loads.
+// The next head's keys (or the next tile's first) are loaded during a head's products.
+//
+// SORT: requests that share chunks list them in orders of their own.  The records of a request (up to kSortRecords) are
+// walked in the order in which they are stored, and the workgroups of one key split of all requests run on one XCD: they
+// then read the same part of the store at about the same time, through one L2.  Every key's sum is its own, so results
+// do not depend on the order.
+constexpr int kTokenRows = 64, kTokenGroups = 16;  // query rows, and groups of up to 16 of one KV head, held in LDS
+constexpr int kSortRecords = 256;
+struct SortedRecord {
+  int64_t koff;
+  int32_t len, pos, kst, base;  // base: index of its first key among the request's keys
+};
+struct SortedTable {
+  SortedRecord rec[kSortRecords] __attribute__((aligned(16)));
+  uint32_t key[kSortRecords] __attribute__((aligned(16)));
+  int tiles[kSortRecords];  // tiles of the records up to and with this one
+  int wave_sum[4];
+
+  // Sum of x over the threads before this one, and over all.
+  __device__ int before(int x, int& total) {
+    const int tid = threadIdx.x, incl = wave_incl_scan(x);
+    __syncthreads();
+    if ((tid & 63) == 63) wave_sum[tid >> 6] = incl;
+    __syncthreads();
+    int sum = incl - x;
+    for (int w = 0; w < tid >> 6; ++w) sum += wave_sum[w];
+    total = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
+    return sum;
+  }
+  // 256 threads; n <= kSortRecords records in units of 128 KiB of the store, table order within a unit.
+  __device__ void build(const lazy_chunk_t* table, int count, int tk) {
+    const int t = threadIdx.x;
+    lazy_chunk_t c = {};
+    if (t < count) c = table[t];
+    int all;
+    const int base = before(t < count ? c.len : 0, all);
+    const uint32_t own = t < count ? (uint32_t)(c.k_offset >> 16) << 8 | (uint32_t)t : 0xffffffffu;
+    key[t] = own;
+    __syncthreads();
+    int rank = 0;
+    for (int j = 0; j < count; j += 4) {
+      const u32x4 o = *reinterpret_cast<const u32x4*>(key + j);
+      rank += (o[0] < own) + (o[1] < own) + (o[2] < own) + (o[3] < own);
+    }
+    if (t < count) rec[rank] = {c.k_offset, c.len, c.pos_offset, c.k_stride, base};
+    __syncthreads();
+    const int mine = t < count ? (rec[t].len + tk - 1) / tk : 0;
+    tiles[t] = before(mine, all) + mine;
+    __syncthreads();
+  }
+};
+// A request's 64-key tiles, record after record of its table or of the sorted one, with the index of each record's first
+// key among the request's keys.
+template <bool SORT>
+struct TokenIter {
+  const SortedTable* table;
+  cptr<lazy_chunk_t> recs;
+  int i, j0, left, base;
+  bool sorted;
+  Rec cur;
+  __device__ void load() {
+    if (SORT && sorted) {
+      const SortedRecord r = table->rec[i];
+      cur.koff =
+          (int64_t)((uint64_t)(uint32_t)uniform((int)((uint64_t)r.koff >> 32)) << 32 | (uint32_t)uniform((int)r.koff));
+      cur.len = uniform(r.len);
+      cur.pos = uniform(r.pos);
+      cur.kst = uniform(r.kst);
+      base = uniform(r.base);
+    } else {
+      cur = load_rec(recs + i);
+    }
+  }
+  __device__ void start(const lazy_chunk_t* chunks, int c0, int c1, int split, int splits) {
+    KeyIter it;
+    it.start(chunks, c0, c1, split, splits);
+    sorted = false;
+    table = nullptr;
+    recs = it.recs;
+    i = it.i;
+    j0 = it.j0;
+    left = it.left;
+    base = it.base;
+    cur = it.cur;
+  }
+  __device__ void start(const SortedTable* t, int n, int split, int splits) {
+    sorted = true;
+    table = t;
+    recs = nullptr;
+    const int total = n > 0 ? uniform(t->tiles[n - 1]) : 0;
+    const int lo = (int)((int64_t)total * split / splits), hi = (int)((int64_t)total * (split + 1) / splits);
+    left = hi - lo;
+    i = j0 = base = 0;
+    cur = {};
+    if (left <= 0) return;
+    int a = 0, b = n - 1;  // the first record whose tiles reach past lo
+    while (a < b) {
+      const int mid = (a + b) >> 1;
+      if (uniform(t->tiles[mid]) > lo)
+        b = mid;
+      else
+        a = mid + 1;
+    }
+    i = a;
+    load();
+    j0 = (lo - (uniform(t->tiles[i]) - (cur.len + kSub - 1) / kSub)) * kSub;
+  }
+  __device__ void next() {
+    --left;
+    j0 += kSub;
+    if (left <= 0 || j0 < cur.len) return;
+    j0 = 0;
+    do {  // tiles are left, so a record with keys lies ahead
+      if (!(SORT && sorted)) base += cur.len;
+      ++i;
+      load();
+    } while (cur.len == 0);
+  }
+};
+
+template <int D, int KMI, int HS, bool SORT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) void weigh_token(WeightArgs a) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
-  constexpr int QLD = D + kPad, H = D / 64;
-  __shared__ uint16_t q[kRowGroups * 16 * QLD] __attribute__((aligned(16)));
-  __shared__ float nlse[kRowGroups * 16] __attribute__((aligned(16)));
-  __shared__ float rslope[kRowGroups * 16] __attribute__((aligned(16)));
+  constexpr int QLD = D + kPad, H = D / 64, TPR = D / 16;
+  typedef TokenIter<SORT> Iter;
+  __shared__ uint16_t q[kTokenRows * QLD] __attribute__((aligned(16)));
+  __shared__ float nlse[kTokenGroups * 16] __attribute__((aligned(16)));
+  __shared__ float rslope[kTokenGroups * 16] __attribute__((aligned(16)));
   __shared__ double freq[D / 2];
+  __shared__ float2 qcs[D / 2];
+  __shared__ float sums[2][4][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, kq = lane >> 4;
-  const int r = blockIdx.y, qpos = a.q_pos0[r], room = a.key_start[r + 1] - a.key_start[r];
-  if (ROT && tid < D / 2) freq[tid] = theta_rev(tid, D, a.rope_log2_base, a.inv_freq);
-  const int per_head = (a.group + 15) / 16, groups = a.hkv * per_head;
-  for (int g0 = 0; g0 < groups; g0 += kRowGroups) {
-    const int ng = min(kRowGroups, groups - g0);
+  int r = blockIdx.y, split = HS == 1 ? blockIdx.x : blockIdx.x >> 2;
+  const int sub = HS == 1 ? wave : blockIdx.x & 3;
+  if (SORT) {  // the splits' order, an eighth of it for each XCD
+    const int id = blockIdx.x + gridDim.x * blockIdx.y, total = gridDim.x * gridDim.y, per = total >> 3;
+    const int at = id < per << 3 ? (id & 7) * per + (id >> 3) : id;
+    split = at / (int)gridDim.y;
+    r = at - split * (int)gridDim.y;
+  }
+  const int qpos = a.q_pos0[r], room = a.key_start[r + 1] - a.key_start[r];
+  const int c0 = a.chunk_start[r], c1 = a.chunk_start[r + 1];
+  Iter it0;
+  bool sorted = false;
+  if constexpr (SORT) {
+    __shared__ SortedTable table;
+    sorted = c1 - c0 <= kSortRecords;
+    if (sorted) {
+      table.build(a.chunks + c0, c1 - c0, kSub);
+      it0.start(&table, c1 - c0, split, a.splits);
+    }
+  }
+  if (!sorted) it0.start(a.chunks, c0, c1, split, a.splits);
+  if (ROT && tid < D / 2) {
+    const double rev = theta_rev(tid, D, a.rope_log2_base, a.inv_freq);
+    freq[tid] = rev;
+    qcs[tid] = rope_cs(a.rotate_q ? qpos : 0, rev);
+  }
+  const int per_head = (a.group + 15) / 16, groups = a.hkv * per_head, per_group = min(a.group, 16);
+  const int most = min(kTokenGroups, kTokenRows / per_group);
+  for (int g0 = 0; g0 < groups; g0 += most) {
+    const int ng = min(most, groups - g0);
     __syncthreads();
-    constexpr int TPR = D / 16;
-    for (int e = tid; e < ng * 16 * TPR; e += 256) {
-      const int row = e / TPR, t0 = 8 * (e % TPR), grp = g0 + row / 16, in = (grp % per_head) * 16 + row % 16;
-      const bool ok = in < a.group;
-      const int h = (grp / per_head) * a.group + (ok ? in : 0);
+    for (int e = tid; e < ng * per_group * TPR; e += 256) {
+      const int row = e / TPR, t0 = 8 * (e % TPR), grp = g0 + row / per_group;
+      const int in = min((grp % per_head) * 16 + row % per_group, a.group - 1);
       u32x4 lo, hi;
-      load_pairs<D, IL>(a.q + ((int64_t)r * a.hq + h) * D, t0, lo, hi);
+      load_pairs<D, IL>(a.q + ((int64_t)r * a.hq + (grp / per_head) * a.group + in) * D, t0, lo, hi);
       float yl[8], yh[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         yl[k] = element(lo, k);
         yh[k] = element(hi, k);
-        if (a.rotate_q) rotate_by(element(lo, k), element(hi, k), rope_cs(qpos, freq[t0 + k]), yl[k], yh[k]);
+        if (ROT) rotate_by(element(lo, k), element(hi, k), qcs[t0 + k], yl[k], yh[k]);
         yl[k] *= a.scale_log2;
         yh[k] *= a.scale_log2;
       }
       store_pairs<D, false>(q + row * QLD, t0, yl, yh);
-      if (t0 == 0) {
-        const float lse = a.lse[(int64_t)r * a.hq + h];
-        nlse[row] = !ok || lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
-        rslope[row] = ALIBI ? alibi_slope(h, a.hq, a.inv_freq, 1.f) : 0.f;
-      }
+    }
+    for (int e = tid; e < ng * 16; e += 256) {  // rows past a group's end: exp2(score - inf) = 0
+      const int grp = g0 + e / 16, in = (grp % per_head) * 16 + e % 16, h = (grp / per_head) * a.group + in;
+      const float lse = in < a.group ? a.lse[(int64_t)r * a.hq + h] : -INFINITY;
+      nlse[e] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
+      rslope[e] = ALIBI && in < a.group ? alibi_slope(h, a.hq, a.inv_freq, 1.f) : 0.f;
     }
     __syncthreads();
-    KeyIter it;
-    it.start(a.chunks, a.chunk_start[r], a.chunk_start[r + 1], blockIdx.x, a.splits);
-    for (; it.left > 0; it.next()) {
-      const int key = it.j0 + 16 * wave + col;
+    // A wave's groups: first, first + step, ...
+    const int first = HS == 1 ? 0 : wave, step = HS;
+    const auto fetch = [&](const Iter& t, int k, u32x4 (&raw)[H][2]) {
+      const int key = t.j0 + 16 * sub + col;
+      const uint16_t* krow = k_ptr(a.k_pool, t.cur, (g0 + k) / per_head, key < t.cur.len ? key : t.j0, D);
+#pragma unroll
+      for (int s = 0; s < H; ++s) {
+        const int t0 = 32 * s + 8 * kq;
+        raw[s][0] = *reinterpret_cast<const u32x4*>(krow + (IL ? 2 * t0 : t0));
+        raw[s][1] = *reinterpret_cast<const u32x4*>(krow + (IL ? 2 * t0 + 8 : D / 2 + t0));
+      }
+    };
+    Iter it = it0;
+    u32x4 raw[H][2];
+    if (it.left > 0 && first < ng) fetch(it, first, raw);
+    int parity = 0;
+    const uint16_t* const qrow = q + min(col, per_group - 1) * QLD + 8 * kq;
+    while (it.left > 0) {
+      Iter ahead = it;
+      ahead.next();
+      const int key = it.j0 + 16 * sub + col;
       const bool in = key < it.cur.len;
       const int p = it.cur.pos + key;
       float2 cs[H][8];
@@ -260,13 +428,12 @@ __global__ __launch_bounds__(256) void weigh_token(WeightArgs a) {
           for (int e = 0; e < 8; ++e) cs[s][e] = rope_cs(LOCAL ? it.cur.pos : p, freq[32 * s + 8 * kq + e]);
       }
       float sum = 0.f;
-      for (int k = 0; k < ng; ++k) {
-        const uint16_t* krow = k_ptr(a.k_pool, it.cur, (g0 + k) / per_head, in ? key : it.j0, D);
+      for (int k = first; k < ng; k += step) {
         bf16x8 kf[2 * H];
 #pragma unroll
         for (int s = 0; s < H; ++s) {
-          u32x4 lo, hi;
-          load_pairs<D, IL>(krow, 32 * s + 8 * kq, lo, hi);
+          u32x4 lo = raw[s][0], hi = raw[s][1];
+          if (IL) deinterleave8(raw[s][0], raw[s][1], lo, hi);
           if (ROT) {
             float yl[8], yh[8];
 #pragma unroll
@@ -277,12 +444,15 @@ __global__ __launch_bounds__(256) void weigh_token(WeightArgs a) {
           kf[s] = as_bf16x8(lo);
           kf[s + H] = as_bf16x8(hi);
         }
+        if (k + step < ng)
+          fetch(it, k + step, raw);
+        else if (ahead.left > 0)
+          fetch(ahead, first, raw);
         f32x4 s4 = *reinterpret_cast<const f32x4*>(nlse + 16 * k + 4 * kq);
 #pragma unroll
         for (int s = 0; s < 2 * H; ++s)
           s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              as_bf16x8(*reinterpret_cast<const u32x4*>(q + (16 * k + col) * QLD + 32 * s + 8 * kq)), kf[s], s4, 0, 0,
-              0);
+              as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + k * per_group * QLD + 32 * s)), kf[s], s4, 0, 0, 0);
         if (ALIBI) {
           const f32x4 sl = *reinterpret_cast<const f32x4*>(rslope + 16 * k + 4 * kq);
 #pragma unroll
@@ -292,15 +462,22 @@ __global__ __launch_bounds__(256) void weigh_token(WeightArgs a) {
       }
       sum += __shfl_xor(sum, 16, 64);
       sum += __shfl_xor(sum, 32, 64);
+      if (HS > 1) {  // the waves' sums, in their order; two buffers, so one barrier a tile
+        if (kq == 0) sums[parity][wave][col] = sum;
+        __syncthreads();
+        if (wave == 0) sum = (sums[parity][0][col] + sums[parity][1][col]) + (sums[parity][2][col] + sums[parity][3][col]);
+        parity ^= 1;
+      }
       if (a.causal && p > qpos) sum = 0.f;
       const int at = it.base + key;
-      if (kq == 0 && in && at < room) {
+      if ((HS == 1 || wave == 0) && kq == 0 && in && at < room) {
         float* w = a.weights + a.key_start[r] + at;
         if (g0 > 0)
           *w += sum;
         else
           *w = a.weights_in ? fmaf(a.decay, a.weights_in[a.key_start[r] + at], sum) : sum;
       }
+      it = ahead;
     }
   }
 }
@@ -680,7 +857,12 @@ hipError_t prompt_mode(const WeightArgs& a, int max_kv_len, hipStream_t s) {
 }
 template <int D, int KMI>
 hipError_t token_mode(const WeightArgs& a, hipStream_t s) {
-  weigh_token<D, KMI><<<dim3(a.splits, a.batch), 256, 0, s>>>(a);
+  if (a.head_split)
+    weigh_token<D, KMI, 4, false><<<dim3(4 * a.splits, a.batch), 256, 0, s>>>(a);
+  else if (a.sort_records)
+    weigh_token<D, KMI, 1, true><<<dim3(a.splits, a.batch), 256, 0, s>>>(a);
+  else
+    weigh_token<D, KMI, 1, false><<<dim3(a.splits, a.batch), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

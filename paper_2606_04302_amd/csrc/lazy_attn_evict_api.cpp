@@ -12,6 +12,7 @@ namespace {
 using lazy::ceil_div, lazy::check_params, lazy::kNumCUs;
 
 constexpr int kTileKeys = 64;
+constexpr int64_t kSortBytes = 512 << 10;
 
 int status(hipError_t e) { return e == hipSuccess ? LAZY_OK : LAZY_EHIP; }
 
@@ -134,8 +135,13 @@ int lazy_attn_decode_key_weights(const lazy_attn_params_t* p, const void* q, con
   a.weights = weights;
   a.total_q = batch;
   a.batch = batch;
-  // Four workgroups a CU, at least one tile each.
-  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(4 * kNumCUs, batch), ceil_div(max_kv_len, kTileKeys)));
+  // Four workgroups a CU, at least one tile each; where there are fewer tiles than that, four workgroups a tile.
+  const int64_t tiles = ceil_div(max_kv_len, kTileKeys);
+  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(4 * kNumCUs, batch), tiles));
+  a.head_split = p->num_kv_heads > 1 && tiles * batch <= kNumCUs;
+  // Storage order: where a workgroup reads enough for the caches to matter (sorting takes it 1-2 us).
+  a.sort_records = batch > 1 && !a.head_split &&
+                   (int64_t)max_kv_len / a.splits * p->num_kv_heads * p->head_dim * 2 >= kSortBytes;
   a.decay = decay;
   return status(lazy::launch_decode_weights(a, p->head_dim, p->key_positions == LAZY_KEYS_LOCAL,
                                             p->rope_style == LAZY_ROPE_INTERLEAVED, p->rope_style == LAZY_ALIBI,

@@ -139,6 +139,8 @@ struct WeightArgs {
   int32_t rotate_q;
   int32_t splits;             // key splits of a request
   int32_t row_splits;
+  int32_t sort_records;       // single tokens: 1 walks a request's records in storage order
+  int32_t head_split;         // single tokens: 1 where the waves of a workgroup share the heads
   int32_t num_keys;
   float decay;
   double rope_log2_base;
