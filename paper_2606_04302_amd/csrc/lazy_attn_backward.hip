@@ -1,9 +1,9 @@
 // Backward pass of the prefill attention for gfx950: gradients of the queries and of the stored keys and values.
 //
 // Four launches.  (1) prepare_rows: queries rotated to their positions, times scale * log2 e, in bf16 and packed by KV
-// head (row = token * G + head in group), and two numbers a row, -lse log2 e and -delta.  (2) grad_kv: dk and dv, one
-// 64-key tile of the store at a time.  (3) grad_q: partial dq, one row tile and key split at a time.  (4) finish_rows:
-// partial dq summed, turned back and rounded (and merge_tiles: the same for tiles whose uses were cut into parts).
+// head (row = token * G + head in group), dO packed alike, and two numbers a row, -lse log2 e and -delta.  (2) grad_kv: dk
+// and dv, one tile of the store at a time.  (3) grad_q: partial dq, one row tile and key split at a time.  (4) finish:
+// partial dq summed, turned back and rounded, and the same for tiles whose uses were cut into parts.
 // The probabilities are recomputed in (2) and in (3): seven products of the two kernels against five if dq were summed
 // over key tiles with atomics, whose order would change results from call to call.
 //
@@ -25,16 +25,19 @@ namespace {
 
 constexpr int kMaxBlockTokens = 16;
 
-// Queries rotated, scaled and packed by KV head; row constants.  One workgroup a block of tokens, D / 16 threads a row.
+// Queries rotated, scaled and packed by KV head; row constants.  One workgroup a block of tokens, D / 16 threads a row;
+// workgroups past the last block write the table of angles.
 template <int D, bool IL>
-__global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
+__global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
   __shared__ float2 cs[kMaxBlockTokens][D / 2];
+  if ((int)blockIdx.x >= blocks) {
+    if (a.rotate_k) angle_rows<D>(a, blockIdx.x - blocks);
+    return;
+  }
   const GradBlock b = a.blocks[blockIdx.x];
   if (a.rotate_q) {
-    for (int e = threadIdx.x; e < b.tokens * (D / 2); e += 256) {
-      const int t = e % (D / 2);
-      cs[e / (D / 2)][t] = rope_cs(b.t0 + e / (D / 2) + b.pos_shift, theta_rev(t, D, a.rope_log2_base, a.inv_freq));
-    }
+    for (int e = threadIdx.x; e < b.tokens * (D / 2); e += 256)
+      cs[e / (D / 2)][e % (D / 2)] = rope_cs(b.t0 + e / (D / 2) + b.pos_shift, revolutions(a, e % (D / 2)));
     __syncthreads();
   }
   constexpr int TPR = D / 16;
@@ -75,27 +78,6 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
   }
 }
 
-// Angles of the first kGradTileKeys positions, which every tile's keys add to the position of their key 0.
-template <int D>
-__global__ __launch_bounds__(256) void angle_rows(GradArgs a) {
-  const int e = blockIdx.x * 256 + threadIdx.x, t = e % (D / 2);
-  reinterpret_cast<float2*>(a.ws_angles)[e] = rope_cs(e / (D / 2), theta_rev(t, D, a.rope_log2_base, a.inv_freq));
-}
-
-// Rows of 16-byte chunks copied to a tile in LDS without passing through registers: lane l of a wave writes the 16 bytes
-// at 16 l from a uniform base, so the tile's permutation of chunks is made by the lanes' source addresses.
-__device__ __forceinline__ void copy_async(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
-                                   (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
-}
-// Every copy and LDS access so far has ended; nothing moves across.
-__device__ __forceinline__ void wait_copies() {
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
-
 // Key and value gradients.  A workgroup owns a tile of two 64-key halves, each of its four waves 32 keys: K (rotated) stays
 // in registers and V in LDS, as the right-hand operands of S = Q K^T and dP = dO V^T, whose accumulators have a key in
 // every lane and 32 query rows in registers and lane halves; P and dS leave them as the right-hand operands of
@@ -129,11 +111,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   int* const rpos = rpos_all[wave];
   float* const rslope = rslope_all[wave];
   float2* const turn = turn_all[wave];
-  const double rev = ROT ? theta_rev(lane % (D / 2), D, a.rope_log2_base, a.inv_freq) : 0.0;
+  const double rev = ROT ? revolutions(a, lane % (D / 2)) : 0.0;
   const float2* angles = reinterpret_cast<const float2*>(a.ws_angles);
   const int own_key = min(key, t.keys - 1);  // lanes past the last key repeat it; their columns are not stored
 
-  bf16x8 kf[D / 16];
+  u32x4 kf[D / 16];
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = f32x16{};
@@ -170,6 +152,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     if (row0 == seg.row_begin) {  // a new use: its keys, and dk turned on to its frame
       const int l = again(lane);
       const int here = LOCAL ? seg.half[hf].record_pos : pos;
+      load_keys<D, IL>(krow, l >> 5, kf);
       if (ROT) {
         if (!first && here != frame) {
           if (l < D / 2) turn[l] = rope_cs(here - frame, rev);
@@ -190,28 +173,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if (l < D / 2) turn[l] = rope_cs(here, rev);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        const int t0 = 16 * s + 8 * (l >> 5);
-        u32x4 lo, hi;
-        load_pairs<D, IL>(krow, t0, lo, hi);
-        if (ROT) {
-          float yl[8], yh[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (LOCAL)
-              rotate_by(element(lo, e), element(hi, e), turn[t0 + e], yl[e], yh[e]);
-            else
-              rotate_pair(element(lo, e), element(hi, e), turn[t0 + e], angles[(k32 + (l & 31)) * (D / 2) + t0 + e],
-                          yl[e], yh[e]);
-          }
-          lo = pack8(yl);
-          hi = pack8(yh);
-        }
-        kf[s] = as_bf16x8(lo);
-        kf[s + D / 32] = as_bf16x8(hi);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      rotate_keys<D, KM, IL, 2>(kf, l >> 5, turn, [&](int t) {
+        return *reinterpret_cast<const f32x4*>(angles + (k32 + (l & 31)) * (D / 2) + t);
+      });
       frame = here;
       first = false;
     }
@@ -238,7 +202,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(tq, 0, k), kf[k], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(tq, 0, k), as_bf16x8(kf[k]), s, 0, 0, 0);
       const bf16x8 fv = as_bf16x8(*reinterpret_cast<const u32x4*>(tv[wave] + 512 * k + 8 * lane));
       dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(td, 0, k), fv, dp, 0, 0, 0);
       if (k & 1) __builtin_amdgcn_sched_barrier(0);
@@ -383,34 +347,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             *reinterpret_cast<const u32x4*>(stage + tile_at<D>(row, chunk));
     }
     wait_copies();
-  }
-}
-
-// Sum of a tile's parts, in their order.  Workgroup: one (tile, KV head); D / 16 threads a key.
-template <int D, bool IL>
-__global__ __launch_bounds__(256) void merge_tiles(GradArgs a) {
-  const int g = blockIdx.x % a.hkv;
-  const GradMerge* const m = a.merges + blockIdx.x / a.hkv;
-  constexpr int TPR = D / 16;
-  const int t0 = 8 * (threadIdx.x % TPR);
-  for (int row = threadIdx.x / TPR; row < 2 * kGradHalves * kGradTileKeys; row += 256 / TPR) {
-    const bool values = row / kGradTileKeys % 2;
-    const int key = row % kGradTileKeys;
-    const GradHalf h = m->half[row / (2 * kGradTileKeys)];
-    if (key >= h.keys) continue;
-    float lo[8] = {}, hi[8] = {};
-    for (int p = m->part; p < m->part + m->parts; ++p) {
-      const float* src = a.ws_parts + (((int64_t)p * a.hkv + g) * 2 * kGradHalves * kGradTileKeys + row) * D + t0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        lo[e] += src[e];
-        hi[e] += src[D / 2 + e];
-      }
-    }
-    if (values)
-      store_pairs<D, false>(a.dv_pool + h.v_off + ((int64_t)g * h.vst + key) * D, t0, lo, hi);
-    else
-      store_pairs<D, IL>(a.dk_pool + h.k_off + ((int64_t)g * h.kst + key) * D, t0, lo, hi);
   }
 }
 
@@ -578,7 +514,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int qmax = uniform(token_of(qs * a.group + min(item.row0 + 32 * NW, nrows) - 1, a.group_magic) + shift);
 
   if (ROT) {
-    const double rev = theta_rev(tid % (D / 2), D, a.rope_log2_base, a.inv_freq);
+    const double rev = revolutions(a, tid % (D / 2));
     if (tid < D / 2) sm.freq[tid] = rev;
     for (int e = tid; e < kAngleRows * (D / 2); e += NT)
       *reinterpret_cast<float2*>(sm.csd + e / (D / 2) * S::CSD_LD + cs_idx<D>(e % (D / 2))) = rope_cs(e / (D / 2), rev);
@@ -656,32 +592,68 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
           f32x4{dq[db][4 * q4], dq[db][4 * q4 + 1], dq[db][4 * q4 + 2], dq[db][4 * q4 + 3]};
 }
 
-// Partial query gradients summed in the order of the splits, turned back from the rows' positions, scaled, rounded.
+// Keys of a tile's parts that a workgroup sums, and workgroups a (tile, KV head).
+constexpr int kMergeRows = 32, kMergeBlocks = 2 * kGradHalves * kGradTileKeys / kMergeRows;
+
+// Partial results added up in their order, two kinds of workgroups in one launch.  The first `blocks`: partial query
+// gradients of a block of tokens, turned back from the rows' positions, scaled, rounded.  The others: 32 rows of the key
+// or value gradients of a tile whose uses were cut into parts.  D / 16 threads a row.
 template <int D, bool IL>
-__global__ __launch_bounds__(256) void finish_rows(GradArgs a) {
+__global__ __launch_bounds__(256) void finish(GradArgs a, int blocks) {
+  constexpr int TPR = D / 16;
+  const int t0 = 8 * (threadIdx.x % TPR);
+  const auto sum = [&](const float* p, int64_t stride, int count, float (&lo)[8], float (&hi)[8]) {
+    for (int s0 = 0; s0 < count; s0 += 4) {
+      f32x4 x[4][4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const float* src = p + min(s0 + s, count - 1) * stride + t0;
+        x[s][0] = reinterpret_cast<const f32x4*>(src)[0];
+        x[s][1] = reinterpret_cast<const f32x4*>(src)[1];
+        x[s][2] = reinterpret_cast<const f32x4*>(src + D / 2)[0];
+        x[s][3] = reinterpret_cast<const f32x4*>(src + D / 2)[1];
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        if (s0 + s >= count) break;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          lo[e] += x[s][e >> 2][e & 3];
+          hi[e] += x[s][2 + (e >> 2)][e & 3];
+        }
+      }
+    }
+  };
+  if ((int)blockIdx.x >= blocks) {
+    const int id = blockIdx.x - blocks, g = id / kMergeBlocks % a.hkv;
+    const GradMerge* const m = a.merges + id / (kMergeBlocks * a.hkv);
+    for (int i = threadIdx.x / TPR; i < kMergeRows; i += 256 / TPR) {
+      const int row = id % kMergeBlocks * kMergeRows + i, key = row % kGradTileKeys;
+      const GradHalf h = m->half[row / (2 * kGradTileKeys)];
+      if (key >= h.keys) continue;
+      float lo[8] = {}, hi[8] = {};
+      const int64_t stride = (int64_t)a.hkv * 2 * kGradHalves * kGradTileKeys * D;
+      sum(a.ws_parts + m->part * stride + ((int64_t)g * 2 * kGradHalves * kGradTileKeys + row) * D, stride, m->parts, lo,
+          hi);
+      if (row / kGradTileKeys % 2)
+        store_pairs<D, false>(a.dv_pool + h.v_off + ((int64_t)g * h.vst + key) * D, t0, lo, hi);
+      else
+        store_pairs<D, IL>(a.dk_pool + h.k_off + ((int64_t)g * h.kst + key) * D, t0, lo, hi);
+    }
+    return;
+  }
   __shared__ float2 cs[kMaxBlockTokens][D / 2];
   const GradBlock b = a.blocks[blockIdx.x];
   if (a.rotate_q) {
-    for (int e = threadIdx.x; e < b.tokens * (D / 2); e += 256) {
-      const int t = e % (D / 2);
-      cs[e / (D / 2)][t] = rope_cs(-(b.t0 + e / (D / 2) + b.pos_shift), theta_rev(t, D, a.rope_log2_base, a.inv_freq));
-    }
+    for (int e = threadIdx.x; e < b.tokens * (D / 2); e += 256)
+      cs[e / (D / 2)][e % (D / 2)] = rope_cs(-(b.t0 + e / (D / 2) + b.pos_shift), revolutions(a, e % (D / 2)));
     __syncthreads();
   }
-  constexpr int TPR = D / 16;
-  const int t0 = 8 * (threadIdx.x % TPR);
   for (int row = threadIdx.x / TPR; row < b.tokens * a.hq; row += 256 / TPR) {
     const int tok = row / a.hq, h = row % a.hq;
     const int64_t src = (int64_t)(h / a.group) * a.rows + (int64_t)(b.t0 + tok) * a.group + h % a.group;
     float lo[8] = {}, hi[8] = {};
-    for (int s = 0; s < b.splits; ++s) {
-      const float* p = a.ws_dq + ((int64_t)s * a.hkv * a.rows + src) * D + t0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        lo[e] += p[e];
-        hi[e] += p[D / 2 + e];
-      }
-    }
+    sum(a.ws_dq + src * D, a.hkv * a.rows * D, b.splits, lo, hi);
     const float scale = a.scale_log2 * kLn2;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -696,10 +668,8 @@ __global__ __launch_bounds__(256) void finish_rows(GradArgs a) {
 template <int D, int KMI>
 hipError_t launch(const GradArgs& a, const lazy_backward_info_t& i, hipStream_t stream) {
   constexpr bool IL = interleaved_of(KMI);
-  if (i.num_blocks) prepare_rows<D, IL><<<i.num_blocks, 256, 0, stream>>>(a);
-  if (i.num_tiles) angle_rows<D><<<kGradTileKeys * (D / 2) / 256, 256, 0, stream>>>(a);
+  prepare_rows<D, IL><<<i.num_blocks + kAngleBlocks<D>, 256, 0, stream>>>(a, i.num_blocks);
   if (i.num_tiles) grad_kv<D, KMI><<<i.num_tiles * a.hkv, 256, 0, stream>>>(a);
-  if (i.num_merges) merge_tiles<D, IL><<<i.num_merges * a.hkv, 256, 0, stream>>>(a);
   if (i.num_row_items) {
     if constexpr (D == 128) {
       if (i.row_blocks == 2)
@@ -709,8 +679,9 @@ hipError_t launch(const GradArgs& a, const lazy_backward_info_t& i, hipStream_t 
     } else {
       grad_q<D, KMI, 4, 2><<<i.num_row_items * a.hkv, 256, 0, stream>>>(a);
     }
-    finish_rows<D, IL><<<i.num_blocks, 256, 0, stream>>>(a);
   }
+  const int merges = i.num_merges * a.hkv * kMergeBlocks;
+  if (i.num_blocks + merges) finish<D, IL><<<i.num_blocks + merges, 256, 0, stream>>>(a, i.num_blocks);
   return hipGetLastError();
 }
 

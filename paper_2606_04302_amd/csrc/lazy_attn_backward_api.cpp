@@ -64,7 +64,8 @@ extern "C" int lazy_attn_prefill_backward(const lazy_attn_params_t* p, const voi
   a.group_magic = a.group == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
   a.causal = p->causal;
   a.rotate_q = !p->q_prerotated && p->rope_style != LAZY_ALIBI;
-  a.rope_log2_base = lazy::rope_log2_base(p);
+  a.rotate_k = p->rope_style != LAZY_ALIBI;
+  lazy::rope_revolutions(p, a.rev);
   a.scale_log2 = lazy::scale_log2(p);
   const hipError_t err =
       lazy::launch_backward(a, p->head_dim, p->key_positions == LAZY_KEYS_LOCAL,

@@ -232,7 +232,7 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
   std::vector<GradBlock> blocks;
   std::vector<int64_t> row_cost;
   int32_t row_slots = 0;
-  const int block_tokens = std::max(1, std::min(16, 64 / p->num_q_heads));
+  const int block_tokens = std::max(1, std::min(16, 32 / p->num_q_heads));
   for (int r = 0; r < batch; ++r) {
     const int32_t qs = q_start[r], n = q_start[r + 1] - qs;
     if (n == 0) continue;

@@ -15,9 +15,13 @@ namespace {
 struct KeyIter : TileIter<kSub> {
   int base;  // index of the current record's key 0
   __device__ void start(const lazy_chunk_t* table, int c0, int c1, int split, int splits) {
-    init(table, c0, c1, split, splits);
-    int sum = 0;
-    for (int k = c0 + (threadIdx.x & 63); k < i; k += 64) sum += table[k].len;
+    const First first = first_block(table, c0, c1);
+    init(table, c0, c1, split, splits, first);
+    const int lane = threadIdx.x & 63;
+    int sum = 0;  // keys of the records before i
+#pragma unroll
+    for (int u = 0; u < 4; ++u) sum += c0 + 64 * u + lane < i ? (u == 0 ? first.mine.len : first.len[u - 1]) : 0;
+    for (int k = c0 + 256 + lane; k < i; k += 64) sum += table[k].len;
     base = __builtin_amdgcn_readlane(wave_incl_scan(sum), 63);
   }
   __device__ void next() {
@@ -36,13 +40,17 @@ struct KeyIter : TileIter<kSub> {
   }
 };
 
-constexpr int kRowStep = 32;
-constexpr int kPrepTokens = 8;
+constexpr int kPrepTokens = 2;
 
-// Queries rotated, scaled and packed by KV head, and -lse log2 e of each row.
+// Queries rotated, scaled and packed by KV head, and -lse log2 e of each row; workgroups past the last block write the
+// table of angles.
 template <int D, bool IL>
-__global__ __launch_bounds__(256) void prepare_queries(WeightArgs a) {
+__global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks) {
   __shared__ float2 cs[kPrepTokens][D / 2];
+  if ((int)blockIdx.x >= blocks) {
+    if (a.rotate_k) angle_rows<D>(a, blockIdx.x - blocks);
+    return;
+  }
   const int first = blockIdx.x * kPrepTokens, tokens = min(kPrepTokens, a.total_q - first);
   if (a.rotate_q) {
     for (int e = threadIdx.x; e < tokens * (D / 2); e += 256) {
@@ -55,8 +63,7 @@ __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a) {
         else
           hi = mid;
       }
-      cs[e / (D / 2)][t] =
-          rope_cs(a.q_pos0[lo] + tok - a.q_start[lo], theta_rev(t, D, a.rope_log2_base, a.inv_freq));
+      cs[e / (D / 2)][t] = rope_cs(a.q_pos0[lo] + tok - a.q_start[lo], revolutions(a, t));
     }
     __syncthreads();
   }
@@ -86,90 +93,170 @@ __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a) {
 }
 
 // Weights of a prompt: workgroup (key split and row split, KV head, request), four waves with a 64-key tile each, whose
-// rotated keys stay in registers while the rows of the request pass through LDS.  S = Q K^T has a key in every lane and
-// 32 rows in registers and lane halves, so a key's sum never leaves its lane.
+// rotated keys stay in registers while the rows of the request pass through LDS, kStepRows at a time, copied to the other
+// of two buffers during the products.  S = Q K^T has a key in every lane and 32 rows in registers and lane halves, so a
+// key's sum never leaves its lane.
+constexpr int kStepRows = 64;
 template <int D, int KMI>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void weigh_prompt(WeightArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) void weigh_prompt(WeightArgs a) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
-  constexpr int C = D / 8;
-  __shared__ uint16_t tq[kRowStep * D] __attribute__((aligned(16)));
-  __shared__ float nlse[kRowStep] __attribute__((aligned(16)));
-  __shared__ int rpos[kRowStep] __attribute__((aligned(16)));
-  __shared__ float rslope[kRowStep] __attribute__((aligned(16)));
-  __shared__ double freq[D / 2];
+  constexpr int C = D / 8, COPIES = kStepRows * C / 256;
+  __shared__ uint16_t tq0[kStepRows * D] __attribute__((aligned(16)));
+  __shared__ float nl0[kStepRows] __attribute__((aligned(16)));
+  __shared__ uint16_t tq1[kStepRows * D] __attribute__((aligned(16)));
+  __shared__ float nl1[kStepRows] __attribute__((aligned(16)));
+  __shared__ int rpos_all[4][kStepRows] __attribute__((aligned(16)));
+  __shared__ float rslope_all[4][kStepRows] __attribute__((aligned(16)));
+  __shared__ float2 turn_all[4][D / 2] __attribute__((aligned(16)));
+  // Angles of positions 0 .. 31, one row each; 16-byte chunk c of row r at place c ^ (r % 16).
+  __shared__ float trows[KM == kKeysNope ? 32 * D : 4] __attribute__((aligned(16)));
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), h2 = lane >> 5;
   const int r = blockIdx.z, g = blockIdx.y, split = blockIdx.x % a.splits, rs = blockIdx.x / a.splits;
   const int qs = a.q_start[r], nrows = (a.q_start[r + 1] - qs) * a.group, shift = a.q_pos0[r] - qs;
-  const int steps = (nrows + kRowStep - 1) / kRowStep;
-  const int row_begin = qs * a.group + (int)((int64_t)steps * rs / a.row_splits) * kRowStep;
-  const int row_end = qs * a.group + min(nrows, (int)((int64_t)steps * (rs + 1) / a.row_splits) * kRowStep);
+  const int steps = (nrows + kStepRows - 1) / kStepRows;
+  const int row_begin = qs * a.group + (int)((int64_t)steps * rs / a.row_splits) * kStepRows;
+  const int row_end = qs * a.group + min(nrows, (int)((int64_t)steps * (rs + 1) / a.row_splits) * kStepRows);
   const int room = a.key_start[r + 1] - a.key_start[r];
-  if (ROT && tid < D / 2) freq[tid] = theta_rev(tid, D, a.rope_log2_base, a.inv_freq);
+  const double rev = ROT ? revolutions(a, lane % (D / 2)) : 0.0;
+  const uint16_t* qbase = a.ws_q + (int64_t)g * a.rows * D;
+  const float* nbase = a.ws_nlse + (int64_t)g * a.rows;
+  const auto fetch = [&](int row0, uint16_t* tq, float* nl) {
+    const int most = row_end - 1 - row0;  // rows past the end repeat the last one; they are masked
+    const int e0 = again(tid);
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) {
+      const int row = (256 * i + e0) / C, chunk = ((256 * i + e0) % C) ^ swizzle<D>(row & 31);
+      copy_async(qbase + (int64_t)row0 * D + min(row, most) * D + 8 * chunk, tq + 2048 * i + 512 * wave);
+    }
+    if (e0 < 64)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(nbase + row0 + min(e0, most)),
+                                       (__attribute__((address_space(3))) uint32_t*)nl, 4, 0, 0);
+  };
+  if (KM == kKeysNope) {
+    const int e0 = again(tid);
+#pragma unroll
+    for (int i = 0; i < 32 * D / 1024; ++i) {
+      const int row = (256 * i + e0) / (D / 4), chunk = ((256 * i + e0) % (D / 4)) ^ (row & 15);
+      copy_async(a.ws_angles + row * D + 4 * chunk, trows + 1024 * i + 256 * wave);
+    }
+  }
+  if (row_begin < row_end) fetch(row_begin, tq0, nl0);
   KeyIter it;
   it.start(a.chunks, a.chunk_start[r], a.chunk_start[r + 1], split, a.splits);
   const int rounds = (it.left + 3) / 4;
   it.skip(wave);
   __syncthreads();
-  const uint16_t* qbase = a.ws_q + (int64_t)g * a.rows * D;
   float* part = a.ws_part + (int64_t)(rs * a.hkv + g) * a.num_keys + a.key_start[r];
+  int* const rpos = rpos_all[wave];
+  float* const rslope = rslope_all[wave];
   for (int round = 0; round < rounds; ++round) {
     const bool have = it.left > 0;
     const int nvalid = have ? min(kSub, it.cur.len - it.j0) : 0, b0 = have ? it.cur.pos + it.j0 : 0;
-    bf16x8 kf[2][D / 16];
+    u32x4 kf[2][D / 16];
     float acc[2] = {0.f, 0.f};
     if (have) {
 #pragma unroll
+      for (int b = 0; b < 2; ++b)
+        load_keys<D, IL>(k_ptr(a.k_pool, it.cur, g, it.j0 + min(32 * b + (lane & 31), nvalid - 1), D), h2, kf[b]);
+    }
+    if (KM == kKeysNope && round == 0) {  // the first wait: angle rows (and the first query rows) in LDS for all
+      wait_copies();
+      __syncthreads();
+    }
+    if (have) {
+      // Local-position keys turn by their record's position, the others by that of their 32-key block and a row's.
+#pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int key = 32 * b + (lane & 31);
-        load_keys<D, KM, IL>(k_ptr(a.k_pool, it.cur, g, it.j0 + min(key, nvalid - 1), D), h2,
-                             LOCAL ? it.cur.pos : b0 + key, freq, kf[b]);
+        if (ROT && (b == 0 || !LOCAL)) {
+          if (lane < D / 2) turn_all[wave][lane] = rope_cs(LOCAL ? it.cur.pos : b0 + 32 * b, rev);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        rotate_keys<D, KM, IL, 1>(kf[b], h2, turn_all[wave], [&](int t) {
+          return *reinterpret_cast<const f32x4*>(trows + (lane & 31) * D + 4 * ((t / 2) ^ (lane & 15)));
+        });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
     }
-    for (int row0 = row_begin; row0 < row_end; row0 += kRowStep) {
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kRowStep * C / 256; ++i) {
-        const int e = 256 * i + tid, row = e / C, chunk = e % C;
-        *reinterpret_cast<u32x4*>(tq + tile_at<D>(row, chunk)) = *reinterpret_cast<const u32x4*>(
-            qbase + (int64_t)min(row0 + row, row_end - 1) * D + 8 * chunk);
+    const auto compute = [&](int row0, const uint16_t* tq, const float* nl) {
+      const int rows = min(kStepRows, row_end - row0);
+      const int qmin = token_of(row0, a.group_magic) + shift, qmax = token_of(row0 + rows - 1, a.group_magic) + shift;
+      if (!have || (a.causal && b0 > qmax)) return;
+      const bool masked = (a.causal && b0 + kSub - 1 > qmin) || rows < kStepRows;
+      if (ALIBI || masked) {
+        const int src = row0 + lane, tok = token_of(src, a.group_magic);
+        rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + shift : INT32_MAX;
+        if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
-      if (tid < kRowStep) {
-        const int src = row0 + tid, tok = token_of(src, a.group_magic);
-        nlse[tid] = src < row_end ? a.ws_nlse[(int64_t)g * a.rows + src] : -INFINITY;
-        rpos[tid] = tok + shift;
-        if (ALIBI) rslope[tid] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
-      }
-      __syncthreads();
-      const int qmin = token_of(row0, a.group_magic) + shift;
-      const int qmax = token_of(min(row0 + kRowStep, row_end) - 1, a.group_magic) + shift;
-      if (!have || (a.causal && b0 > qmax)) continue;
-      const TileOperands<D> op(lane);
-      f32x16 s[2];
+      const TileOperands<D> op(again(lane));
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(nlse + 8 * q4 + 4 * h2);
+      for (int half = 0; half < kStepRows / 32; ++half) {
+        f32x16 s[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[0][4 * q4 + e] = s[1][4 * q4 + e] = x[e];
-      }
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(nl + 32 * half + 8 * q4 + 4 * h2);
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        const bf16x8 fq = op.row(tq, 0, k);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq, kf[b][k], s[b], 0, 0, 0);
-      }
-      const bool masked = a.causal && b0 + kSub - 1 > qmin;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int p = b0 + 32 * b + (lane & 31);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
-          if (ALIBI) s[b][i] = fmaf(rslope[row], (float)(p - rpos[row]), s[b][i]);
-          s[b][i] = fast_exp2(s[b][i]);
-          if (masked) s[b][i] = p <= rpos[row] ? s[b][i] : 0.f;
-          acc[b] += s[b][i];
+          for (int e = 0; e < 4; ++e) s[0][4 * q4 + e] = s[1][4 * q4 + e] = x[e];
         }
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const bf16x8 fq = op.row(tq, 32 * half, k);
+#pragma unroll
+          for (int b = 0; b < 2; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq, as_bf16x8(kf[b][k]), s[b], 0, 0, 0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (ALIBI) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int row = 32 * half + 8 * (i >> 2) + 4 * h2 + (i & 3);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+              s[b][i] = fmaf(rslope[row], (float)(b0 + 32 * b + (lane & 31) - rpos[row]), s[b][i]);
+          }
+        }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int last = rpos[32 * half + 8 * (i >> 2) + 4 * h2 + (i & 3)];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              const int p = a.causal ? b0 + 32 * b + (lane & 31) : 0;
+              s[b][i] = p <= last ? s[b][i] : -INFINITY;
+            }
+          }
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float sum[2] = {0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[i & 1] += fast_exp2(s[b][i]);
+          acc[b] += sum[0] + sum[1];
+        }
+      }
+    };
+    // The first rows lie in buffer 0 at the start of every round.
+    for (int row0 = row_begin; row0 < row_end; row0 += 2 * kStepRows) {
+      const int second = row0 + kStepRows, third = row0 + 2 * kStepRows;
+      wait_copies();
+      __syncthreads();
+      if (second < row_end) fetch(second, tq1, nl1);
+      compute(row0, tq0, nl0);
+      if (second < row_end) {
+        wait_copies();
+        __syncthreads();
+      }
+      // what comes next into buffer 0: the third step, or the next round's first
+      if (second < row_end) {
+        if (third < row_end)
+          fetch(third, tq0, nl0);
+        else if (round + 1 < rounds)
+          fetch(row_begin, tq0, nl0);
+        compute(second, tq1, nl1);
+      } else if (round + 1 < rounds && row0 != row_begin) {
+        __syncthreads();
+        fetch(row_begin, tq0, nl0);
       }
     }
     if (have) {
@@ -182,6 +269,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
     it.skip(4);
   }
+  wait_copies();
 }
 
 // Partial sums of the row splits and KV heads added up in their order.  Keys behind the table's last one are left alone.
@@ -365,7 +453,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
   }
   if (!sorted) it0.start(a.chunks, c0, c1, split, a.splits);
   if (ROT && tid < D / 2) {
-    const double rev = theta_rev(tid, D, a.rope_log2_base, a.inv_freq);
+    const double rev = revolutions(a, tid);
     freq[tid] = rev;
     qcs[tid] = rope_cs(a.rotate_q ? qpos : 0, rev);
   }
@@ -788,7 +876,7 @@ __global__ __launch_bounds__(256) void gather_keys(CompactArgs a) {
   int want = tid < kGather && i < count ? a.kept[o0 + i] : -1;
   const int asked = want;
   if (tid < kGather) ksrc[tid] = -1;
-  if (TURN && tid < D / 2) freq[tid] = theta_rev(tid, D, a.rope_log2_base, a.inv_freq);
+  if (TURN && tid < D / 2) freq[tid] = revolutions(a, tid);
   const lazy_chunk_t dst = a.dst[r];
   int base = 0;
   for (int c0 = a.chunk_start[r]; c0 < a.chunk_start[r + 1]; c0 += 256) {
@@ -849,8 +937,8 @@ __global__ __launch_bounds__(256) void gather_keys(CompactArgs a) {
 
 template <int D, int KMI>
 hipError_t prompt_mode(const WeightArgs& a, int max_kv_len, hipStream_t s) {
-  if (a.total_q > 0)
-    prepare_queries<D, interleaved_of(KMI)><<<(a.total_q + kPrepTokens - 1) / kPrepTokens, 256, 0, s>>>(a);
+  const int blocks = (a.total_q + kPrepTokens - 1) / kPrepTokens;
+  prepare_queries<D, interleaved_of(KMI)><<<blocks + kAngleBlocks<D>, 256, 0, s>>>(a, blocks);
   weigh_prompt<D, KMI><<<dim3(a.splits * a.row_splits, a.hkv, a.batch), 256, 0, s>>>(a);
   sum_weights<<<dim3((max_kv_len + 255) / 256, a.batch), 256, 0, s>>>(a);
   return hipGetLastError();

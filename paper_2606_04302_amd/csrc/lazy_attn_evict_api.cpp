@@ -18,7 +18,7 @@ int status(hipError_t e) { return e == hipSuccess ? LAZY_OK : LAZY_EHIP; }
 
 struct PromptSizes {
   int splits, row_splits;
-  size_t q, nlse, part, bytes;
+  size_t q, nlse, angles, part, bytes;
 };
 
 // A workgroup takes four 64-key tiles at a time; its rows are divided where the tiles alone do not fill the chip.
@@ -27,9 +27,9 @@ PromptSizes prompt_sizes(const lazy_attn_params_t* p, int32_t batch, int32_t tot
   PromptSizes z = {};
   const int64_t rows = (int64_t)total_q * p->num_q_heads, tiles = std::max<int64_t>(1, ceil_div(max_kv_len, kTileKeys));
   z.splits = (int)std::min<int64_t>(ceil_div(tiles, 4), 1 << 20);
-  const int64_t steps = ceil_div((int64_t)max_q_len * (p->num_q_heads / p->num_kv_heads), 32);
+  const int64_t steps = ceil_div((int64_t)max_q_len * (p->num_q_heads / p->num_kv_heads), 64);
   const int64_t groups = (int64_t)z.splits * p->num_kv_heads * std::max(batch, 1);
-  z.row_splits = (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(2 * kNumCUs, groups), steps / 4, 16}));
+  z.row_splits = (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(2 * kNumCUs, groups), steps / 2, 16}));
   const auto put = [&z](size_t bytes) {
     const size_t here = z.bytes;
     z.bytes += (bytes + 255) & ~(size_t)255;
@@ -37,6 +37,7 @@ PromptSizes prompt_sizes(const lazy_attn_params_t* p, int32_t batch, int32_t tot
   };
   z.q = put((size_t)rows * p->head_dim * sizeof(uint16_t));
   z.nlse = put((size_t)rows * sizeof(float));
+  z.angles = put((size_t)kTileKeys * p->head_dim * sizeof(float));
   z.part = put((size_t)z.row_splits * p->num_kv_heads * (size_t)num_keys * sizeof(float));
   return z;
 }
@@ -49,7 +50,8 @@ void fill(lazy::WeightArgs& a, const lazy_attn_params_t* p) {
   a.group_magic = a.group == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
   a.causal = p->causal;
   a.rotate_q = !p->q_prerotated && p->rope_style != LAZY_ALIBI;
-  a.rope_log2_base = lazy::rope_log2_base(p);
+  a.rotate_k = p->rope_style != LAZY_ALIBI;
+  lazy::rope_revolutions(p, a.rev);
   a.scale_log2 = lazy::scale_log2(p);
 }
 
@@ -97,6 +99,7 @@ int lazy_attn_prefill_key_weights(const lazy_attn_params_t* p, const void* q, co
   a.weights = weights;
   a.ws_q = reinterpret_cast<uint16_t*>(ws + z.q);
   a.ws_nlse = reinterpret_cast<float*>(ws + z.nlse);
+  a.ws_angles = reinterpret_cast<float*>(ws + z.angles);
   a.ws_part = reinterpret_cast<float*>(ws + z.part);
   a.rows = (int64_t)total_q * g;
   a.total_q = total_q;
@@ -194,7 +197,7 @@ int lazy_cache_compact(const lazy_attn_params_t* p, const void* k_pool, const vo
   a.weights_out = weights_out;
   a.inv_freq = p->inv_freq;
   a.hkv = p->num_kv_heads;
-  a.rope_log2_base = lazy::rope_log2_base(p);
+  lazy::rope_revolutions(p, a.rev);
   const bool local = p->key_positions == LAZY_KEYS_LOCAL;
   return status(lazy::launch_compact(a, p->head_dim, batch, max_kept, rotate ? 1 : local ? 2 : 0, local,
                                      p->rope_style == LAZY_ROPE_INTERLEAVED, static_cast<hipStream_t>(stream)));

@@ -108,8 +108,9 @@ struct GradArgs {
   uint32_t group_magic;        // ceil(2^32 / group), 0 for group 1
   int32_t causal;
   int32_t rotate_q;            // 0: queries arrive rotated, or nothing is (ALiBi)
-  double rope_log2_base;
+  int32_t rotate_k;            // 0: ALiBi
   float scale_log2;
+  double rev[64];              // rotations per position of each pair, in revolutions (unused with inv_freq)
 };
 
 // Arguments of the key-weight kernels (prompt rows packed by KV head as for the backward pass).
@@ -126,6 +127,7 @@ struct WeightArgs {
   float* weights;
   uint16_t* ws_q;             // [hkv][rows][D] rotated queries times scale * log2 e
   float* ws_nlse;             // [hkv][rows] -lse log2 e
+  float* ws_angles;           // [64][D/2] (cos, sin) of positions 0 .. 63
   float* ws_part;             // [row_splits * hkv][num_keys] partial sums
   const float* inv_freq;
   int64_t rows;
@@ -137,14 +139,15 @@ struct WeightArgs {
   uint32_t group_magic;
   int32_t causal;
   int32_t rotate_q;
+  int32_t rotate_k;
   int32_t splits;             // key splits of a request
   int32_t row_splits;
   int32_t sort_records;       // single tokens: 1 walks a request's records in storage order
   int32_t head_split;         // single tokens: 1 where the waves of a workgroup share the heads
   int32_t num_keys;
   float decay;
-  double rope_log2_base;
   float scale_log2;
+  double rev[64];             // as for the backward pass
 };
 
 struct CompactArgs {
@@ -162,7 +165,7 @@ struct CompactArgs {
   float* weights_out;
   const float* inv_freq;
   int32_t hkv;
-  double rope_log2_base;
+  double rev[64];
 };
 
 // Packed rows (token, head in group) handled by one prefill workgroup, and keys per decode tile.

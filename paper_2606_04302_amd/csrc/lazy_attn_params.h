@@ -38,4 +38,11 @@ inline double rope_log2_base(const lazy_attn_params_t* p) {
   return p->inv_freq || p->rope_style == LAZY_ALIBI ? 0.0 : log2((double)p->rope_base);
 }
 
+// Rotations per position of every pair, in revolutions (not used with a table of the caller's, or with ALiBi).
+inline void rope_revolutions(const lazy_attn_params_t* p, double (&rev)[64]) {
+  const double l = rope_log2_base(p);
+  for (int t = 0; t < 64; ++t)
+    rev[t] = t < p->head_dim / 2 ? exp2(-2.0 * t / p->head_dim * l) * 0.15915494309189533577 : 0.0;
+}
+
 }  // namespace lazy

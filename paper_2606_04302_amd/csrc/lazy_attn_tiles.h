@@ -50,6 +50,20 @@ struct TileOperands {
   }
 };
 
+// Rows of 16-byte chunks copied to a tile in LDS without passing through registers: lane l of a wave writes the 16 bytes
+// at 16 l from a uniform base, so the tile's permutation of chunks is made by the lanes' source addresses.
+__device__ __forceinline__ void copy_async(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
+                                   (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
+}
+// Every copy and LDS access so far has ended; nothing moves across.
+__device__ __forceinline__ void wait_copies() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // Packed row -> token: row / G by multiplication (total_q * G * G < 2^32, checked by the planner).
 __device__ __forceinline__ int token_of(int row, uint32_t magic) { return magic ? (int)__umulhi(row, magic) : row; }
 
@@ -82,24 +96,63 @@ __device__ __forceinline__ void store_pairs(uint16_t* v, int t0, const float (&l
   }
 }
 
-// Rotates the raw key operands of a 32-key block to their positions.  Lane: key lane % 32 of the block, elements
-// 16 s + 8 h2 .. + 7 of operand s; its pairs lie in operand s + D / 32.
-template <int D, int KM, bool IL>
-__device__ __forceinline__ void load_keys(const uint16_t* krow, int h2, int p, const double* freq, bf16x8 (&kf)[D / 16]) {
+// Rotations per position of pair t, in revolutions: from the caller's table, or as the host worked them out.
+template <class Args>
+__device__ __forceinline__ double revolutions(const Args& a, int t) {
+  return a.inv_freq ? (double)a.inv_freq[t] * kInvTwoPi : a.rev[t];
+}
+
+// Angles of positions 0 .. 63, which a tile's keys add to the position of its key 0: (cos, sin) of [64][D/2] pairs by
+// kAngleBlocks workgroups of 256.
+template <int D>
+constexpr int kAngleBlocks = 64 * (D / 2) / 256;
+template <int D, class Args>
+__device__ __forceinline__ void angle_rows(const Args& a, int block) {
+  const int e = block * 256 + threadIdx.x;
+  reinterpret_cast<float2*>(a.ws_angles)[e] = rope_cs(e / (D / 2), revolutions(a, e % (D / 2)));
+}
+
+// The operands of a 32-key block.  Lane: key `row` of its 64-key tile, elements 16 s + 8 h2 .. + 7 of operand s; its pairs
+// lie in operand s + D / 32.  First as they are stored, all loads in flight together (interleaved pairs: 16 elements).
+template <int D, bool IL>
+__device__ __forceinline__ void load_keys(const uint16_t* krow, int h2, u32x4 (&kf)[D / 16]) {
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) {
     const int t0 = 16 * s + 8 * h2;
-    u32x4 lo, hi;
-    load_pairs<D, IL>(krow, t0, lo, hi);
+    kf[s] = *reinterpret_cast<const u32x4*>(krow + (IL ? 2 * t0 : t0));
+    kf[s + D / 32] = *reinterpret_cast<const u32x4*>(krow + (IL ? 2 * t0 + 8 : D / 2 + t0));
+  }
+}
+// Then rotated.  base: (cos, sin) of the tile's position (local-position keys: of their record's), in LDS; rows(t): those
+// of the lane's key within the tile, for pairs t and t + 1.
+// AHEAD: operands whose rows are in flight together.
+template <int D, int KM, bool IL, int AHEAD, class Rows>
+__device__ __forceinline__ void rotate_keys(u32x4 (&kf)[D / 16], int h2, const float2* base, Rows rows) {
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    const int t0 = 16 * s + 8 * h2;
+    u32x4 lo = kf[s], hi = kf[s + D / 32];
+    if (IL) deinterleave8(kf[s], kf[s + D / 32], lo, hi);
     if (KM == kKeysNope || KM == kKeysLocal) {
       float yl[8], yh[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) rotate_by(element(lo, e), element(hi, e), rope_cs(p, freq[t0 + e]), yl[e], yh[e]);
+      for (int e = 0; e < 8; e += 2) {
+        if (KM == kKeysLocal) {
+          rotate_by(element(lo, e), element(hi, e), base[t0 + e], yl[e], yh[e]);
+          rotate_by(element(lo, e + 1), element(hi, e + 1), base[t0 + e + 1], yl[e + 1], yh[e + 1]);
+        } else {
+          const f32x4 r = rows(t0 + e);
+          rotate_pair(element(lo, e), element(hi, e), base[t0 + e], make_float2(r[0], r[1]), yl[e], yh[e]);
+          rotate_pair(element(lo, e + 1), element(hi, e + 1), base[t0 + e + 1], make_float2(r[2], r[3]), yl[e + 1],
+                      yh[e + 1]);
+        }
+      }
       lo = pack8(yl);
       hi = pack8(yh);
     }
-    kf[s] = as_bf16x8(lo);
-    kf[s + D / 32] = as_bf16x8(hi);
+    kf[s] = lo;
+    kf[s + D / 32] = hi;
+    if (s % AHEAD == AHEAD - 1) __builtin_amdgcn_sched_barrier(0);
   }
 }
 
