@@ -94,7 +94,7 @@ struct GradWorkLayout {
     };
     q = put(rows * d * sizeof(uint16_t));                                        // rotated, scaled queries
     dout = put(rows * d * sizeof(uint16_t));                                     // packed like the queries
-    info = put((rows + kGradRows) * 2 * sizeof(float));                          // (-lse log2 e, -delta) of each row
+    info = put(rows * 2 * sizeof(float));                                        // -lse log2 e of each row, then -delta
     angles = put((size_t)kGradTileKeys * d * sizeof(float));                     // rotations of positions 0 .. 63
     dq = put((size_t)i.row_slots * rows * d * sizeof(float));                    // partial query gradients
     // partial key and value gradients

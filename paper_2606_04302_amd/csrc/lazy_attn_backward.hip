@@ -73,7 +73,8 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
       const float lse = a.lse[src];
       if (a.dlse) sum -= a.dlse[src];
       // A row that sees no key: exp2(score - inf) = 0.
-      a.ws_info[dst] = make_float2(lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f, -sum);
+      a.ws_info[dst] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
+      a.ws_info[a.hkv * a.rows + dst] = -sum;
     }
   }
 }
@@ -94,10 +95,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   // Two buffers as variables of their own: the compiler then knows that copies to one do not touch reads of the other.
   __shared__ uint16_t tq0[kGradRows * D] __attribute__((aligned(16)));
   __shared__ uint16_t td0[kGradRows * D] __attribute__((aligned(16)));
-  __shared__ float2 in0[kGradRows] __attribute__((aligned(16)));
+  __shared__ float in0[2 * kGradRows] __attribute__((aligned(16)));  // -lse log2 e, then -delta, of the rows
   __shared__ uint16_t tq1[kGradRows * D] __attribute__((aligned(16)));
   __shared__ uint16_t td1[kGradRows * D] __attribute__((aligned(16)));
-  __shared__ float2 in1[kGradRows] __attribute__((aligned(16)));
+  __shared__ float in1[2 * kGradRows] __attribute__((aligned(16)));
   __shared__ uint16_t tv[4][32 * D] __attribute__((aligned(16)));  // a wave's V operands, then its results
   __shared__ int rpos_all[4][kGradRows] __attribute__((aligned(16)));
   __shared__ float rslope_all[4][kGradRows] __attribute__((aligned(16)));
@@ -127,11 +128,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
   const uint16_t* qbase = a.ws_q + (int64_t)g * a.rows * D;
   const uint16_t* dbase = a.ws_do + (int64_t)g * a.rows * D;
-  const float2* ibase = a.ws_info + (int64_t)g * a.rows;
+  const float* ibase = a.ws_info + (int64_t)g * a.rows;
   int frame = 0;  // position by which dk is rotated (NoPE: that of the half's key 0)
   bool first = true;
 
-  const auto fetch = [&](int si, int row0, uint16_t* tq, uint16_t* td, float2* in) {
+  const auto fetch = [&](int si, int row0, uint16_t* tq, uint16_t* td, float* in) {
     const int most = a.segs[si].row_end - 1 - row0;  // rows past the use's end repeat its last one
     const uint16_t* q = qbase + (int64_t)row0 * D;
     const uint16_t* d = dbase + (int64_t)row0 * D;
@@ -143,10 +144,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       copy_async(q + off, tq + 2048 * i + 512 * wave);
       copy_async(d + off, td + 2048 * i + 512 * wave);
     }
-    if (e0 < kGradRows / 2) copy_async(ibase + row0 + 2 * e0, in);  // two rows a lane
+    if (wave == 0)
+      copy_async4(ibase + (lane & 32 ? a.hkv * a.rows : 0) + row0 + min(lane & 31, most), in);
   };
 
-  const auto compute = [&](int si, int row0, const uint16_t* tq, const uint16_t* td, const float2* in) {
+  const auto compute = [&](int si, int row0, const uint16_t* tq, const uint16_t* td, const float* in) {
     const GradSeg& seg = a.segs[si];
     const int rows = min(kGradRows, seg.row_end - row0), pos = seg.half[hf].pos;
     if (row0 == seg.row_begin) {  // a new use: its keys, and dk turned on to its frame
@@ -190,24 +192,42 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
 
     const TileOperands<D> op(again(lane));
+    // Operands are read one step ahead of their products, and the scheduler is fenced at every step: the reads in flight
+    // hide their latency without taking more registers than there are.
+    const auto value = [&](int k) {
+      return as_bf16x8(*reinterpret_cast<const u32x4*>(tv[wave] + 512 * k + 8 * lane));
+    };
     f32x16 s, dp;
+    bf16x8 fq[2], fd[2], fv[2];
+    fq[0] = op.row(tq, 0, 0);
+    fd[0] = op.row(td, 0, 0);
+    fv[0] = value(0);
 #pragma unroll
-    for (int q2 = 0; q2 < 8; ++q2) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(in + 8 * (q2 >> 1) + 4 * h2 + 2 * (q2 & 1));
-      s[2 * q2] = x[0];
-      dp[2 * q2] = x[1];
-      s[2 * q2 + 1] = x[2];
-      dp[2 * q2 + 1] = x[3];
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(in + 8 * q4 + 4 * h2);
+      const f32x4 y = *reinterpret_cast<const f32x4*>(in + kGradRows + 8 * q4 + 4 * h2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[4 * q4 + e] = x[e];
+        dp[4 * q4 + e] = y[e];
+      }
     }
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(tq, 0, k), as_bf16x8(kf[k]), s, 0, 0, 0);
-      const bf16x8 fv = as_bf16x8(*reinterpret_cast<const u32x4*>(tv[wave] + 512 * k + 8 * lane));
-      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(td, 0, k), fv, dp, 0, 0, 0);
-      if (k & 1) __builtin_amdgcn_sched_barrier(0);
+      if (k + 1 < D / 16) {
+        fq[(k + 1) & 1] = op.row(tq, 0, k + 1);
+        fd[(k + 1) & 1] = op.row(td, 0, k + 1);
+        fv[(k + 1) & 1] = value(k + 1);
+      }
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[k & 1], as_bf16x8(kf[k]), s, 0, 0, 0);
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[k & 1], fv[k & 1], dp, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
+    fd[0] = op.column(td, 0, 0);
+    fq[0] = op.column(tq, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
     if (ALIBI) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -240,9 +260,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       const bf16x8 pf = as_bf16x8(pack8(x)), sf = as_bf16x8(pack8(y));
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
-        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.column(td, 16 * k, db), pf, dv[db], 0, 0, 0);
-        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.column(tq, 16 * k, db), sf, dk[db], 0, 0, 0);
-        if (db & 1) __builtin_amdgcn_sched_barrier(0);
+        const int at = k * (D / 32) + db, ahead = at + 1;
+        if (ahead < 2 * (D / 32)) {
+          fd[ahead & 1] = op.column(td, 16 * (ahead / (D / 32)), ahead % (D / 32));
+          fq[ahead & 1] = op.column(tq, 16 * (ahead / (D / 32)), ahead % (D / 32));
+        }
+        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[at & 1], pf, dv[db], 0, 0, 0);
+        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[at & 1], sf, dk[db], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     __builtin_amdgcn_s_setprio(0);
@@ -351,8 +376,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // Loads a 64-key tile of K and V for a workgroup of NT threads, NT / 64 a key row, rotates the keys and writes both to
-// LDS (unpadded tiles, pairs in half-split order).
-template <int D, int KMI, int NT, bool REGS>
+// LDS (unpadded tiles, pairs in half-split order).  The angles of the 32 rows are read from LDS for every tile: kept in
+// registers by the eight-wave kernel they cost it 27 spilled ones (16 ragged requests of 17K keys: 1457 instead of 1027
+// us).
+template <int D, int KMI, int NT>
 struct TileLoader {
   using S = TileLayout<D>;
   static constexpr int KM = keys_of(KMI);
@@ -360,18 +387,10 @@ struct TileLoader {
   static constexpr int TPR = NT / kSub, PP = D / (2 * TPR), NV = PP / 8, VC = kSub * (D / 8) / NT;
   static_assert(PP % 8 == 0 && VC * TPR == D / 8);
   u32x4 ka[NV], kb[NV], vr[VC];  // raw pairs: first and second halves (interleaved: 16 elements as stored)
-  float2 cdr[REGS && KM == kKeysNope ? PP : 1];
   int row, part;
   __device__ void init(int t) {
     row = t / TPR;
     part = t % TPR;
-  }
-  __device__ void constants(const float* csd) {
-    if (KM == kKeysNope && REGS) {
-#pragma unroll
-      for (int e = 0; e < PP; ++e)
-        cdr[e] = *reinterpret_cast<const float2*>(csd + (row & (kAngleRows - 1)) * S::CSD_LD + cs_idx<D>(part * PP + e));
-    }
   }
   // Rows past the record's end repeat its last key; their products are masked.
   __device__ void fetch(const uint16_t* k, const uint16_t* v, int nvalid) {
@@ -402,8 +421,8 @@ struct TileLoader {
           if (LOCAL) {
             rotate_by(element(lo, e), element(hi, e), *reinterpret_cast<const float2*>(cb + ci), yl[e], yh[e]);
           } else {
-            const float2 c = REGS ? cdr[8 * i + e] : *reinterpret_cast<const float2*>(cd + ci);
-            rotate_pair(element(lo, e), element(hi, e), *reinterpret_cast<const float2*>(cb + ci), c, yl[e], yh[e]);
+            rotate_pair(element(lo, e), element(hi, e), *reinterpret_cast<const float2*>(cb + ci),
+                        *reinterpret_cast<const float2*>(cd + ci), yl[e], yh[e]);
           }
         }
         lo = pack8(yl);
@@ -445,13 +464,22 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
       dp[i] = nd;
     }
     __builtin_amdgcn_s_setprio(1);
+    // Operands one step ahead of their products.
+    bf16x8 fk[2] = {op.row(tk, 32 * kb, 0)}, fv[2] = {op.row(tv, 32 * kb, 0)};
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(tk, 32 * kb, k), qf[k], s, 0, 0, 0);
-      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.row(tv, 32 * kb, k), df[k], dp, 0, 0, 0);
-      if (k & 1) __builtin_amdgcn_sched_barrier(0);
+      if (k + 1 < D / 16) {
+        fk[(k + 1) & 1] = op.row(tk, 32 * kb, k + 1);
+        fv[(k + 1) & 1] = op.row(tv, 32 * kb, k + 1);
+      }
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[k & 1], qf[k], s, 0, 0, 0);
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[k & 1], df[k], dp, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
+    fk[0] = op.column(tk, 32 * kb, 0);
+    fk[1] = op.column(tk, 32 * kb, 1);
+    __builtin_amdgcn_sched_barrier(0);
     if (ALIBI) {
       const float base = slope * (float)(b0 + 32 * kb + 4 * h2 - qpos);
 #pragma unroll
@@ -474,9 +502,13 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
       for (int e = 0; e < 8; ++e) y[e] = dp[8 * k + e];
       const bf16x8 sf = as_bf16x8(pack8(y));
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-        dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.column(tk, 32 * kb + 16 * k, db), sf, dq[db], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int db = 0; db < D / 32; ++db) {
+        const int at = k * (D / 32) + db, ahead = at + 2;
+        dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[at & 1], sf, dq[db], 0, 0, 0);
+        if (ahead < 2 * (D / 32))
+          fk[at & 1] = op.column(tk, 32 * kb + 16 * (ahead / (D / 32)), ahead % (D / 32));
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     __builtin_amdgcn_s_setprio(0);
   }
@@ -504,8 +536,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     qf[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + 16 * s + 8 * h2));
     df[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(drow + 16 * s + 8 * h2));
   }
-  const float2 in = a.ws_info[(int64_t)g * a.rows + src];
-  const float nl = pr < nrows ? in.x : -INFINITY, nd = in.y;
+  const float* in = a.ws_info + (int64_t)g * a.rows + src;
+  const float nl = pr < nrows ? in[0] : -INFINITY, nd = in[a.hkv * a.rows];
   const float slope = ALIBI ? alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f) : 0.f;
   f32x16 dq[D / 32];
 #pragma unroll
@@ -520,9 +552,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       *reinterpret_cast<float2*>(sm.csd + e / (D / 2) * S::CSD_LD + cs_idx<D>(e % (D / 2))) = rope_cs(e / (D / 2), rev);
   }
   __syncthreads();
-  TileLoader<D, KMI, NT, NW == 8> ld;
+  TileLoader<D, KMI, NT> ld;
   ld.init(tid);
-  ld.constants(sm.csd);
   TileIter<kSub> it;
   it.init(a.chunks, a.chunk_start[r], a.chunk_start[r + 1], item.split, item.splits);
   bool have = it.seek(a.causal, qmax);

@@ -53,7 +53,7 @@ extern "C" int lazy_attn_prefill_backward(const lazy_attn_params_t* p, const voi
   a.ws_q = reinterpret_cast<uint16_t*>(work + ws.q);
   a.ws_do = reinterpret_cast<uint16_t*>(work + ws.dout);
   a.ws_angles = reinterpret_cast<float*>(work + ws.angles);
-  a.ws_info = reinterpret_cast<float2*>(work + ws.info);
+  a.ws_info = reinterpret_cast<float*>(work + ws.info);
   a.ws_dq = reinterpret_cast<float*>(work + ws.dq);
   a.ws_parts = reinterpret_cast<float*>(work + ws.parts);
   a.inv_freq = p->inv_freq;

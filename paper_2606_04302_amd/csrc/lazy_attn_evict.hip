@@ -129,9 +129,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
       const int row = (256 * i + e0) / C, chunk = ((256 * i + e0) % C) ^ swizzle<D>(row & 31);
       copy_async(qbase + (int64_t)row0 * D + min(row, most) * D + 8 * chunk, tq + 2048 * i + 512 * wave);
     }
-    if (e0 < 64)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(nbase + row0 + min(e0, most)),
-                                       (__attribute__((address_space(3))) uint32_t*)nl, 4, 0, 0);
+    if (wave == 0) copy_async4(nbase + row0 + min(e0, most), nl);
   };
   if (KM == kKeysNope) {
     const int e0 = again(tid);

@@ -96,7 +96,7 @@ struct GradArgs {
   uint16_t* dv_pool;
   uint16_t* ws_q;              // [hkv][rows][D] rotated queries times scale * log2 e, pairs in half-split order
   uint16_t* ws_do;             // [hkv][rows][D] dout
-  float2* ws_info;             // [hkv][rows] (-lse log2 e, -delta)
+  float* ws_info;              // [2][hkv][rows] -lse log2 e, then -delta
   float* ws_angles;            // [64][D/2] (cos, sin) of positions 0 .. 63
   float* ws_dq;                // [row_slots][hkv][rows][D]
   float* ws_parts;             // [num_parts][hkv][dk, dv][64][D]
