@@ -202,6 +202,8 @@ def _need(cond, msg):
 
 
 def _dev(t, dtype, name):
+    if t.is_cuda and t.dtype == dtype and t.is_contiguous():
+        return  # the messages below cost more to format than the checks (a call has up to a dozen tensors)
     _need(t.is_cuda, f"{name} must be a device tensor")
     _need(t.dtype == dtype, f"{name} must be {dtype}, got {t.dtype}")
     _need(t.is_contiguous(), f"{name} must be contiguous")
