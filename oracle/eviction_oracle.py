@@ -6,14 +6,16 @@ import math
 import numpy as np
 
 from . import lazy_oracle as O
-from .gradient_oracle import U
 
 
 def key_weights(q, q_start, q_pos0, pool_k, chunks, chunk_start, hq, hkv, d, base, causal, lse, pairing="half",
                 key_positions="nope", inv_freq=None, softmax_scale=0.0, q_prerotated=False):
-    """Per request: [keys] sums over query rows and heads of exp(s - lse), and first-order bounds of their error where
-    rotated queries and keys are rounded to bf16 (a score is off by at most 2 u scale sum |q'||k'|) and sums are fp32
-    (2^-16 of the sum covers a few hundred additions of 2^-24 each)."""
+    """Per request: [keys] sums over query rows and heads of exp(s - lse), and bounds of the error of an evaluation that
+    keeps rotated queries and keys as sums of two bf16 numbers each and multiplies them without the two second parts'
+    product.  With u = 2^-8 per rounding, every product q'k' is off by at most u^2 for each operand's rest and u^2 for
+    what is left out, 3 2^-16; sums of at most 384 products in fp32 add 384 2^-24 = 1.5 2^-16 and angles good to 2e-7
+    under 0.1 2^-16: together 4.6 2^-16 = 1.15 2^-14 of scale sum |q'||k'|.  The exponent's other part, lse (below 64
+    here), is rounded to fp32 twice: 2^-17.  Sums of probabilities: 2^-16 covers 256 additions of 2^-24 each."""
     G = hq // hkv
     scale = softmax_scale or 1.0 / math.sqrt(d)
     alibi = pairing == "alibi"
@@ -41,9 +43,9 @@ def key_weights(q, q_start, q_pos0, pool_k, chunks, chunk_start, hq, hkv, d, bas
             hidden = np.isneginf(L) | ((kpos[None, :] > qpos[:, None]) if causal else False)
             with np.errstate(invalid="ignore", over="ignore"):
                 P = np.where(hidden, 0.0, np.exp(s - L))
-            E = 2 * U * scale * np.abs(Q[h]) @ np.abs(K[h // G]).T
+            E = 1.25 * 2.0 ** -14 * scale * np.abs(Q[h]) @ np.abs(K[h // G]).T + 2.0 ** -17
             w += P.sum(0)
-            bound += (P * (1.25 * E + 2.0 ** -16)).sum(0)
+            bound += (P * (E + 2.0 ** -16)).sum(0)
         got.append((w, bound + 1e-30))
     return got
 

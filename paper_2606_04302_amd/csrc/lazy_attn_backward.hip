@@ -86,8 +86,8 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
 // read by rows for the first two products and transposed for the last two; the next 32 are copied to the other buffer
 // during the products.  -lse and -delta are the accumulators' initial values.  dK is kept in the rotated frame of the use
 // at hand and turned on when the next use has another position.
-template <int D, int KMI>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kv(GradArgs a) {
+template <int D, int KMI, int WPE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE, WPE))) void grad_kv(GradArgs a) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
   constexpr int C = D / 8;  // chunks of a row
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if (l < D / 2) turn[l] = rope_cs(here, rev);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
-      rotate_keys<D, KM, IL, 2>(kf, l >> 5, turn, [&](int t) {
+      rotate_keys<D, KM, IL>(kf, l >> 5, turn, [&](int t) {
         return *reinterpret_cast<const f32x4*>(angles + (k32 + (l & 31)) * (D / 2) + t);
       });
       frame = here;
@@ -700,7 +700,7 @@ template <int D, int KMI>
 hipError_t launch(const GradArgs& a, const lazy_backward_info_t& i, hipStream_t stream) {
   constexpr bool IL = interleaved_of(KMI);
   prepare_rows<D, IL><<<i.num_blocks + kAngleBlocks<D>, 256, 0, stream>>>(a, i.num_blocks);
-  if (i.num_tiles) grad_kv<D, KMI><<<i.num_tiles * a.hkv, 256, 0, stream>>>(a);
+  if (i.num_tiles) grad_kv<D, KMI, D == 64 ? 3 : 2><<<i.num_tiles * a.hkv, 256, 0, stream>>>(a);
   if (i.num_row_items) {
     if constexpr (D == 128) {
       if (i.row_blocks == 2)

@@ -1,5 +1,10 @@
 // Eviction by accumulated attention weight for gfx950: key weights of prompts and of single tokens, the selection of the
 // heaviest keys, and the gathering of the kept ones.
+//
+// Key weights are sums that later calls go on with and that ranks are taken of, so their scores are formed more exactly
+// than an attention output needs: rotated queries and keys are each kept as two bf16 parts (2^-16 instead of 2^-8), and a
+// score is the sum of three products, first x first and the two mixed ones.  With one part each, sums over 8 to 32 heads
+// were 1e-4 to 5e-4 off (2-norm), now about 1e-6.  ALiBi rotates nothing: one part is exact.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -42,7 +47,7 @@ struct KeyIter : TileIter<kSub> {
 
 constexpr int kPrepTokens = 2;
 
-// Queries rotated, scaled and packed by KV head, and -lse log2 e of each row; workgroups past the last block write the
+// Queries rotated, in two parts, packed by KV head, and -lse log2 e of each row; workgroups past the last block write the
 // table of angles.
 template <int D, bool IL>
 __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks) {
@@ -75,16 +80,23 @@ __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks)
     const int64_t dst = (int64_t)(h / a.group) * a.rows + (int64_t)(first + tok) * a.group + h % a.group;
     u32x4 lo, hi;
     load_pairs<D, IL>(a.q + src * D, t0, lo, hi);
-    float yl[8], yh[8];
+    if (a.rotate_k) {
+      float yl[8], yh[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      yl[e] = element(lo, e);
-      yh[e] = element(hi, e);
-      if (a.rotate_q) rotate_by(element(lo, e), element(hi, e), cs[tok][t0 + e], yl[e], yh[e]);
-      yl[e] *= a.scale_log2;
-      yh[e] *= a.scale_log2;
+      for (int e = 0; e < 8; ++e) {
+        yl[e] = element(lo, e);
+        yh[e] = element(hi, e);
+        if (a.rotate_q) rotate_by(element(lo, e), element(hi, e), cs[tok][t0 + e], yl[e], yh[e]);
+      }
+      u32x4 rest;
+      uint16_t* const second = a.ws_q + (a.hkv * a.rows + dst) * D;
+      split8(yl, lo, rest);
+      *reinterpret_cast<u32x4*>(second + t0) = rest;
+      split8(yh, hi, rest);
+      *reinterpret_cast<u32x4*>(second + D / 2 + t0) = rest;
     }
-    store_pairs<D, false>(a.ws_q + dst * D, t0, yl, yh);
+    *reinterpret_cast<u32x4*>(a.ws_q + dst * D + t0) = lo;
+    *reinterpret_cast<u32x4*>(a.ws_q + dst * D + D / 2 + t0) = hi;
     if (t0 == 0) {
       const float lse = a.lse[src];
       a.ws_nlse[dst] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
@@ -92,19 +104,19 @@ __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks)
   }
 }
 
-// Weights of a prompt: workgroup (key split and row split, KV head, request), four waves with a 64-key tile each, whose
-// rotated keys stay in registers while the rows of the request pass through LDS, kStepRows at a time, copied to the other
+// Weights of a prompt: workgroup (key split and row split, KV head, request), two 64-key tiles at a time, 32 keys a wave,
+// whose rotated parts stay in registers while the rows of the request pass through LDS, 32 at a time, copied to the other
 // of two buffers during the products.  S = Q K^T has a key in every lane and 32 rows in registers and lane halves, so a
 // key's sum never leaves its lane.
-constexpr int kStepRows = 64;
+constexpr int kStepRows = 32;
 template <int D, int KMI>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) void weigh_prompt(WeightArgs a) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
-  constexpr int C = D / 8, COPIES = kStepRows * C / 256;
-  __shared__ uint16_t tq0[kStepRows * D] __attribute__((aligned(16)));
+  constexpr int C = D / 8, COPIES = kStepRows * C / 256, PARTS = ROT ? 2 : 1;
+  __shared__ uint16_t tq0[PARTS * kStepRows * D] __attribute__((aligned(16)));
   __shared__ float nl0[kStepRows] __attribute__((aligned(16)));
-  __shared__ uint16_t tq1[kStepRows * D] __attribute__((aligned(16)));
+  __shared__ uint16_t tq1[PARTS * kStepRows * D] __attribute__((aligned(16)));
   __shared__ float nl1[kStepRows] __attribute__((aligned(16)));
   __shared__ int rpos_all[4][kStepRows] __attribute__((aligned(16)));
   __shared__ float rslope_all[4][kStepRows] __attribute__((aligned(16)));
@@ -120,16 +132,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
   const int room = a.key_start[r + 1] - a.key_start[r];
   const double rev = ROT ? revolutions(a, lane % (D / 2)) : 0.0;
   const uint16_t* qbase = a.ws_q + (int64_t)g * a.rows * D;
+  const int64_t second = a.hkv * a.rows * D;
   const float* nbase = a.ws_nlse + (int64_t)g * a.rows;
   const auto fetch = [&](int row0, uint16_t* tq, float* nl) {
     const int most = row_end - 1 - row0;  // rows past the end repeat the last one; they are masked
     const int e0 = again(tid);
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
-      const int row = (256 * i + e0) / C, chunk = ((256 * i + e0) % C) ^ swizzle<D>(row & 31);
-      copy_async(qbase + (int64_t)row0 * D + min(row, most) * D + 8 * chunk, tq + 2048 * i + 512 * wave);
+      const int row = (256 * i + e0) / C, chunk = ((256 * i + e0) % C) ^ swizzle<D>(row);
+      const uint16_t* src = qbase + (int64_t)row0 * D + min(row, most) * D + 8 * chunk;
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part)
+        copy_async(src + part * second, tq + part * kStepRows * D + 2048 * i + 512 * wave);
     }
-    if (wave == 0) copy_async4(nbase + row0 + min(e0, most), nl);
+    if (tid < kStepRows) copy_async4(nbase + row0 + min(e0, most), nl);
   };
   if (KM == kKeysNope) {
     const int e0 = again(tid);
@@ -142,39 +158,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
   if (row_begin < row_end) fetch(row_begin, tq0, nl0);
   KeyIter it;
   it.start(a.chunks, a.chunk_start[r], a.chunk_start[r + 1], split, a.splits);
-  const int rounds = (it.left + 3) / 4;
-  it.skip(wave);
+  const int rounds = (it.left + 1) / 2;
+  it.skip(wave >> 1);
   __syncthreads();
   float* part = a.ws_part + (int64_t)(rs * a.hkv + g) * a.num_keys + a.key_start[r];
   int* const rpos = rpos_all[wave];
   float* const rslope = rslope_all[wave];
+  const int key = 32 * (wave & 1) + (lane & 31);
   for (int round = 0; round < rounds; ++round) {
-    const bool have = it.left > 0;
-    const int nvalid = have ? min(kSub, it.cur.len - it.j0) : 0, b0 = have ? it.cur.pos + it.j0 : 0;
-    u32x4 kf[2][D / 16];
+    const int nvalid = it.left > 0 ? min(kSub, it.cur.len - it.j0) : 0, b0 = nvalid ? it.cur.pos + it.j0 : 0;
+    const bool have = 32 * (wave & 1) < nvalid;
+    u32x4 kh[D / 16], kl[D / 16];
     float acc[2] = {0.f, 0.f};
-    if (have) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-        load_keys<D, IL>(k_ptr(a.k_pool, it.cur, g, it.j0 + min(32 * b + (lane & 31), nvalid - 1), D), h2, kf[b]);
-    }
+    if (have) load_keys<D, IL>(k_ptr(a.k_pool, it.cur, g, it.j0 + min(key, nvalid - 1), D), h2, kh);
     if (KM == kKeysNope && round == 0) {  // the first wait: angle rows (and the first query rows) in LDS for all
       wait_copies();
       __syncthreads();
     }
-    if (have) {
+    if (have && ROT) {
       // Local-position keys turn by their record's position, the others by that of their 32-key block and a row's.
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if (ROT && (b == 0 || !LOCAL)) {
-          if (lane < D / 2) turn_all[wave][lane] = rope_cs(LOCAL ? it.cur.pos : b0 + 32 * b, rev);
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        }
-        rotate_keys<D, KM, IL, 1>(kf[b], h2, turn_all[wave], [&](int t) {
-          return *reinterpret_cast<const f32x4*>(trows + (lane & 31) * D + 4 * ((t / 2) ^ (lane & 15)));
-        });
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      }
+      if (lane < D / 2) turn_all[wave][lane] = rope_cs(LOCAL ? it.cur.pos : b0 + 32 * (wave & 1), rev);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      rotate_keys_split<D, KM, IL>(kh, kl, h2, turn_all[wave], [&](int t) {
+        return *reinterpret_cast<const f32x4*>(trows + (lane & 31) * D + 4 * ((t / 2) ^ (lane & 15)));
+      });
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     const auto compute = [&](int row0, const uint16_t* tq, const float* nl) {
       const int rows = min(kStepRows, row_end - row0);
@@ -182,90 +190,80 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
       if (!have || (a.causal && b0 > qmax)) return;
       const bool masked = (a.causal && b0 + kSub - 1 > qmin) || rows < kStepRows;
       if (ALIBI || masked) {
-        const int src = row0 + lane, tok = token_of(src, a.group_magic);
-        rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + shift : INT32_MAX;
-        if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
+        if (lane < kStepRows) {
+          const int src = row0 + lane, tok = token_of(src, a.group_magic);
+          rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + shift : INT32_MAX;
+          if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
+        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
       const TileOperands<D> op(again(lane));
+      f32x16 s = f32x16{};
+      bf16x8 fh[2] = {op.row(tq, 0, 0)}, fl[2];
+      if (ROT) fl[0] = op.row(tq + kStepRows * D, 0, 0);
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int half = 0; half < kStepRows / 32; ++half) {
-        f32x16 s[2];
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(nl + 32 * half + 8 * q4 + 4 * h2);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[0][4 * q4 + e] = s[1][4 * q4 + e] = x[e];
+      for (int k = 0; k < D / 16; ++k) {
+        if (k + 1 < D / 16) {
+          fh[(k + 1) & 1] = op.row(tq, 0, k + 1);
+          if (ROT) fl[(k + 1) & 1] = op.row(tq + kStepRows * D, 0, k + 1);
         }
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const bf16x8 fq = op.row(tq, 32 * half, k);
-#pragma unroll
-          for (int b = 0; b < 2; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq, as_bf16x8(kf[b][k]), s[b], 0, 0, 0);
+        if (ROT) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fl[k & 1], as_bf16x8(kh[k]), s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fh[k & 1], as_bf16x8(kl[k]), s, 0, 0, 0);
         }
-        __builtin_amdgcn_s_setprio(0);
-        if (ALIBI) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fh[k & 1], as_bf16x8(kh[k]), s, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int row = 32 * half + 8 * (i >> 2) + 4 * h2 + (i & 3);
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(nl + 8 * q4 + 4 * h2);
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-              s[b][i] = fmaf(rslope[row], (float)(b0 + 32 * b + (lane & 31) - rpos[row]), s[b][i]);
-          }
-        }
-        if (masked) {
+        for (int e = 0; e < 4; ++e) s[4 * q4 + e] = fmaf(s[4 * q4 + e], a.scale_log2, x[e]);
+      }
+      if (ALIBI) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int last = rpos[32 * half + 8 * (i >> 2) + 4 * h2 + (i & 3)];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              const int p = a.causal ? b0 + 32 * b + (lane & 31) : 0;
-              s[b][i] = p <= last ? s[b][i] : -INFINITY;
-            }
-          }
-        }
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          float sum[2] = {0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sum[i & 1] += fast_exp2(s[b][i]);
-          acc[b] += sum[0] + sum[1];
+        for (int i = 0; i < 16; ++i) {
+          const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
+          s[i] = fmaf(rslope[row], (float)(b0 + key - rpos[row]), s[i]);
         }
       }
+      if (masked) {
+        const int p = a.causal ? b0 + key : 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = p <= rpos[8 * (i >> 2) + 4 * h2 + (i & 3)] ? s[i] : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[i & 1] += fast_exp2(s[i]);
     };
     // The first rows lie in buffer 0 at the start of every round.
     for (int row0 = row_begin; row0 < row_end; row0 += 2 * kStepRows) {
-      const int second = row0 + kStepRows, third = row0 + 2 * kStepRows;
+      const int other = row0 + kStepRows, third = row0 + 2 * kStepRows;
       wait_copies();
       __syncthreads();
-      if (second < row_end) fetch(second, tq1, nl1);
+      if (other < row_end) fetch(other, tq1, nl1);
       compute(row0, tq0, nl0);
-      if (second < row_end) {
+      if (other < row_end) {
         wait_copies();
         __syncthreads();
-      }
-      // what comes next into buffer 0: the third step, or the next round's first
-      if (second < row_end) {
+        // what comes next into buffer 0: the third step, or the next round's first
         if (third < row_end)
           fetch(third, tq0, nl0);
         else if (round + 1 < rounds)
           fetch(row_begin, tq0, nl0);
-        compute(second, tq1, nl1);
+        compute(other, tq1, nl1);
       } else if (round + 1 < rounds && row0 != row_begin) {
         __syncthreads();
         fetch(row_begin, tq0, nl0);
       }
     }
     if (have) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int key = 32 * b + (lane & 31), at = it.base + it.j0 + key;
-        const float sum = xor32_sum(acc[b]);
-        if (h2 == 0 && key < nvalid && at < room) part[at] = sum;
-      }
+      const int at = it.base + it.j0 + key;
+      const float sum = xor32_sum(acc[0] + acc[1]);
+      if (h2 == 0 && key < nvalid && at < room) part[at] = sum;
     }
-    it.skip(4);
+    it.skip(2);
   }
   wait_copies();
 }
@@ -417,12 +415,13 @@ struct TokenIter {
 };
 
 template <int D, int KMI, int HS, bool SORT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) void weigh_token(WeightArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) void weigh_token(WeightArgs a) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
   constexpr int QLD = D + kPad, H = D / 64, TPR = D / 16;
   typedef TokenIter<SORT> Iter;
-  __shared__ uint16_t q[kTokenRows * QLD] __attribute__((aligned(16)));
+  constexpr int PARTS = ROT ? 2 : 1;
+  __shared__ uint16_t q[PARTS * kTokenRows * QLD] __attribute__((aligned(16)));
   __shared__ float nlse[kTokenGroups * 16] __attribute__((aligned(16)));
   __shared__ float rslope[kTokenGroups * 16] __attribute__((aligned(16)));
   __shared__ double freq[D / 2];
@@ -465,16 +464,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
       const int in = min((grp % per_head) * 16 + row % per_group, a.group - 1);
       u32x4 lo, hi;
       load_pairs<D, IL>(a.q + ((int64_t)r * a.hq + (grp / per_head) * a.group + in) * D, t0, lo, hi);
-      float yl[8], yh[8];
+      uint16_t* const to = q + row * QLD + t0;
+      if (ROT) {
+        float yl[8], yh[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        yl[k] = element(lo, k);
-        yh[k] = element(hi, k);
-        if (ROT) rotate_by(element(lo, k), element(hi, k), qcs[t0 + k], yl[k], yh[k]);
-        yl[k] *= a.scale_log2;
-        yh[k] *= a.scale_log2;
+        for (int k = 0; k < 8; ++k)
+          rotate_by(element(lo, k), element(hi, k), qcs[t0 + k], yl[k], yh[k]);
+        u32x4 rest;
+        split8(yl, lo, rest);
+        *reinterpret_cast<u32x4*>(to + kTokenRows * QLD) = rest;
+        split8(yh, hi, rest);
+        *reinterpret_cast<u32x4*>(to + kTokenRows * QLD + D / 2) = rest;
       }
-      store_pairs<D, false>(q + row * QLD, t0, yl, yh);
+      *reinterpret_cast<u32x4*>(to) = lo;
+      *reinterpret_cast<u32x4*>(to + D / 2) = hi;
     }
     for (int e = tid; e < ng * 16; e += 256) {  // rows past a group's end: exp2(score - inf) = 0
       const int grp = g0 + e / 16, in = (grp % per_head) * 16 + e % 16, h = (grp / per_head) * a.group + in;
@@ -515,7 +518,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
       }
       float sum = 0.f;
       for (int k = first; k < ng; k += step) {
-        bf16x8 kf[2 * H];
+        u32x4 kh[2 * H], kl[2 * H];
 #pragma unroll
         for (int s = 0; s < H; ++s) {
           u32x4 lo = raw[s][0], hi = raw[s][1];
@@ -524,21 +527,33 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
             float yl[8], yh[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) rotate_by(element(lo, e), element(hi, e), cs[s][e], yl[e], yh[e]);
-            lo = pack8(yl);
-            hi = pack8(yh);
+            split8(yl, lo, kl[s]);
+            split8(yh, hi, kl[s + H]);
           }
-          kf[s] = as_bf16x8(lo);
-          kf[s + H] = as_bf16x8(hi);
+          kh[s] = lo;
+          kh[s + H] = hi;
         }
         if (k + step < ng)
           fetch(it, k + step, raw);
         else if (ahead.left > 0)
           fetch(ahead, first, raw);
-        f32x4 s4 = *reinterpret_cast<const f32x4*>(nlse + 16 * k + 4 * kq);
+        f32x4 s4 = f32x4{};
 #pragma unroll
-        for (int s = 0; s < 2 * H; ++s)
-          s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + k * per_group * QLD + 32 * s)), kf[s], s4, 0, 0, 0);
+        for (int s = 0; s < 2 * H; ++s) {
+          const uint16_t* at = qrow + k * per_group * QLD + 32 * s;
+          const bf16x8 fh = as_bf16x8(*reinterpret_cast<const u32x4*>(at));
+          if (ROT) {
+            const bf16x8 fl = as_bf16x8(*reinterpret_cast<const u32x4*>(at + kTokenRows * QLD));
+            s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fl, as_bf16x8(kh[s]), s4, 0, 0, 0);
+            s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, as_bf16x8(kl[s]), s4, 0, 0, 0);
+          }
+          s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, as_bf16x8(kh[s]), s4, 0, 0, 0);
+        }
+        {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(nlse + 16 * k + 4 * kq);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s4[e] = fmaf(s4[e], a.scale_log2, x[e]);
+        }
         if (ALIBI) {
           const f32x4 sl = *reinterpret_cast<const f32x4*>(rslope + 16 * k + 4 * kq);
 #pragma unroll

@@ -21,21 +21,21 @@ struct PromptSizes {
   size_t q, nlse, angles, part, bytes;
 };
 
-// A workgroup takes four 64-key tiles at a time; its rows are divided where the tiles alone do not fill the chip.
+// A workgroup takes two 64-key tiles at a time; its rows are divided where the tiles alone do not fill the chip.
 PromptSizes prompt_sizes(const lazy_attn_params_t* p, int32_t batch, int32_t total_q, int32_t max_q_len,
                          int32_t max_kv_len, int32_t num_keys) {
   PromptSizes z = {};
   const int64_t rows = (int64_t)total_q * p->num_q_heads, tiles = std::max<int64_t>(1, ceil_div(max_kv_len, kTileKeys));
-  z.splits = (int)std::min<int64_t>(ceil_div(tiles, 4), 1 << 20);
-  const int64_t steps = ceil_div((int64_t)max_q_len * (p->num_q_heads / p->num_kv_heads), 64);
+  z.splits = (int)std::min<int64_t>(ceil_div(tiles, 4), 1 << 20);  // two rounds each
+  const int64_t steps = ceil_div((int64_t)max_q_len * (p->num_q_heads / p->num_kv_heads), 32);
   const int64_t groups = (int64_t)z.splits * p->num_kv_heads * std::max(batch, 1);
-  z.row_splits = (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(2 * kNumCUs, groups), steps / 2, 16}));
+  z.row_splits = (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(2 * kNumCUs, groups), steps / 4, 16}));
   const auto put = [&z](size_t bytes) {
     const size_t here = z.bytes;
     z.bytes += (bytes + 255) & ~(size_t)255;
     return here;
   };
-  z.q = put((size_t)rows * p->head_dim * sizeof(uint16_t));
+  z.q = put((size_t)rows * p->head_dim * sizeof(uint16_t) * (p->rope_style == LAZY_ALIBI ? 1 : 2));
   z.nlse = put((size_t)rows * sizeof(float));
   z.angles = put((size_t)kTileKeys * p->head_dim * sizeof(float));
   z.part = put((size_t)z.row_splits * p->num_kv_heads * (size_t)num_keys * sizeof(float));
@@ -138,9 +138,9 @@ int lazy_attn_decode_key_weights(const lazy_attn_params_t* p, const void* q, con
   a.weights = weights;
   a.total_q = batch;
   a.batch = batch;
-  // Four workgroups a CU, at least one tile each; where there are fewer tiles than that, four workgroups a tile.
+  // Three workgroups a CU, at least one tile each; where there are fewer tiles than that, four workgroups a tile.
   const int64_t tiles = ceil_div(max_kv_len, kTileKeys);
-  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(4 * kNumCUs, batch), tiles));
+  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(3 * kNumCUs, batch), tiles));
   a.head_split = p->num_kv_heads > 1 && tiles * batch <= kNumCUs;
   // Storage order: where a workgroup reads enough for the caches to matter (sorting takes it 1-2 us).
   a.sort_records = batch > 1 && !a.head_split &&

@@ -125,7 +125,7 @@ struct WeightArgs {
   const float* lse;           // [total_q][hq]
   const float* weights_in;    // or null
   float* weights;
-  uint16_t* ws_q;             // [hkv][rows][D] rotated queries times scale * log2 e
+  uint16_t* ws_q;             // [2][hkv][rows][D] rotated queries in two parts (ALiBi: the first only)
   float* ws_nlse;             // [hkv][rows] -lse log2 e
   float* ws_angles;           // [64][D/2] (cos, sin) of positions 0 .. 63
   float* ws_part;             // [row_splits * hkv][num_keys] partial sums

@@ -88,6 +88,16 @@ __device__ __forceinline__ float element(const u32x4& v, int e) { return (e & 1)
 __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
   return u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
 }
+// Eight fp32 values as the sum of two bf16 ones each: rounded, and what is left, rounded.  The sum is within 2^-16 of the
+// value (relative), against 2^-8 for the first alone.  (Cutting off the lower half instead of rounding costs as many
+// instructions and makes every rest twice as large and of its value's sign.)
+__device__ __forceinline__ void split8(const float (&v)[8], u32x4& hi, u32x4& lo) {
+  hi = pack8(v);
+  float rest[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rest[e] = v[e] - element(hi, e);
+  lo = pack8(rest);
+}
 template <int D, bool IL>
 __device__ __forceinline__ void store_pairs(uint16_t* v, int t0, const float (&lo)[8], const float (&hi)[8]) {
   if (IL) {
@@ -130,34 +140,47 @@ __device__ __forceinline__ void load_keys(const uint16_t* krow, int h2, u32x4 (&
 }
 // Then rotated.  base: (cos, sin) of the tile's position (local-position keys: of their record's), in LDS; rows(t): those
 // of the lane's key within the tile, for pairs t and t + 1.
-// AHEAD: operands whose rows are in flight together.
-template <int D, int KM, bool IL, int AHEAD, class Rows>
+template <int D, int KM, bool IL, class Rows>
+__device__ __forceinline__ void rotate_pairs(const u32x4& a, const u32x4& b, int t0, const float2* base, Rows rows,
+                                             float (&yl)[8], float (&yh)[8]) {
+  u32x4 lo = a, hi = b;
+  if (IL) deinterleave8(a, b, lo, hi);
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    if (KM == kKeysLocal) {
+      rotate_by(element(lo, e), element(hi, e), base[t0 + e], yl[e], yh[e]);
+      rotate_by(element(lo, e + 1), element(hi, e + 1), base[t0 + e + 1], yl[e + 1], yh[e + 1]);
+    } else {
+      const f32x4 r = rows(t0 + e);
+      rotate_pair(element(lo, e), element(hi, e), base[t0 + e], make_float2(r[0], r[1]), yl[e], yh[e]);
+      rotate_pair(element(lo, e + 1), element(hi, e + 1), base[t0 + e + 1], make_float2(r[2], r[3]), yl[e + 1], yh[e + 1]);
+    }
+  }
+}
+// Rounded to bf16 (ALiBi: only interleaved pairs would be split, and it has none).
+template <int D, int KM, bool IL, class Rows>
 __device__ __forceinline__ void rotate_keys(u32x4 (&kf)[D / 16], int h2, const float2* base, Rows rows) {
+  if (KM == kKeysAlibi) return;
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) {
-    const int t0 = 16 * s + 8 * h2;
-    u32x4 lo = kf[s], hi = kf[s + D / 32];
-    if (IL) deinterleave8(kf[s], kf[s + D / 32], lo, hi);
-    if (KM == kKeysNope || KM == kKeysLocal) {
-      float yl[8], yh[8];
+    float yl[8], yh[8];
+    rotate_pairs<D, KM, IL>(kf[s], kf[s + D / 32], 16 * s + 8 * h2, base, rows, yl, yh);
+    kf[s] = pack8(yl);
+    kf[s + D / 32] = pack8(yh);
+    if (s & 1) __builtin_amdgcn_sched_barrier(0);
+  }
+}
+// As two bf16 parts.
+template <int D, int KM, bool IL, class Rows>
+__device__ __forceinline__ void rotate_keys_split(u32x4 (&kh)[D / 16], u32x4 (&kl)[D / 16], int h2, const float2* base,
+                                                  Rows rows) {
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        if (KM == kKeysLocal) {
-          rotate_by(element(lo, e), element(hi, e), base[t0 + e], yl[e], yh[e]);
-          rotate_by(element(lo, e + 1), element(hi, e + 1), base[t0 + e + 1], yl[e + 1], yh[e + 1]);
-        } else {
-          const f32x4 r = rows(t0 + e);
-          rotate_pair(element(lo, e), element(hi, e), base[t0 + e], make_float2(r[0], r[1]), yl[e], yh[e]);
-          rotate_pair(element(lo, e + 1), element(hi, e + 1), base[t0 + e + 1], make_float2(r[2], r[3]), yl[e + 1],
-                      yh[e + 1]);
-        }
-      }
-      lo = pack8(yl);
-      hi = pack8(yh);
-    }
-    kf[s] = lo;
-    kf[s + D / 32] = hi;
-    if (s % AHEAD == AHEAD - 1) __builtin_amdgcn_sched_barrier(0);
+  for (int s = 0; s < D / 32; ++s) {
+    float yl[8], yh[8];
+    rotate_pairs<D, KM, IL>(kh[s], kh[s + D / 32], 16 * s + 8 * h2, base, rows, yl, yh);
+    split8(yl, kh[s], kl[s]);
+    split8(yh, kh[s + D / 32], kl[s + D / 32]);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
