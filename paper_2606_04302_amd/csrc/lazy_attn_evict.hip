@@ -178,11 +178,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
     if (have && ROT) {
       // Local-position keys turn by their record's position, the others by that of their 32-key block and a row's.
       if (lane < D / 2) turn_all[wave][lane] = rope_cs(LOCAL ? it.cur.pos : b0 + 32 * (wave & 1), rev);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      wait_reads();
       rotate_keys_split<D, KM, IL>(kh, kl, h2, turn_all[wave], [&](int t) {
         return *reinterpret_cast<const f32x4*>(trows + (lane & 31) * D + 4 * ((t / 2) ^ (lane & 15)));
       });
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      wait_reads();
     }
     const auto compute = [&](int row0, const uint16_t* tq, const float* nl) {
       const int rows = min(kStepRows, row_end - row0);
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
           rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + shift : INT32_MAX;
           if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wait_reads();
       }
       const TileOperands<D> op(again(lane));
       f32x16 s = f32x16{};
@@ -286,21 +286,31 @@ __global__ __launch_bounds__(256) void sum_weights(WeightArgs a) {
   }
 }
 
-// Weights of one new token per request.  S = Q K^T with 16x16x32 products: a key in lane % 16, query heads
-// 4 (lane / 16) + 0..3 of a group of 16 in its registers, so a key's sum over a group stays in four lanes.  Rotated
-// queries lie in LDS, kTokenRows rows at a time.
+// Weights of one new token per request: S = Q K^T of 16 keys and one KV head's queries at a time, a key in lane % 16.
+// Rotated queries lie in LDS, kTokenRows rows at a time.
+//   FEW (groups of up to kFewHeads query heads, keys that turn): products of 32-bit operands, 4 heads by 4 keys by 1
+//     element, the lanes' quarters taking a quarter of the elements each; two swaps of halves add them up and leave one
+//     head's score to a lane.  Nothing is split, and no rows of zeros are multiplied.
+//   Otherwise 16x16x32 products of bf16 in two parts (ALiBi keys: one, exact), query heads 4 (lane / 16) + 0..3 of a group
+//     of 16 in a lane's registers.
+//   64 requests of 16384 keys, us, 4x4x1 against 16x16x32: groups of 4 278 / 382, of 7 198 / 211, of 8 395 / 431, of 16
+//   167 / 130.
 //   HS = 1: workgroup (key split, request); a wave takes 16 keys of each 64-key tile for all KV heads, whose angles it
 //     forms once.
 //   HS = 4: workgroup (16 keys of every tile of a key split, request); its waves share the KV heads and add up their sums
 //     through LDS.  For batches whose tiles alone would leave CUs without work: a wave then waits for a quarter of the
 //     loads.
-// The next head's keys (or the next tile's first) are loaded during a head's products.
+// The next head's keys (or the next tile's first) are copied to LDS during a head's products, whole rows at a time: loads
+// in the operands' layout touch 64 places of 16 bytes each and took 235 us for the same 2.1 GB by themselves, when all of
+// them hit the first cache.  Bound there by the copies, which pass the L2s (253 us without the products), and close behind
+// by rotation and products (234 us with copies of the same few rows).
 //
 // SORT: requests that share chunks list them in orders of their own.  The records of a request (up to kSortRecords) are
 // walked in the order in which they are stored, and the workgroups of one key split of all requests run on one XCD: they
-// then read the same part of the store at about the same time, through one L2.  Every key's sum is its own, so results
-// do not depend on the order.
-constexpr int kTokenRows = 64, kTokenGroups = 16;  // query rows, and groups of up to 16 of one KV head, held in LDS
+// then read the same part of the store at about the same time.  Every key's sum is its own, so results do not depend on
+// the order.
+constexpr int kFewHeads = 8;
+constexpr int kTokenRows = 32, kTokenGroups = 16;  // query rows, and groups of up to 16 of one KV head, held in LDS
 constexpr int kSortRecords = 256;
 struct SortedRecord {
   int64_t koff;
@@ -345,44 +355,23 @@ struct SortedTable {
     __syncthreads();
   }
 };
-// A request's 64-key tiles, record after record of its table or of the sorted one, with the index of each record's first
-// key among the request's keys.
-template <bool SORT>
-struct TokenIter {
+// A request's 64-key tiles, record after record of its sorted table, with the index of each record's first key among the
+// request's keys.
+struct SortedIter {
   const SortedTable* table;
-  cptr<lazy_chunk_t> recs;
   int i, j0, left, base;
-  bool sorted;
   Rec cur;
   __device__ void load() {
-    if (SORT && sorted) {
-      const SortedRecord r = table->rec[i];
-      cur.koff =
-          (int64_t)((uint64_t)(uint32_t)uniform((int)((uint64_t)r.koff >> 32)) << 32 | (uint32_t)uniform((int)r.koff));
-      cur.len = uniform(r.len);
-      cur.pos = uniform(r.pos);
-      cur.kst = uniform(r.kst);
-      base = uniform(r.base);
-    } else {
-      cur = load_rec(recs + i);
-    }
-  }
-  __device__ void start(const lazy_chunk_t* chunks, int c0, int c1, int split, int splits) {
-    KeyIter it;
-    it.start(chunks, c0, c1, split, splits);
-    sorted = false;
-    table = nullptr;
-    recs = it.recs;
-    i = it.i;
-    j0 = it.j0;
-    left = it.left;
-    base = it.base;
-    cur = it.cur;
+    const SortedRecord r = table->rec[i];
+    cur.koff =
+        (int64_t)((uint64_t)(uint32_t)uniform((int)((uint64_t)r.koff >> 32)) << 32 | (uint32_t)uniform((int)r.koff));
+    cur.len = uniform(r.len);
+    cur.pos = uniform(r.pos);
+    cur.kst = uniform(r.kst);
+    base = uniform(r.base);
   }
   __device__ void start(const SortedTable* t, int n, int split, int splits) {
-    sorted = true;
     table = t;
-    recs = nullptr;
     const int total = n > 0 ? uniform(t->tiles[n - 1]) : 0;
     const int lo = (int)((int64_t)total * split / splits), hi = (int)((int64_t)total * (split + 1) / splits);
     left = hi - lo;
@@ -407,26 +396,40 @@ struct TokenIter {
     if (left <= 0 || j0 < cur.len) return;
     j0 = 0;
     do {  // tiles are left, so a record with keys lies ahead
-      if (!(SORT && sorted)) base += cur.len;
       ++i;
       load();
     } while (cur.len == 0);
   }
 };
 
-template <int D, int KMI, int HS, bool SORT>
+// Half a wave's (W = 32) or half a row pair's (W = 16) sums of x, and of y in the other half.
+template <int W>
+__device__ __forceinline__ float add_halves(float x, float y) {
+  const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+  const auto z = W == 32 ? __builtin_amdgcn_permlane32_swap(a, b, false, false)
+                         : __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  return __uint_as_float(z[0]) + __uint_as_float(z[1]);
+}
+
+template <int D, int KMI, int HS, bool SORT, bool FEW>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) void weigh_token(WeightArgs a) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
   constexpr int QLD = D + kPad, H = D / 64, TPR = D / 16;
-  typedef TokenIter<SORT> Iter;
-  constexpr int PARTS = ROT ? 2 : 1;
-  __shared__ uint16_t q[PARTS * kTokenRows * QLD] __attribute__((aligned(16)));
+  constexpr int PARTS = ROT ? 2 : 1, FLD = D + 4;
+  static_assert(ROT || !FEW);
+  __shared__ uint16_t q[FEW ? 2 * kTokenRows * FLD : PARTS * kTokenRows * QLD] __attribute__((aligned(16)));
+  float* const qf = reinterpret_cast<float*>(q);
   __shared__ float nlse[kTokenGroups * 16] __attribute__((aligned(16)));
-  __shared__ float rslope[kTokenGroups * 16] __attribute__((aligned(16)));
-  __shared__ double freq[D / 2];
+  __shared__ float rslope[ALIBI ? kTokenGroups * 16 : 4] __attribute__((aligned(16)));
   __shared__ float2 qcs[D / 2];
   __shared__ float sums[2][4][16];
+  // Angles of a wave's 16 keys: those of its first key, and of positions 0 .. 15 (rows 4 banks apart).  In 64 bits for
+  // every key and pair they took a seventh of the time.
+  constexpr int RLD = D + 4;
+  __shared__ uint16_t tiles[4 * 16 * D] __attribute__((aligned(16)));  // a wave's 16 keys of one head
+  __shared__ float2 base_all[4][D / 2] __attribute__((aligned(16)));
+  __shared__ float rows16[KM == kKeysNope ? 16 * RLD : 4] __attribute__((aligned(16)));
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, kq = lane >> 4;
   int r = blockIdx.y, split = HS == 1 ? blockIdx.x : blockIdx.x >> 2;
   const int sub = HS == 1 ? wave : blockIdx.x & 3;
@@ -438,149 +441,233 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
   }
   const int qpos = a.q_pos0[r], room = a.key_start[r + 1] - a.key_start[r];
   const int c0 = a.chunk_start[r], c1 = a.chunk_start[r + 1];
-  Iter it0;
-  bool sorted = false;
-  if constexpr (SORT) {
-    __shared__ SortedTable table;
-    sorted = c1 - c0 <= kSortRecords;
-    if (sorted) {
-      table.build(a.chunks + c0, c1 - c0, kSub);
-      it0.start(&table, c1 - c0, split, a.splits);
-    }
-  }
-  if (!sorted) it0.start(a.chunks, c0, c1, split, a.splits);
   if (ROT && tid < D / 2) {
-    const double rev = revolutions(a, tid);
-    freq[tid] = rev;
-    qcs[tid] = rope_cs(a.rotate_q ? qpos : 0, rev);
+    qcs[tid] = rope_cs(a.rotate_q ? qpos : 0, revolutions(a, tid));
+  }
+  const double own_rev = ROT ? revolutions(a, lane % (D / 2)) : 0.0;
+  if (KM == kKeysNope) {
+    static_assert(256 % (D / 2) == 0, "a thread's entries share one pair");
+    for (int e = tid; e < 16 * (D / 2); e += 256)
+      *reinterpret_cast<float2*>(rows16 + e / (D / 2) * RLD + 2 * (e % (D / 2))) = rope_cs(e / (D / 2), own_rev);
   }
   const int per_head = (a.group + 15) / 16, groups = a.hkv * per_head, per_group = min(a.group, 16);
   const int most = min(kTokenGroups, kTokenRows / per_group);
-  for (int g0 = 0; g0 < groups; g0 += most) {
-    const int ng = min(most, groups - g0);
-    __syncthreads();
-    for (int e = tid; e < ng * per_group * TPR; e += 256) {
-      const int row = e / TPR, t0 = 8 * (e % TPR), grp = g0 + row / per_group;
-      const int in = min((grp % per_head) * 16 + row % per_group, a.group - 1);
-      u32x4 lo, hi;
-      load_pairs<D, IL>(a.q + ((int64_t)r * a.hq + (grp / per_head) * a.group + in) * D, t0, lo, hi);
-      uint16_t* const to = q + row * QLD + t0;
-      if (ROT) {
-        float yl[8], yh[8];
+  uint16_t* const tile = tiles + wave * 16 * D;
+  // All groups of query heads over the tiles from it0 on.
+  const auto walk = [&](const auto& it0) {
+    for (int g0 = 0; g0 < groups; g0 += most) {
+      const int ng = min(most, groups - g0);
+      __syncthreads();
+      for (int e = tid; e < ng * per_group * TPR; e += 256) {
+        const int row = e / TPR, t0 = 8 * (e % TPR), grp = g0 + row / per_group;
+        const int in = min((grp % per_head) * 16 + row % per_group, a.group - 1);
+        u32x4 lo, hi;
+        load_pairs<D, IL>(a.q + ((int64_t)r * a.hq + (grp / per_head) * a.group + in) * D, t0, lo, hi);
+        uint16_t* const to = q + row * QLD + t0;
+        if (ROT) {
+          float yl[8], yh[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          rotate_by(element(lo, k), element(hi, k), qcs[t0 + k], yl[k], yh[k]);
-        u32x4 rest;
-        split8(yl, lo, rest);
-        *reinterpret_cast<u32x4*>(to + kTokenRows * QLD) = rest;
-        split8(yh, hi, rest);
-        *reinterpret_cast<u32x4*>(to + kTokenRows * QLD + D / 2) = rest;
-      }
-      *reinterpret_cast<u32x4*>(to) = lo;
-      *reinterpret_cast<u32x4*>(to + D / 2) = hi;
-    }
-    for (int e = tid; e < ng * 16; e += 256) {  // rows past a group's end: exp2(score - inf) = 0
-      const int grp = g0 + e / 16, in = (grp % per_head) * 16 + e % 16, h = (grp / per_head) * a.group + in;
-      const float lse = in < a.group ? a.lse[(int64_t)r * a.hq + h] : -INFINITY;
-      nlse[e] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
-      rslope[e] = ALIBI && in < a.group ? alibi_slope(h, a.hq, a.inv_freq, 1.f) : 0.f;
-    }
-    __syncthreads();
-    // A wave's groups: first, first + step, ...
-    const int first = HS == 1 ? 0 : wave, step = HS;
-    const auto fetch = [&](const Iter& t, int k, u32x4 (&raw)[H][2]) {
-      const int key = t.j0 + 16 * sub + col;
-      const uint16_t* krow = k_ptr(a.k_pool, t.cur, (g0 + k) / per_head, key < t.cur.len ? key : t.j0, D);
+          for (int k = 0; k < 8; ++k)
+            rotate_by(element(lo, k), element(hi, k), qcs[t0 + k], yl[k], yh[k]);
+          if (FEW) {
+            float* const f = qf + row * FLD + t0;
 #pragma unroll
-      for (int s = 0; s < H; ++s) {
-        const int t0 = 32 * s + 8 * kq;
-        raw[s][0] = *reinterpret_cast<const u32x4*>(krow + (IL ? 2 * t0 : t0));
-        raw[s][1] = *reinterpret_cast<const u32x4*>(krow + (IL ? 2 * t0 + 8 : D / 2 + t0));
+            for (int k = 0; k < 8; k += 4) {
+              *reinterpret_cast<f32x4*>(f + k) = f32x4{yl[k], yl[k + 1], yl[k + 2], yl[k + 3]};
+              *reinterpret_cast<f32x4*>(f + D / 2 + k) = f32x4{yh[k], yh[k + 1], yh[k + 2], yh[k + 3]};
+            }
+            continue;
+          }
+          u32x4 rest;
+          split8(yl, lo, rest);
+          *reinterpret_cast<u32x4*>(to + kTokenRows * QLD) = rest;
+          split8(yh, hi, rest);
+          *reinterpret_cast<u32x4*>(to + kTokenRows * QLD + D / 2) = rest;
+        }
+        *reinterpret_cast<u32x4*>(to) = lo;
+        *reinterpret_cast<u32x4*>(to + D / 2) = hi;
       }
-    };
-    Iter it = it0;
-    u32x4 raw[H][2];
-    if (it.left > 0 && first < ng) fetch(it, first, raw);
-    int parity = 0;
-    const uint16_t* const qrow = q + min(col, per_group - 1) * QLD + 8 * kq;
-    while (it.left > 0) {
-      Iter ahead = it;
-      ahead.next();
-      const int key = it.j0 + 16 * sub + col;
-      const bool in = key < it.cur.len;
-      const int p = it.cur.pos + key;
+      for (int e = tid; e < ng * 16; e += 256) {  // rows past a group's end: exp2(score - inf) = 0
+        const int grp = g0 + e / 16, in = (grp % per_head) * 16 + e % 16, h = (grp / per_head) * a.group + in;
+        const float lse = in < a.group ? a.lse[(int64_t)r * a.hq + h] : -INFINITY;
+        nlse[e] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
+        if (ALIBI) rslope[e] = in < a.group ? alibi_slope(h, a.hq, a.inv_freq, 1.f) : 0.f;
+      }
+      __syncthreads();
+      // A wave's groups: first, first + step, ...
+      const int first = HS == 1 ? 0 : wave, step = HS;
+      const float* const prior = g0 > 0 ? a.weights : a.weights_in;
+      const float fade = g0 > 0 ? 1.f : a.decay;
+      const auto fetch = [&](const auto& t, int k) {
+        const uint16_t* const from = k_ptr(a.k_pool, t.cur, (g0 + k) / per_head, t.j0, D);
+        const int last = t.cur.len - 1 - t.j0;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          const int row = (64 * i + lane) / (D / 8), chunk = (64 * i + lane) % (D / 8) ^ swizzle<D>(row);
+          copy_async(from + (uint32_t)(min(16 * sub + row, last) * D + 8 * chunk), tile + 512 * i);
+        }
+      };
+      const uint16_t* const qrow = q + min(col, per_group - 1) * QLD + 8 * kq;
+      const float* const frow = qf + 8 * kq;
+      auto it = it0, ahead = it0;
+      int k = first, kf = first, parity = 0;
+      float sum = 0.f, old = 0.f;
       float2 cs[H][8];
-      if (ROT) {
+      const auto fetch_next = [&] {
+        if (ahead.left <= 0) return;
+        fetch(ahead, kf);
+        kf += step;
+        if (kf >= ng) {
+          kf = first;
+          ahead.next();
+        }
+      };
+      const auto begin = [&] {
+        const int key = it.j0 + 16 * sub + col, at = it.base + key;
+        sum = old = 0.f;
+        if (prior && key < it.cur.len && at < room) old = prior[a.key_start[r] + at];
+        if (ROT) {
+          float2* const base = base_all[wave];
+          if (lane < D / 2) base[lane] = rope_cs(LOCAL ? it.cur.pos : it.cur.pos + it.j0 + 16 * sub, own_rev);
+          wait_reads();
 #pragma unroll
-        for (int s = 0; s < H; ++s)
+          for (int s = 0; s < H; ++s)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) cs[s][e] = rope_cs(LOCAL ? it.cur.pos : p, freq[32 * s + 8 * kq + e]);
-      }
-      float sum = 0.f;
-      for (int k = first; k < ng; k += step) {
-        u32x4 kh[2 * H], kl[2 * H];
+            for (int e = 0; e < 8; e += 2) {
+              const int t = 32 * s + 8 * kq + e;
+              const f32x4 x = *reinterpret_cast<const f32x4*>(base + t);
+              f32x4 y = {1.f, 0.f, 1.f, 0.f};
+              if (!LOCAL) y = *reinterpret_cast<const f32x4*>(rows16 + col * RLD + 2 * t);
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                cs[s][e + i] = LOCAL ? make_float2(x[2 * i], x[2 * i + 1])
+                                     : make_float2(fmaf(x[2 * i], y[2 * i], -(x[2 * i + 1] * y[2 * i + 1])),
+                                                   fmaf(x[2 * i + 1], y[2 * i], x[2 * i] * y[2 * i + 1]));
+            }
+        }
+      };
+      const auto finish = [&] {
+        const int key = it.j0 + 16 * sub + col, at = it.base + key;
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (HS > 1) {  // the waves' sums, in their order; two buffers, so one barrier a tile
+          if (kq == 0) sums[parity][wave][col] = sum;
+          __syncthreads();
+          if (wave == 0) sum = (sums[parity][0][col] + sums[parity][1][col]) + (sums[parity][2][col] + sums[parity][3][col]);
+          parity ^= 1;
+        }
+        if (a.causal && it.cur.pos + key > qpos) sum = 0.f;
+        if ((HS == 1 || wave == 0) && kq == 0 && key < it.cur.len && at < room)
+          a.weights[a.key_start[r] + at] = prior ? fmaf(fade, old, sum) : sum;
+        it.next();
+      };
+      const auto consume = [&] {
+        u32x4 raw[H][2];
+        wait_copies();
 #pragma unroll
         for (int s = 0; s < H; ++s) {
-          u32x4 lo = raw[s][0], hi = raw[s][1];
-          if (IL) deinterleave8(raw[s][0], raw[s][1], lo, hi);
-          if (ROT) {
-            float yl[8], yh[8];
+          const int c = 4 * s + kq;
+          raw[s][0] = *reinterpret_cast<const u32x4*>(tile + tile_at<D>(col, IL ? 2 * c : c));
+          raw[s][1] = *reinterpret_cast<const u32x4*>(tile + tile_at<D>(col, IL ? 2 * c + 1 : D / 16 + c));
+        }
+        if (k == first) begin();
+        wait_reads();
+        fetch_next();
+        if constexpr (FEW) {
+          float yl[H][8], yh[H][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) rotate_by(element(lo, e), element(hi, e), cs[s][e], yl[e], yh[e]);
-            split8(yl, lo, kl[s]);
-            split8(yh, hi, kl[s + H]);
+          for (int s = 0; s < H; ++s) {
+            u32x4 lo = raw[s][0], hi = raw[s][1];
+            if (IL) deinterleave8(raw[s][0], raw[s][1], lo, hi);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rotate_by(element(lo, e), element(hi, e), cs[s][e], yl[s][e], yh[s][e]);
           }
-          kh[s] = lo;
-          kh[s + H] = hi;
-        }
-        if (k + step < ng)
-          fetch(it, k + step, raw);
-        else if (ahead.left > 0)
-          fetch(ahead, first, raw);
-        f32x4 s4 = f32x4{};
+          for (int m = 0; m < per_group; m += 4) {
+            const float* const at = frow + (k * per_group + min(m + (lane & 3), per_group - 1)) * FLD;
+            f32x4 s4[2] = {f32x4{}, f32x4{}};
 #pragma unroll
-        for (int s = 0; s < 2 * H; ++s) {
-          const uint16_t* at = qrow + k * per_group * QLD + 32 * s;
-          const bf16x8 fh = as_bf16x8(*reinterpret_cast<const u32x4*>(at));
-          if (ROT) {
-            const bf16x8 fl = as_bf16x8(*reinterpret_cast<const u32x4*>(at + kTokenRows * QLD));
-            s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fl, as_bf16x8(kh[s]), s4, 0, 0, 0);
-            s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, as_bf16x8(kl[s]), s4, 0, 0, 0);
+            for (int s = 0; s < H; ++s)
+#pragma unroll
+              for (int e = 0; e < 8; e += 4) {
+                const f32x4 fl = *reinterpret_cast<const f32x4*>(at + 32 * s + e);
+                const f32x4 fh = *reinterpret_cast<const f32x4*>(at + D / 2 + 32 * s + e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  s4[0] = __builtin_amdgcn_mfma_f32_4x4x1f32(fl[i], yl[s][e + i], s4[0], 0, 0, 0);
+                  s4[1] = __builtin_amdgcn_mfma_f32_4x4x1f32(fh[i], yh[s][e + i], s4[1], 0, 0, 0);
+                }
+              }
+            s4[0] += s4[1];
+            const float x = add_halves<32>(s4[0][0], s4[0][2]), y = add_halves<32>(s4[0][1], s4[0][3]);
+            sum += fast_exp2(fmaf(add_halves<16>(x, y), a.scale_log2, nlse[16 * k + m + kq]));
           }
-          s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, as_bf16x8(kh[s]), s4, 0, 0, 0);
-        }
-        {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(nlse + 16 * k + 4 * kq);
+        } else {
+          u32x4 kh[2 * H], kl[2 * H];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s4[e] = fmaf(s4[e], a.scale_log2, x[e]);
-        }
-        if (ALIBI) {
-          const f32x4 sl = *reinterpret_cast<const f32x4*>(rslope + 16 * k + 4 * kq);
+          for (int s = 0; s < H; ++s) {
+            u32x4 lo = raw[s][0], hi = raw[s][1];
+            if (IL) deinterleave8(raw[s][0], raw[s][1], lo, hi);
+            if (ROT) {
+              float yl[8], yh[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s4[e] = fmaf(sl[e], (float)(p - qpos), s4[e]);
+              for (int e = 0; e < 8; ++e) rotate_by(element(lo, e), element(hi, e), cs[s][e], yl[e], yh[e]);
+              split8(yl, lo, kl[s]);
+              split8(yh, hi, kl[s + H]);
+            }
+            kh[s] = lo;
+            kh[s + H] = hi;
+          }
+          f32x4 s4 = f32x4{};
+#pragma unroll
+          for (int s = 0; s < 2 * H; ++s) {
+            const uint16_t* at = qrow + k * per_group * QLD + 32 * s;
+            const bf16x8 fh = as_bf16x8(*reinterpret_cast<const u32x4*>(at));
+            if (ROT) {
+              const bf16x8 fl = as_bf16x8(*reinterpret_cast<const u32x4*>(at + kTokenRows * QLD));
+              s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fl, as_bf16x8(kh[s]), s4, 0, 0, 0);
+              s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, as_bf16x8(kl[s]), s4, 0, 0, 0);
+            }
+            s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, as_bf16x8(kh[s]), s4, 0, 0, 0);
+          }
+          {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(nlse + 16 * k + 4 * kq);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s4[e] = fmaf(s4[e], a.scale_log2, x[e]);
+          }
+          if (ALIBI) {
+            const f32x4 sl = *reinterpret_cast<const f32x4*>(rslope + 16 * k + 4 * kq);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s4[e] = fmaf(sl[e], (float)(it.cur.pos + it.j0 + 16 * sub + col - qpos), s4[e]);
+          }
+          sum += (fast_exp2(s4[0]) + fast_exp2(s4[1])) + (fast_exp2(s4[2]) + fast_exp2(s4[3]));
         }
-        sum += (fast_exp2(s4[0]) + fast_exp2(s4[1])) + (fast_exp2(s4[2]) + fast_exp2(s4[3]));
+        k += step;
+        if (k >= ng) {
+          k = first;
+          finish();
+        }
+      };
+      if (first < ng) {
+        fetch_next();
+        while (it.left > 0) consume();
+      } else {
+        while (it.left > 0) finish();
       }
-      sum += __shfl_xor(sum, 16, 64);
-      sum += __shfl_xor(sum, 32, 64);
-      if (HS > 1) {  // the waves' sums, in their order; two buffers, so one barrier a tile
-        if (kq == 0) sums[parity][wave][col] = sum;
-        __syncthreads();
-        if (wave == 0) sum = (sums[parity][0][col] + sums[parity][1][col]) + (sums[parity][2][col] + sums[parity][3][col]);
-        parity ^= 1;
-      }
-      if (a.causal && p > qpos) sum = 0.f;
-      const int at = it.base + key;
-      if ((HS == 1 || wave == 0) && kq == 0 && in && at < room) {
-        float* w = a.weights + a.key_start[r] + at;
-        if (g0 > 0)
-          *w += sum;
-        else
-          *w = a.weights_in ? fmaf(a.decay, a.weights_in[a.key_start[r] + at], sum) : sum;
-      }
-      it = ahead;
+    }
+  };
+  if constexpr (SORT) {
+    __shared__ SortedTable table;
+    if (c1 - c0 <= kSortRecords) {
+      table.build(a.chunks + c0, c1 - c0, kSub);
+      SortedIter it;
+      it.start(&table, c1 - c0, split, a.splits);
+      walk(it);
+      return;
     }
   }
+  KeyIter it;
+  it.start(a.chunks, c0, c1, split, a.splits);
+  walk(it);
 }
 
 // Selection: a radix select of the b-th largest score, 11, 11 and 10 bits at a time, and an ordered compaction.  Scores
@@ -956,15 +1043,21 @@ hipError_t prompt_mode(const WeightArgs& a, int max_kv_len, hipStream_t s) {
   sum_weights<<<dim3((max_kv_len + 255) / 256, a.batch), 256, 0, s>>>(a);
   return hipGetLastError();
 }
+template <int D, int KMI, bool FEW>
+hipError_t token_heads(const WeightArgs& a, hipStream_t s) {
+  if (a.head_split)
+    weigh_token<D, KMI, 4, false, FEW><<<dim3(4 * a.splits, a.batch), 256, 0, s>>>(a);
+  else if (a.sort_records)
+    weigh_token<D, KMI, 1, true, FEW><<<dim3(a.splits, a.batch), 256, 0, s>>>(a);
+  else
+    weigh_token<D, KMI, 1, false, FEW><<<dim3(a.splits, a.batch), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
 template <int D, int KMI>
 hipError_t token_mode(const WeightArgs& a, hipStream_t s) {
-  if (a.head_split)
-    weigh_token<D, KMI, 4, false><<<dim3(4 * a.splits, a.batch), 256, 0, s>>>(a);
-  else if (a.sort_records)
-    weigh_token<D, KMI, 1, true><<<dim3(a.splits, a.batch), 256, 0, s>>>(a);
-  else
-    weigh_token<D, KMI, 1, false><<<dim3(a.splits, a.batch), 256, 0, s>>>(a);
-  return hipGetLastError();
+  if constexpr (keys_of(KMI) != kKeysAlibi)
+    if (a.group <= kFewHeads) return token_heads<D, KMI, true>(a, s);
+  return token_heads<D, KMI, false>(a, s);
 }
 
 template <int D, int TURN>

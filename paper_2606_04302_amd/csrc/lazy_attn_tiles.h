@@ -68,6 +68,8 @@ __device__ __forceinline__ void wait_copies() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
+// Every LDS access so far has ended; no memory access moves across.
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // Packed row -> token: row / G by multiplication (total_q * G * G < 2^32, checked by the planner).
 __device__ __forceinline__ int token_of(int row, uint32_t magic) { return magic ? (int)__umulhi(row, magic) : row; }

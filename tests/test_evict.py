@@ -228,6 +228,23 @@ def test_running_sums_and_room_behind_the_keys(gpu, decay):
     check_weights(decode_of(w), {}, f"token decay {decay}", room=5, decay=decay)
 
 
+# Batches whose requests are walked in storage order: a workgroup reads half a megabyte or more.
+BATCHES = {
+    "group 4": (lambda: shared(75, 16, 4, 128, [230, 264, 70], [1], reqs=770), {}),
+    "group 12, interleaved": (lambda: shared(76, 24, 2, 128, [500, 40, 517], [1], reqs=769),
+                              dict(rope_style=ops.ROPE_INTERLEAVED)),
+    "local, d64": (lambda: shared(77, 8, 4, 64, [600, 500], [1], reqs=768), dict(key_positions=ops.KEYS_LOCAL)),
+    "more records than are sorted": (lambda: W.paginate(shared(78, 4, 4, 128, [270, 260], [1], reqs=768), 1), {}),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", BATCHES)
+def test_token_weights_of_many_requests(gpu, name):
+    make, ckw = BATCHES[name]
+    check_weights(decode_of(make()), ckw, name)
+
+
 @pytest.mark.gpu
 def test_requests_without_queries_or_keys(gpu):
     w = W.custom(71, 4, 2, 64, 1e4, [dict(chunks=[(70, 0)], q_len=0, q_pos0=0), dict(chunks=[], q_len=3, q_pos0=0),
