@@ -854,9 +854,11 @@ struct SelectArgs {
   int32_t* ws;  // [batch][slices] of SliceWork (long requests)
   int sink, recent, slices;
 };
-// A slice's counts of each pass's digits.
+// A slice's counts of each pass's digits; the digits found so far, the rank left, and earlier slices' scores above them.
 struct SliceWork {
   int hist[3][kBins];
+  uint32_t prefix;
+  int need, above, unused;
 };
 
 __device__ __forceinline__ bool trivial_selection(const SelectArgs& a, int n, int b, int o0) {
@@ -910,51 +912,49 @@ __global__ __launch_bounds__(kSelectThreads) void select_slices(SelectArgs a) {
   if (w >= used) return;
   const int j0 = w * kSlice, count = min(kSlice, n - j0);
   const int filled = load_scores<PASS == 0>(sm, a.weights + k0, j0, count, n, a.sink, a.recent);
-  if (tid < 2) before_s[tid] = 0;
-  // The digits counted so far, from every slice's counts.
+  SliceWork& own = all[w];
   uint32_t prefix = 0;
   int need = b;
-#pragma unroll
-  for (int pass = 0; pass < PASS; ++pass) {
-    int c[2] = {0, 0};
+  if constexpr (PASS > 0) {  // the digit counted last, from every slice's counts
+    if (tid < 2) before_s[tid] = PASS > 1 && tid == 0 ? own.above : 0;
+    if (PASS > 1) {
+      prefix = own.prefix;
+      need = own.need;
+    }
+    int c[2] = {0, 0}, earlier[2] = {0, 0};
     const int b1 = kBins - 1 - 2 * tid;
     for (int v0 = 0; v0 < used; v0 += 8) {
       int2 x[8];
 #pragma unroll
       for (int v = 0; v < 8; ++v)
-        x[v] = *reinterpret_cast<const int2*>(&all[min(v0 + v, used - 1)].hist[pass][b1 - 1]);
+        x[v] = *reinterpret_cast<const int2*>(&all[min(v0 + v, used - 1)].hist[PASS - 1][b1 - 1]);
 #pragma unroll
       for (int v = 0; v < 8; ++v) {
         c[0] += v0 + v < used ? x[v].y : 0;
         c[1] += v0 + v < used ? x[v].x : 0;
+        earlier[0] += v0 + v < w ? x[v].y : 0;
+        earlier[1] += v0 + v < w ? x[v].x : 0;
       }
     }
     find_digit(sm, c, need);
     const int digit = sm.digit;
-    prefix = with_digit(prefix, digit, pass);
+    prefix = with_digit(prefix, digit, PASS - 1);
     need = sm.need;
-    if (PASS == 3) {  // scores of earlier slices above the threshold, and equal to it
-      int above = 0;
-      for (int v0 = 0; v0 < w; v0 += 8) {
-        int2 x[8];
-#pragma unroll
-        for (int v = 0; v < 8; ++v)
-          x[v] = *reinterpret_cast<const int2*>(&all[min(v0 + v, w - 1)].hist[pass][b1 - 1]);
-#pragma unroll
-        for (int v = 0; v < 8; ++v) {
-          if (v0 + v >= w) continue;
-          above += (b1 > digit ? x[v].y : 0) + (b1 - 1 > digit ? x[v].x : 0);
-          if (pass == 2 && (b1 == digit || b1 - 1 == digit)) atomicAdd(&before_s[1], b1 == digit ? x[v].y : x[v].x);
-        }
-      }
-      above = wave_incl_scan(above);
-      if ((tid & 63) == 63 && above) atomicAdd(&before_s[0], above);
-    }
+    const int above = wave_incl_scan((b1 > digit ? earlier[0] : 0) + (b1 - 1 > digit ? earlier[1] : 0));
+    if ((tid & 63) == 63 && above) atomicAdd(&before_s[0], above);
+    if (b1 == digit || b1 - 1 == digit) before_s[1] = b1 == digit ? earlier[0] : earlier[1];
     __syncthreads();
   }
   if (PASS < 3) {
-    if (PASS > 0) count_digits(sm, filled, prefix, PASS);
-    *reinterpret_cast<int2*>(&all[w].hist[PASS][2 * tid]) = own_bins(sm, tid);
+    if (PASS > 0) {
+      if (tid == 0) {
+        own.prefix = prefix;
+        own.need = need;
+        own.above = before_s[0];
+      }
+      count_digits(sm, filled, prefix, PASS);
+    }
+    *reinterpret_cast<int2*>(&own.hist[PASS][2 * tid]) = own_bins(sm, tid);
   } else {
     write_kept(sm, j0, filled, prefix, need, before_s[0], before_s[1], a.kept + o0);
   }
