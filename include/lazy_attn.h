@@ -232,7 +232,8 @@ LAZY_API int lazy_attn_combine(const void* part_o, const float* part_lse, int32_
  *     dq_i = scale R(-p_i) sum_j dS_ij R(p_j) k_j, dk_j = scale sum_i R(-p_j) dS_ij R(p_i) q_i,
  * where the sums for a stored key run over every request, position and query head that reads it: a chunk that several
  * requests share receives the sum of their gradients, each turned back from its own position.  Rows that see no key
- * (lse = -inf) give and receive nothing.
+ * (lse = -inf) give and receive nothing, whatever q, out and dout hold there.  Everything else that is read has to be
+ * finite: the matrix cores also multiply a tile's hidden pairs, by zero.
  *
  * Which requests read a stored key is worked out once per set of tables, on the host, by lazy_attn_backward_plan:
  * every 64 stored keys become a tile with the list of its uses, tiles with much work are cut into parts, and the rows
@@ -268,7 +269,7 @@ typedef struct lazy_backward_info {
  * (records of length 0 are passed over), or records whose stored keys overlap in a way that gives a key no single
  * gradient: other strides, a distance that is no whole number of keys, or keys that two records pair with different
  * values.  Records of one chunk that overlap with the same strides and pairing (other lengths, other first keys) are
- * fine.  LAZY_EUNSUPPORTED: total_q * G * G >= 2^32.
+ * fine.  LAZY_EUNSUPPORTED: total_q * G * G >= 2^32, or more work items than a launch holds (2^24 tiles and KV heads).
  */
 LAZY_API int lazy_attn_backward_plan(const lazy_attn_params_t* params, const int32_t* q_start, const int32_t* q_pos0,
                                      const lazy_chunk_t* chunks, const int32_t* chunk_start, int32_t batch, void* plan,
@@ -284,7 +285,8 @@ LAZY_API size_t lazy_attn_backward_workspace_size(const lazy_attn_params_t* para
  *   dlse     [total_q][Hq] fp32, gradient by lse (a loss over merged partial results depends on it), or NULL
  *   dq       [total_q][Hq][D] bf16, fully overwritten
  *   dk_pool, dv_pool  bf16 bases laid out like k_pool and v_pool (they may be the same pointer, provided that no
- *            record's keys are another's values).  Every key of every record is overwritten, with zeros where no query
+ *            record's keys are another's values; they are not k_pool's or v_pool's own memory: LAZY_EINVAL if the
+ *            same pointer).  Every key of every record is overwritten, with zeros where no query
  *            sees it; everything else is left as it was.
  *   workspace  at least lazy_attn_backward_workspace_size(...) bytes, 16-byte aligned.
  * Gradients are rounded to bf16 once, from fp32 sums; q (rotated, times the scale) and the keys are rounded to bf16
@@ -310,14 +312,16 @@ LAZY_API int lazy_attn_prefill_backward(const lazy_attn_params_t* params, const 
  * for key_start[r+1] - key_start[r] keys, which may be more than it has (a growing tail): what lies behind a request's
  * last key is neither read nor written, and keys without room are passed over.
  *     weights_j = decay * weights_in_j + sum over the request's query tokens and all query heads of exp(s - lse)
- * with s the scaled score of the attention entry points (0 for hidden keys and for rows with lse = -inf).  q, q_start,
+ * with s the scaled score of the attention entry points (0 for hidden keys and for rows with lse = -inf, whatever
+ * q holds there).  q, q_start,
  * q_pos0 (q_pos) and lse are what the attention call had and wrote; any rows of a prompt may be given, say its last
  * ones, as long as q_pos0 is the position of the first of them.
  *   weights_in  fp32 running sums, or NULL (then decay has no effect); may be the same array as weights
  *   decay       finite, what the running sums are multiplied by (1: plain accumulation)
  *   num_keys    size of the weights arrays, key_start[batch] (the prefill form sizes its workspace by it)
  *   workspace   device scratch of at least ..._workspace_size(...) bytes, 16-byte aligned (may be NULL if 0)
- * Sums are fp32 in a fixed order: equal calls give equal bits.  num_splits and cache_hint have no effect.
+ * Rotated queries and keys keep 16 bits or more (attention outputs, which are bf16, are formed with 8).  Sums are fp32 in
+ * a fixed order: equal calls give equal bits.  num_splits and cache_hint have no effect.
  */
 LAZY_API int lazy_attn_prefill_key_weights(const lazy_attn_params_t* params, const void* q, const int32_t* q_start,
                                            const int32_t* q_pos0, const void* k_pool, const lazy_chunk_t* chunks,
@@ -330,7 +334,7 @@ LAZY_API size_t lazy_attn_prefill_key_weights_workspace_size(const lazy_attn_par
                                                              int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
                                                              int32_t num_keys);
 
-/* One new token per request: q [batch][Hq][D], q_pos [batch], lse [batch][Hq].  Reads K once. */
+/* One new token per request: q [batch][Hq][D], q_pos [batch], lse [batch][Hq]. */
 LAZY_API int lazy_attn_decode_key_weights(const lazy_attn_params_t* params, const void* q, const int32_t* q_pos,
                                           const void* k_pool, const lazy_chunk_t* chunks, const int32_t* chunk_start,
                                           const int32_t* key_start, int32_t batch, int32_t max_kv_len, const float* lse,
@@ -362,9 +366,10 @@ LAZY_API size_t lazy_cache_select_workspace_size(int32_t batch, int32_t max_kv_l
  *      from their index in the old record to that in the new one.
  *   1  keys keep their old positions: they are rotated there, as lazy_materialize_k does, for lazy_plain_attn_prefill
  *      and lazy_plain_attn_decode.  LAZY_EUNSUPPORTED with LAZY_ALIBI.
- * max_kept bounds the requests' kept counts.  weights_out (with weights and key_start as above; all three or none)
- * receives the kept keys' weights at kept_start[r] + i (0 for entries that are passed over).  k_out and v_out may lie
- * in the pools' own memory (or be the same pointer) as long as no new record overlaps another or what a table reads.
+ * max_kept bounds the requests' kept counts (LAZY_EUNSUPPORTED from 2^24 on).  weights_out (with weights and key_start
+ * as above; all three or none) receives the kept keys' weights at kept_start[r] + i (0 for entries that name no key, or
+ * one without room in weights).  k_out and v_out may lie in the pools' own memory (or be the same pointer) as long as no
+ * new record overlaps another or what a table reads.
  */
 LAZY_API int lazy_cache_compact(const lazy_attn_params_t* params, const void* k_pool, const void* v_pool,
                                 const lazy_chunk_t* chunks, const int32_t* chunk_start, int32_t batch,

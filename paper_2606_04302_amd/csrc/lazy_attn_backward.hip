@@ -48,6 +48,9 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
     const int64_t dst = (int64_t)(h / a.group) * a.rows + (int64_t)(b.t0 + tok) * a.group + h % a.group;
     u32x4 lo, hi;
     load_pairs<D, IL>(a.q + src * D, t0, lo, hi);
+    const float lse = a.lse[src];
+    const bool dead = lse == -INFINITY;  // a row that sees no key: zeros, whatever stands in it
+    if (dead) lo = hi = u32x4{};
     float yl[8], yh[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -61,7 +64,8 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(a.dout + src * D + 2 * t0 + 8 * k);
+      u32x4 x = *reinterpret_cast<const u32x4*>(a.dout + src * D + 2 * t0 + 8 * k);
+      if (dead) x = u32x4{};
       *reinterpret_cast<u32x4*>(a.ws_do + dst * D + 2 * t0 + 8 * k) = x;
       const u32x4 y = *reinterpret_cast<const u32x4*>(a.out + src * D + 2 * t0 + 8 * k);
 #pragma unroll
@@ -70,11 +74,9 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
 #pragma unroll
     for (int m = 1; m < TPR; m <<= 1) sum += __shfl_xor(sum, m, 64);
     if (t0 == 0) {
-      const float lse = a.lse[src];
       if (a.dlse) sum -= a.dlse[src];
-      // A row that sees no key: exp2(score - inf) = 0.
-      a.ws_info[dst] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
-      a.ws_info[a.hkv * a.rows + dst] = -sum;
+      a.ws_info[dst] = dead ? -INFINITY : -lse * 1.4426950408889634f;  // exp2(0 - inf) = 0
+      a.ws_info[a.hkv * a.rows + dst] = dead ? 0.f : -sum;
     }
   }
 }

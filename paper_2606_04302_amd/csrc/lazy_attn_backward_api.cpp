@@ -27,6 +27,9 @@ extern "C" int lazy_attn_prefill_backward(const lazy_attn_params_t* p, const voi
   const lazy::GradWorkLayout ws(p->num_q_heads, p->num_kv_heads, p->head_dim, *info);
   if (ws.bytes > 0 && (!workspace || workspace_bytes < ws.bytes || ((uintptr_t)workspace & 15u)))
     return LAZY_EWORKSPACE;
+  // The keys and values are read again after the first gradients are written.
+  if (info->num_tiles > 0 && (dk_pool == k_pool || dk_pool == v_pool || dv_pool == k_pool || dv_pool == v_pool))
+    return LAZY_EINVAL;
 
   const char* base = static_cast<const char*>(plan);
   char* work = static_cast<char*>(workspace);

@@ -8,7 +8,6 @@
 #include <algorithm>
 #include <functional>
 #include <map>
-#include <new>
 #include <tuple>
 #include <vector>
 
@@ -117,12 +116,14 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
   // A packed row is divided by G with a 32-bit multiplication in the kernels.
   if (total_q * G * G >= (int64_t)1 << 32 || total_q * G >= INT32_MAX) return LAZY_EUNSUPPORTED;
 
+  constexpr int64_t kMostOffset = (int64_t)1 << 56;  // sums of offsets and strides do not overflow
   // Slabs: records with the same strides, in storage order, joined where their keys overlap.
   std::vector<Use> uses;
   for (int r = 0; r < batch; ++r)
     for (int i = chunk_start[r]; i < chunk_start[r + 1]; ++i) {
       const lazy_chunk_t& c = chunks[i];
       if (c.len < 0 || c.k_stride < c.len || c.v_stride < c.len || c.k_offset < 0 || c.v_offset < 0 ||
+          c.k_offset > kMostOffset || c.v_offset > kMostOffset ||
           (c.k_offset & 7) || (c.v_offset & 7) || c.pos_offset < 0 || (int64_t)c.pos_offset + c.len > LAZY_MAX_POS)
         return LAZY_EDATA;
       if (c.len > 0) uses.push_back({r, i});
@@ -304,8 +305,10 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
   for (size_t i = 0; i < row_order.size(); ++i) row_order[i] = (int32_t)i;
   std::stable_sort(row_order.begin(), row_order.end(), [&](int32_t a, int32_t b) { return row_cost[a] > row_cost[b]; });
 
-  const size_t most = INT32_MAX;
-  if (out_tiles.size() * (size_t)hkv > most || out_segs.size() > most || rows.size() * (size_t)hkv > most)
+  // Launches of 256 threads a tile and a block, 512 a row item, and eight workgroups a merged tile.
+  const size_t most = (size_t)lazy::kMaxGroups - 64;
+  if (out_tiles.size() * (size_t)hkv > most || 2 * rows.size() * (size_t)hkv > most || out_segs.size() > INT32_MAX ||
+      blocks.size() + 8 * merges.size() * (size_t)hkv > most)
     return LAZY_EUNSUPPORTED;
   *info = {};
   info->batch = batch;
@@ -351,7 +354,7 @@ extern "C" int lazy_attn_backward_plan(const lazy_attn_params_t* params, const i
   if (chunk_start[batch] > 0 && !chunks) return LAZY_EINVAL;
   try {
     return make_plan(params, q_start, q_pos0, chunks, chunk_start, batch, plan, plan_capacity, info);
-  } catch (const std::bad_alloc&) {
+  } catch (...) {  // out of memory
     return LAZY_EINVAL;
   }
 }

@@ -11,6 +11,7 @@
 
 #include "lazy_attn_device.h"
 #include "lazy_attn_internal.h"
+#include "lazy_attn_params.h"
 #include "lazy_attn_tiles.h"
 
 namespace lazy {
@@ -80,6 +81,8 @@ __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks)
     const int64_t dst = (int64_t)(h / a.group) * a.rows + (int64_t)(first + tok) * a.group + h % a.group;
     u32x4 lo, hi;
     load_pairs<D, IL>(a.q + src * D, t0, lo, hi);
+    const float lse = a.lse[src];
+    if (lse == -INFINITY) lo = hi = u32x4{};  // a row that gives nothing, whatever stands in it: exp2(0 - inf) = 0
     if (a.rotate_k) {
       float yl[8], yh[8];
 #pragma unroll
@@ -97,10 +100,7 @@ __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks)
     }
     *reinterpret_cast<u32x4*>(a.ws_q + dst * D + t0) = lo;
     *reinterpret_cast<u32x4*>(a.ws_q + dst * D + D / 2 + t0) = hi;
-    if (t0 == 0) {
-      const float lse = a.lse[src];
-      a.ws_nlse[dst] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
-    }
+    if (t0 == 0) a.ws_nlse[dst] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
   }
 }
 
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
   const int steps = (nrows + kStepRows - 1) / kStepRows;
   const int row_begin = qs * a.group + (int)((int64_t)steps * rs / a.row_splits) * kStepRows;
   const int row_end = qs * a.group + min(nrows, (int)((int64_t)steps * (rs + 1) / a.row_splits) * kStepRows);
-  const int room = a.key_start[r + 1] - a.key_start[r];
+  const int room = min(a.key_start[r + 1], a.num_keys) - a.key_start[r];
   const double rev = ROT ? revolutions(a, lane % (D / 2)) : 0.0;
   const uint16_t* qbase = a.ws_q + (int64_t)g * a.rows * D;
   const int64_t second = a.hkv * a.rows * D;
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(256) void sum_weights(WeightArgs a) {
   n = wave_incl_scan(n);
   if ((tid & 63) == 63) total[tid >> 6] = n;
   __syncthreads();
-  n = min(total[0] + total[1] + total[2] + total[3], a.key_start[r + 1] - a.key_start[r]);
+  n = min(total[0] + total[1] + total[2] + total[3], min(a.key_start[r + 1], a.num_keys) - a.key_start[r]);
   for (int j = blockIdx.x * 256 + tid; j < n; j += gridDim.x * 256) {
     const int64_t at = (int64_t)a.key_start[r] + j;
     float w = 0.f;
@@ -461,8 +461,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
       for (int e = tid; e < ng * per_group * TPR; e += 256) {
         const int row = e / TPR, t0 = 8 * (e % TPR), grp = g0 + row / per_group;
         const int in = min((grp % per_head) * 16 + row % per_group, a.group - 1);
+        const int64_t src = (int64_t)r * a.hq + (grp / per_head) * a.group + in;
         u32x4 lo, hi;
-        load_pairs<D, IL>(a.q + ((int64_t)r * a.hq + (grp / per_head) * a.group + in) * D, t0, lo, hi);
+        load_pairs<D, IL>(a.q + src * D, t0, lo, hi);
+        if (a.lse[src] == -INFINITY) lo = hi = u32x4{};
         uint16_t* const to = q + row * QLD + t0;
         if (ROT) {
           float yl[8], yh[8];
@@ -901,14 +903,14 @@ __global__ __launch_bounds__(kSelectThreads) void select_slices(SelectArgs a) {
   __shared__ int before_s[2];
   const int r = blockIdx.y, w = blockIdx.x, tid = threadIdx.x;
   const int k0 = a.key_start[r], room = a.key_start[r + 1] - k0;
-  const int n = min(a.key_count ? max(0, min(a.key_count[r], room)) : room, a.slices * kSlice);
+  const int n = min(a.key_count ? max(0, min(a.key_count[r], room)) : room, (int)min((int64_t)a.slices * kSlice, (int64_t)INT32_MAX));
   const int o0 = a.kept_start[r], b = a.kept_start[r + 1] - o0;
   if (b >= n || b <= 0) {
     if (PASS == 3) trivial_selection(a, n, b, o0);
     return;
   }
   SliceWork* const all = reinterpret_cast<SliceWork*>(a.ws) + (int64_t)r * a.slices;
-  const int used = (n + kSlice - 1) / kSlice;
+  const int used = (n - 1) / kSlice + 1;
   if (w >= used) return;
   const int j0 = w * kSlice, count = min(kSlice, n - j0);
   const int filled = load_scores<PASS == 0>(sm, a.weights + k0, j0, count, n, a.sink, a.recent);
@@ -1008,7 +1010,8 @@ __global__ __launch_bounds__(256) void gather_keys(CompactArgs a) {
   }
   __syncthreads();
   if (a.weights_out && g == 0 && tid < kGather && i < count)
-    a.weights_out[o0 + i] = ksrc[tid] >= 0 ? a.weights[(int64_t)a.key_start[r] + asked] : 0.f;
+    a.weights_out[o0 + i] =
+        ksrc[tid] >= 0 && asked < a.key_start[r + 1] - a.key_start[r] ? a.weights[a.key_start[r] + asked] : 0.f;
   constexpr int TPR = D / 16;
   const int t0 = 8 * (tid % TPR);
   for (int row = tid / TPR; row < kGather; row += 256 / TPR) {
@@ -1040,7 +1043,7 @@ hipError_t prompt_mode(const WeightArgs& a, int max_kv_len, hipStream_t s) {
   const int blocks = (a.total_q + kPrepTokens - 1) / kPrepTokens;
   prepare_queries<D, interleaved_of(KMI)><<<blocks + kAngleBlocks<D>, 256, 0, s>>>(a, blocks);
   weigh_prompt<D, KMI><<<dim3(a.splits * a.row_splits, a.hkv, a.batch), 256, 0, s>>>(a);
-  sum_weights<<<dim3((max_kv_len + 255) / 256, a.batch), 256, 0, s>>>(a);
+  sum_weights<<<dim3(ceil_div(max_kv_len, 256), a.batch), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 template <int D, int KMI, bool FEW>
@@ -1060,19 +1063,23 @@ hipError_t token_mode(const WeightArgs& a, hipStream_t s) {
   return token_heads<D, KMI, false>(a, s);
 }
 
-template <int D, int TURN>
-void compact_mode(const CompactArgs& a, dim3 grid, bool local_keys, bool interleaved, hipStream_t s) {
-  if (local_keys) {
-    if (interleaved)
-      gather_keys<D, TURN, true, true><<<grid, 256, 0, s>>>(a);
-    else
-      gather_keys<D, TURN, true, false><<<grid, 256, 0, s>>>(a);
-  } else {
-    if (interleaved)
-      gather_keys<D, TURN, false, true><<<grid, 256, 0, s>>>(a);
-    else
-      gather_keys<D, TURN, false, false><<<grid, 256, 0, s>>>(a);
-  }
+template <int D, int TURN, bool LOCAL>
+void compact_mode(const CompactArgs& a, dim3 grid, bool interleaved, hipStream_t s) {
+  if (interleaved)
+    gather_keys<D, TURN, LOCAL, true><<<grid, 256, 0, s>>>(a);
+  else
+    gather_keys<D, TURN, LOCAL, false><<<grid, 256, 0, s>>>(a);
+}
+template <int D>
+void compact_dim(const CompactArgs& a, dim3 grid, int turn, bool local_keys, bool interleaved, hipStream_t s) {
+  if (turn == 0)
+    gather_keys<D, 0, false, false><<<grid, 256, 0, s>>>(a);
+  else if (turn == 2)
+    compact_mode<D, 2, true>(a, grid, interleaved, s);
+  else if (local_keys)
+    compact_mode<D, 1, true>(a, grid, interleaved, s);
+  else
+    compact_mode<D, 1, false>(a, grid, interleaved, s);
 }
 
 }  // namespace
@@ -1101,7 +1108,7 @@ hipError_t launch_decode_weights(const WeightArgs& a, int head_dim, bool local_k
 }
 
 size_t select_workspace(int batch, int max_kv_len) {
-  return max_kv_len <= kMostResident ? 0 : sizeof(SliceWork) * (size_t)batch * ((max_kv_len + kSlice - 1) / kSlice);
+  return max_kv_len <= kMostResident ? 0 : sizeof(SliceWork) * (size_t)batch * (size_t)ceil_div(max_kv_len, kSlice);
 }
 
 // The least instance that holds the longest request: LDS decides how many workgroups share a CU.
@@ -1115,7 +1122,7 @@ hipError_t launch_select(const float* weights, const int32_t* key_start, const i
   } else if (max_kv_len <= kMostResident) {
     select_request<kMostResident><<<one, kSelectThreads, 0, s>>>(a);
   } else {
-    a.slices = (max_kv_len + kSlice - 1) / kSlice;
+    a.slices = (int)ceil_div(max_kv_len, kSlice);
     const dim3 grid(a.slices, batch);
     select_slices<0><<<grid, kSelectThreads, 0, s>>>(a);
     select_slices<1><<<grid, kSelectThreads, 0, s>>>(a);
@@ -1127,23 +1134,11 @@ hipError_t launch_select(const float* weights, const int32_t* key_start, const i
 
 hipError_t launch_compact(const CompactArgs& a, int head_dim, int batch, int max_kept, int turn, bool local_keys,
                           bool interleaved, hipStream_t s) {
-  const dim3 grid((max_kept + kGather - 1) / kGather, a.hkv, batch);
-  if (turn == 0) {
-    if (head_dim == 64)
-      gather_keys<64, 0, false, false><<<grid, 256, 0, s>>>(a);
-    else
-      gather_keys<128, 0, false, false><<<grid, 256, 0, s>>>(a);
-  } else if (turn == 1) {
-    if (head_dim == 64)
-      compact_mode<64, 1>(a, grid, local_keys, interleaved, s);
-    else
-      compact_mode<128, 1>(a, grid, local_keys, interleaved, s);
-  } else {
-    if (head_dim == 64)
-      compact_mode<64, 2>(a, grid, true, interleaved, s);
-    else
-      compact_mode<128, 2>(a, grid, true, interleaved, s);
-  }
+  const dim3 grid(ceil_div(max_kept, kGather), a.hkv, batch);
+  if (head_dim == 64)
+    compact_dim<64>(a, grid, turn, local_keys, interleaved, s);
+  else
+    compact_dim<128>(a, grid, turn, local_keys, interleaved, s);
   return hipGetLastError();
 }
 

@@ -9,7 +9,7 @@
 
 namespace {
 
-using lazy::ceil_div, lazy::check_params, lazy::kNumCUs;
+using lazy::ceil_div, lazy::check_params, lazy::kMaxGroups, lazy::kNumCUs;
 
 constexpr int kTileKeys = 64;
 constexpr int64_t kSortBytes = 512 << 10;
@@ -81,7 +81,7 @@ int lazy_attn_prefill_key_weights(const lazy_attn_params_t* p, const void* q, co
   if (!q_start || !q_pos0 || !k_pool || !chunks || !chunk_start || !key_start || !weights) return LAZY_EINVAL;
   const int64_t g = p->num_q_heads / p->num_kv_heads;
   if ((int64_t)total_q * g * g >= (int64_t)1 << 32 || (int64_t)total_q * g >= INT32_MAX) return LAZY_EUNSUPPORTED;
-  if (batch > 65535 || p->num_kv_heads > 65535) return LAZY_EUNSUPPORTED;
+  if (batch > 65535 || p->num_kv_heads > 65535 || total_q > kMaxGroups) return LAZY_EUNSUPPORTED;
   const PromptSizes z = prompt_sizes(p, batch, total_q, max_q_len, max_kv_len, num_keys);
   if (!workspace || workspace_bytes < z.bytes || ((uintptr_t)workspace & 15u)) return LAZY_EWORKSPACE;
   char* ws = static_cast<char*>(workspace);
@@ -181,7 +181,7 @@ int lazy_cache_compact(const lazy_attn_params_t* p, const void* k_pool, const vo
   if (batch == 0 || max_kept == 0) return LAZY_OK;
   if (!k_pool || !v_pool || !chunks || !chunk_start || !kept || !kept_start || !dst || !k_out || !v_out)
     return LAZY_EINVAL;
-  if (batch > 65535 || p->num_kv_heads > 65535) return LAZY_EUNSUPPORTED;
+  if (batch > 65535 || p->num_kv_heads > 65535 || max_kept > kMaxGroups) return LAZY_EUNSUPPORTED;
   lazy::CompactArgs a = {};
   a.k_pool = static_cast<const uint16_t*>(k_pool);
   a.v_pool = static_cast<const uint16_t*>(v_pool);

@@ -10,6 +10,8 @@ namespace lazy {
 
 constexpr int kNumCUs = 256;  // MI355X compute units
 
+// Workgroups of one launch dimension: with 256 threads each, a launch holds fewer than 2^32.
+constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 1;
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline int check_params(const lazy_attn_params_t* p) {

@@ -5,6 +5,7 @@ in the HIP library.  There is no fallback: if the library is missing the first c
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -56,7 +57,6 @@ ITEM_DTYPE = np.dtype([("range_begin", "<i4"), ("num_ranges", "<i4"), ("range_ke
 USER_DTYPE = np.dtype([("request", "<i4"), ("pos_offset", "<i4"), ("slot", "<i4"), ("reserved", "<i4")])
 assert RANGE_DTYPE.itemsize == 32 and ITEM_DTYPE.itemsize == 24 and USER_DTYPE.itemsize == 16
 SHARED_MAX_RANGES = 64  # LAZY_SHARED_MAX_RANGES
-
 
 
 class BackwardInfo(ctypes.Structure):
@@ -227,12 +227,23 @@ def decode_workspace_size(cfg: Config, batch: int, max_kv_len: int) -> int:
     return int(lib().lazy_attn_decode_workspace_size(ctypes.byref(p), batch, max_kv_len))
 
 
-def _workspace(nbytes, device, workspace):
+def _workspace(nbytes, device, workspace, stream=None):
     if nbytes == 0:
         return None
     if workspace is None or workspace.numel() < nbytes:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        with _allocating_for(stream):
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
     return workspace
+
+
+def _allocating_for(stream):
+    """Memory that work on ``stream`` is the first and last to use comes from that stream's pool: it is neither filled
+    by, nor handed on to, the current stream while that work is under way."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(stream)
+    return torch.cuda.stream(stream)
 
 
 def prefill(cfg: Config, q, q_start, q_pos0, k_pool, v_pool, chunks, chunk_start, max_q_len: int, max_kv_len: int,
@@ -413,19 +424,20 @@ def prefill_backward(cfg: Config, q, q_start, q_pos0, k_pool, v_pool, chunks, ch
     _need(isinstance(plan.data, torch.Tensor), "the plan must be on the device (upload_backward_plan)")
     _dev(plan.data, torch.uint8, "plan")
     _need(plan.data.numel() == plan.info.plan_bytes, "the plan's array does not belong to its record")
-    if dq is None:
-        dq = torch.empty_like(q)
-    if dk_pool is None:
-        dk_pool = torch.zeros_like(k_pool)
-        if dv_pool is None and v_pool.data_ptr() == k_pool.data_ptr() and v_pool.shape == k_pool.shape:
-            dv_pool = dk_pool
-    if dv_pool is None:
-        dv_pool = torch.zeros_like(v_pool)
+    with _allocating_for(stream):
+        if dq is None:
+            dq = torch.empty_like(q)
+        if dk_pool is None:
+            dk_pool = torch.zeros_like(k_pool)
+            if dv_pool is None and v_pool.data_ptr() == k_pool.data_ptr() and v_pool.shape == k_pool.shape:
+                dv_pool = dk_pool
+        if dv_pool is None:
+            dv_pool = torch.zeros_like(v_pool)
     for t, like, name in ((dq, q, "dq"), (dk_pool, k_pool, "dk_pool"), (dv_pool, v_pool, "dv_pool")):
         _dev(t, torch.bfloat16, name)
         _need(t.shape == like.shape, f"{name} must have the shape of what it is the gradient of")
     nbytes = backward_workspace_size(cfg, plan)
-    workspace = _workspace(nbytes, q.device, workspace)
+    workspace = _workspace(nbytes, q.device, workspace, stream)
     p = cfg.c()
     _check(lib().lazy_attn_prefill_backward(
         ctypes.byref(p), q.data_ptr(), q_start.data_ptr(), q_pos0.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
@@ -474,7 +486,7 @@ def prefill_key_weights(cfg: Config, q, q_start, q_pos0, k_pool, chunks, chunk_s
     _dev(q_start, torch.int32, "q_start")
     _weight_args(cfg, q, q_pos0, k_pool, chunks, chunk_start, key_start, batch, lse, weights, weights_in)
     nbytes = prefill_key_weights_workspace_size(cfg, batch, q.shape[0], max_q_len, max_kv_len, weights.numel())
-    workspace = _workspace(nbytes, q.device, workspace)
+    workspace = _workspace(nbytes, q.device, workspace, stream)
     p = cfg.c()
     _check(lib().lazy_attn_prefill_key_weights(
         ctypes.byref(p), q.data_ptr(), q_start.data_ptr(), q_pos0.data_ptr(), k_pool.data_ptr(), chunks.data_ptr(),
@@ -490,7 +502,7 @@ def decode_key_weights(cfg: Config, q, q_pos, k_pool, chunks, chunk_start, key_s
     batch = q.shape[0]
     _weight_args(cfg, q, q_pos, k_pool, chunks, chunk_start, key_start, batch, lse, weights, weights_in)
     nbytes = decode_key_weights_workspace_size(cfg, batch, max_kv_len)
-    workspace = _workspace(nbytes, q.device, workspace)
+    workspace = _workspace(nbytes, q.device, workspace, stream)
     p = cfg.c()
     _check(lib().lazy_attn_decode_key_weights(
         ctypes.byref(p), q.data_ptr(), q_pos.data_ptr(), k_pool.data_ptr(), chunks.data_ptr(), chunk_start.data_ptr(),
@@ -517,8 +529,10 @@ def cache_select(weights, key_start, kept_start, max_kv_len: int, kept, sink: in
     if key_count is not None:
         _dev(key_count, torch.int32, "key_count")
         _need(key_count.numel() == batch, "table sizes disagree with the batch")
+    if kept.numel() == 0:
+        return kept
     nbytes = cache_select_workspace_size(batch, max_kv_len)
-    workspace = _workspace(nbytes, weights.device, workspace)
+    workspace = _workspace(nbytes, weights.device, workspace, stream)
     _check(lib().lazy_cache_select(weights.data_ptr(), key_start.data_ptr(), _ptr(key_count), kept_start.data_ptr(),
                                    batch, max_kv_len, sink, recent, kept.data_ptr(), _ptr(workspace), nbytes,
                                    _stream(stream)), "lazy_cache_select")
@@ -544,6 +558,8 @@ def cache_compact(cfg: Config, k_pool, v_pool, chunks, chunk_start, kept, kept_s
         if t is not None:
             _dev(t, torch.float32, name)
     _need(weights_out is None or weights_out.numel() >= kept.numel(), "weights_out must have an entry a kept key")
+    if kept.numel() == 0:
+        return k_out, v_out
     p = cfg.c()
     _check(lib().lazy_cache_compact(
         ctypes.byref(p), k_pool.data_ptr(), v_pool.data_ptr(), chunks.data_ptr(), chunk_start.data_ptr(), batch,

@@ -454,3 +454,67 @@ def test_backward_in_a_graph_and_on_another_stream(gpu):
         torch.cuda.synchronize()
         assert same()
         torch.mm(torch.ones(64, 64, device="cuda"), torch.ones(64, 64, device="cuda"))
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# Calls at the edges
+# ---------------------------------------------------------------------------------------------------------------
+def test_refusals_of_plans_and_pools_without_a_gpu():
+    """More work items than a launch holds, offsets whose sums would overflow, gradients over what they are made from."""
+    heads = 60000
+    cfg = ops.Config(heads, heads, 64, 1e4)
+    with pytest.raises(ops.LazyAttnError) as e:
+        ops.backward_plan(cfg, np.arange(151, dtype=np.int32), np.zeros(150, np.int32), np.zeros(0, W.CHUNK_DTYPE),
+                          np.zeros(151, np.int32))
+    assert e.value.code == ops.LAZY_EUNSUPPORTED
+    w = W.tiny_rag_prefill(0)
+    cfg, plan = make_plan(w)
+    for field in ("k_offset", "v_offset"):
+        c = w.chunks.copy()
+        c[0][field] = (1 << 63) - 8
+        with pytest.raises(ops.LazyAttnError) as e:
+            ops.backward_plan(cfg, w.q_start, w.q_pos0, c, w.chunk_start)
+        assert e.value.code == ops.LAZY_EDATA
+    p, one = cfg.c(), 4096  # addresses that are never read
+    for k, v, dk, dv in ((1, 2, 1, 3), (1, 2, 2, 3), (1, 2, 3, 1), (1, 2, 3, 2), (1, 1, 1, 1)):
+        assert ops.lib().lazy_attn_prefill_backward(
+            ctypes.byref(p), one, one, one, k * one, v * one, one, one, w.batch, w.total_q, one, one, one, None, one,
+            ctypes.byref(plan.info), one, dk * one, dv * one, one, 1 << 40, None) == ops.LAZY_EINVAL
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,style", [(64, ops.ROPE_HALF), (128, ops.ROPE_INTERLEAVED), (128, ops.ALIBI)])
+def test_rows_that_see_nothing_may_hold_anything(gpu, d, style):
+    """Queries, outputs and their gradients of rows with a log-sum-exp of -inf are not finite: no other gradient changes,
+    and theirs is zero."""
+    w = W.custom(44, 4, 2, d, 1e4, [dict(chunks=[("a", 100, 37)], q_len=90, q_pos0=3),
+                                    dict(chunks=[("a", 100, 0), ("b", 65, 100)], q_len=40, q_pos0=20)])
+    args, dl, want = run(w, dict(rope_style=style), dlse=True)[:3]
+    cfg, q, q_start, q_pos0, kp, vp, chunks, chunk_start, out, lse, dout, plan = args
+    dead = torch.isneginf(lse)
+    assert dead.any() and not dead.all()
+    q, out, dout, dl = q.clone(), out.clone(), dout.clone(), dl.clone()
+    q[dead], out[dead], dout[dead], dl[dead] = float("nan"), float("inf"), float("nan"), float("inf")
+    got = [torch.full_like(t, 3.0) for t in want]
+    ops.prefill_backward(cfg, q, q_start, q_pos0, kp, vp, chunks, chunk_start, out, lse, dout, plan, dlse=dl, dq=got[0],
+                         dk_pool=got[1], dv_pool=got[2])
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert not got[0][dead].any()
+
+
+@pytest.mark.gpu
+def test_memory_allocated_for_another_stream(gpu):
+    """Gradients and workspace that the call allocates belong to the stream it runs on."""
+    w = shared(45, 8, 2, 128, [130, 64, 33], [17, 40, 3], slack=None)
+    args, _, want = run(w, {})[:3]
+    ck, cv = (torch.from_numpy(m).cuda() for m in cover_masks(w))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        dq, dk, dv = ops.prefill_backward(*args, stream=stream)
+        side.synchronize()
+        assert torch.equal(dq, want[0])
+        assert torch.equal(dk.reshape(-1)[ck], want[1].reshape(-1)[ck])
+        assert torch.equal(dv.reshape(-1)[cv], want[2].reshape(-1)[cv])
+        assert not dk.reshape(-1)[~(ck | cv)].any()

@@ -537,3 +537,109 @@ def test_eviction_in_a_graph(gpu):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(bufs, want))
         torch.mm(torch.ones(64, 64, device="cuda"), torch.ones(64, 64, device="cuda"))
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# Calls at the edges
+# ---------------------------------------------------------------------------------------------------------------
+def test_largest_bounds_without_a_gpu():
+    """Bounds near 2^31: sizes do not wrap, and what no launch holds is refused."""
+    most, one = (1 << 31) - 1, 4096
+    slices = -(-most // 16384)
+    assert ops.cache_select_workspace_size(1, most) >= slices * 3 * 2048 * 4
+    assert ops.cache_select_workspace_size(3, most) == 3 * ops.cache_select_workspace_size(1, most)
+    p = ops.Config(1, 1, 64, 1e4).c()
+    assert ops.lib().lazy_cache_compact(ctypes.byref(p), one, one, one, one, 1, one, one, most, one, 0, one, one, None,
+                                        None, None, None) == ops.LAZY_EUNSUPPORTED
+    assert ops.lib().lazy_attn_prefill_key_weights(
+        ctypes.byref(p), one, one, one, one, one, one, one, 1, most - 1, 4, 4, 4, one, None, 1.0, one, one, 1 << 50,
+        None) == ops.LAZY_EUNSUPPORTED
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,style", [(4, 2, 64, ops.ROPE_HALF), (12, 1, 128, ops.ROPE_INTERLEAVED),
+                                            (8, 2, 128, ops.ALIBI)])
+def test_rows_that_are_left_out_may_hold_anything(gpu, hq, hkv, d, style):
+    """Rows whose log-sum-exp is -inf give nothing, whatever their queries hold."""
+    w = W.custom(92, hq, hkv, d, 1e4, [dict(chunks=[("a", 100, 0), (30, 100)], q_len=30, q_pos0=100),
+                                       dict(chunks=[("a", 100, 7)], q_len=9, q_pos0=110)])
+    cfg, dw = ops.config_of(w, rope_style=style), ops.upload(w)
+    _, lse = ops.run_lazy(dw, cfg)
+    lse[5:11] = -math.inf
+    lse[:, hq // 2] = -math.inf
+    dead, ks = torch.isneginf(lse), i32(starts(w.kv_lens))
+    out = []
+    for fill in (0.0, math.nan, math.inf):
+        q = dw.q.clone()
+        q[dead] = fill
+        a = torch.empty(int(w.kv_lens.sum()), device="cuda")
+        ops.prefill_key_weights(cfg, q, dw.q_start, dw.q_pos0, dw.pool, dw.chunks, dw.chunk_start, ks, w.max_q_len,
+                                w.max_kv_len, lse, a)
+        b = torch.empty_like(a)
+        rows = [7, 38]
+        ops.decode_key_weights(cfg, q[rows].contiguous(), i32([107, 118]), dw.pool, dw.chunks, dw.chunk_start, ks,
+                               w.max_kv_len, lse[rows].contiguous(), b)
+        out.append((a, b))
+    assert torch.isfinite(out[0][0]).all() and out[0][0].any()
+    assert not out[0][1][:130].any() and out[0][1][130:].any()
+    for a, b in out[1:]:
+        assert torch.equal(a, out[0][0]) and torch.equal(b, out[0][1])
+
+
+@pytest.mark.gpu
+def test_kept_keys_without_room_have_no_weight(gpu):
+    w = shared(93, 4, 2, 64, [100], [4], reqs=2)
+    cfg, dw = ops.config_of(w), ops.upload(w)
+    n, room, cap = int(w.kv_lens[0]), 50, 8
+    kept = np.array([0, 20, 49, 50, 60, n - 1] * 2)
+    ks, os = starts([room, room]), starts([6, 6])
+    weights = torch.arange(1, 2 * room + 1, device="cuda", dtype=torch.float32)
+    per = cap * w.num_kv_heads * w.head_dim
+    dst = np.array([(2 * r * per, (2 * r + 1) * per, 6, 0, cap, cap) for r in range(2)], dtype=W.CHUNK_DTYPE)
+    store = torch.zeros(4 * per, dtype=torch.bfloat16, device="cuda")
+    wo = torch.full((12,), -7.0, device="cuda")
+    ops.cache_compact(cfg, dw.pool, dw.pool, dw.chunks, dw.chunk_start, i32(kept), i32(os), 6,
+                      torch.from_numpy(dst.view(np.uint8).copy()).cuda(), store, store, key_start=i32(ks),
+                      weights=weights, weights_out=wo)
+    assert wo.tolist() == [1, 21, 50, 0, 0, 0, 51, 71, 100, 0, 0, 0]
+
+
+@pytest.mark.gpu
+def test_nothing_is_kept(gpu):
+    w = shared(94, 4, 2, 64, [100], [4], reqs=2)
+    cfg, dw = ops.config_of(w), ops.upload(w)
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    weights = torch.rand(int(w.kv_lens.sum()), device="cuda")
+    assert ops.cache_select(weights, i32(starts(w.kv_lens)), i32([0, 0, 0]), w.max_kv_len, none) is none
+    store = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    ops.cache_compact(cfg, dw.pool, dw.pool, dw.chunks, dw.chunk_start, none, i32([0, 0, 0]), 5,
+                      torch.zeros(64, dtype=torch.uint8, device="cuda"), store, store)
+    assert (store == 1).all()
+
+
+@pytest.mark.gpu
+def test_selection_of_a_long_request_in_a_graph(gpu):
+    n, budget = [40000, 17, 70001], [5000, 4, 70000]
+    gen = torch.Generator("cuda").manual_seed(3)
+    weights = torch.empty(sum(n), device="cuda")
+    ks, os = i32(starts(n)), i32(starts(budget))
+    kept = torch.empty(sum(budget), dtype=torch.int32, device="cuda")
+    ws = torch.empty(ops.cache_select_workspace_size(3, max(n)), dtype=torch.uint8, device="cuda")
+    weights.uniform_(generator=gen)
+
+    def call():
+        ops.cache_select(weights, ks, os, max(n), kept, sink=3, recent=7, workspace=ws)
+
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for step in range(4):
+        weights.uniform_(generator=gen)
+        ws.fill_(171 + step)
+        graph.replay()
+        torch.cuda.synchronize()
+        host, at, to = weights.cpu().numpy(), 0, 0
+        for k, b in zip(n, budget):
+            assert kept[to:to + b].tolist() == E.select(host[at:at + k], b, 3, 7)
+            at, to = at + k, to + b
