@@ -1,6 +1,6 @@
 // Backward pass of the prefill attention for gfx950: gradients of the queries and of the stored keys and values.
 //
-// Four launches.  (1) prepare_rows: queries rotated to their positions, times scale * log2 e, in bf16 and packed by KV
+// Four launches, three where there is little work (grads_together).  (1) prepare_rows: queries rotated to their positions, times scale * log2 e, in bf16 and packed by KV
 // head (row = token * G + head in group), dO packed alike, and two numbers a row, -lse log2 e and -delta.  (2) grad_kv: dk
 // and dv, one tile of the store at a time.  (3) grad_q: partial dq, one row tile and key split at a time.  (4) finish:
 // partial dq summed, turned back and rounded, and the same for tiles whose uses were cut into parts.
@@ -88,8 +88,8 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
 // read by rows for the first two products and transposed for the last two; the next 32 are copied to the other buffer
 // during the products.  -lse and -delta are the accumulators' initial values.  dK is kept in the rotated frame of the use
 // at hand and turned on when the next use has another position.
-template <int D, int KMI, int WPE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE, WPE))) void grad_kv(GradArgs a) {
+template <int D, int KMI>
+__device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
   constexpr int C = D / 8;  // chunks of a row
@@ -105,9 +105,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
   __shared__ int rpos_all[4][kGradRows] __attribute__((aligned(16)));
   __shared__ float rslope_all[4][kGradRows] __attribute__((aligned(16)));
   __shared__ float2 turn_all[4][D / 2] __attribute__((aligned(16)));
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h2 = lane >> 5, g = blockIdx.x % a.hkv;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h2 = lane >> 5, g = id % a.hkv;
   const int hf = wave >> 1, k32 = 32 * (wave & 1), key = k32 + (lane & 31);
-  const GradTile* const tile = a.tiles + blockIdx.x / a.hkv;
+  const GradTile* const tile = a.tiles + id / a.hkv;
   const GradHalf t = tile->half[hf];
   const int seg_begin = tile->seg_begin, seg_end = tile->seg_end, part = tile->part;
   const bool active = k32 < t.keys;  // a wave without keys only helps to copy
@@ -376,6 +376,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
     wait_copies();
   }
 }
+template <int D, int KMI, int WPE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE, WPE))) void grad_kv(GradArgs a) {
+  key_gradients<D, KMI>(a, blockIdx.x);
+}
 
 // Loads a 64-key tile of K and V for a workgroup of NT threads, NT / 64 a key row, rotates the keys and writes both to
 // LDS (unpadded tiles, pairs in half-split order).  The angles of the 32 rows are read from LDS for every tile: kept in
@@ -519,13 +523,13 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
 // Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q and dO in
 // registers; K (rotated) and V pass through LDS, K read by rows and transposed.
 template <int D, int KMI, int NW, int NBUF>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_q(GradArgs a) {
+__device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
   constexpr int KM = keys_of(KMI), NT = NW * 64;
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal;
   using S = TileLayout<D>;
   __shared__ GradQSmem<D, NBUF> sm;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), h2 = lane >> 5, g = blockIdx.x % a.hkv;
-  const GradRowItem item = a.row_items[blockIdx.x / a.hkv];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), h2 = lane >> 5, g = id % a.hkv;
+  const GradRowItem item = a.row_items[id / a.hkv];
   const int r = item.request;
   const int qs = a.q_start[r], nrows = (a.q_start[r + 1] - qs) * a.group, shift = a.q_pos0[r] - qs;
   const int pr = item.row0 + 32 * wave + (lane & 31);
@@ -624,6 +628,18 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       *reinterpret_cast<f32x4*>(out + 32 * db + 8 * q4 + 4 * h2) =
           f32x4{dq[db][4 * q4], dq[db][4 * q4 + 1], dq[db][4 * q4 + 2], dq[db][4 * q4 + 3]};
 }
+template <int D, int KMI, int NW, int NBUF>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_q(GradArgs a) {
+  query_gradients<D, KMI, NW, NBUF>(a, blockIdx.x);
+}
+// Both in one launch, the first `tiles` workgroups for keys and values.
+template <int D, int KMI>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, D == 64 ? 2 : 1))) void grad_all(GradArgs a, int tiles) {
+  if ((int)blockIdx.x < tiles)
+    key_gradients<D, KMI>(a, blockIdx.x);
+  else
+    query_gradients<D, KMI, 4, 1>(a, blockIdx.x - tiles);
+}
 
 // Keys of a tile's parts that a workgroup sums, and workgroups a (tile, KV head).
 constexpr int kMergeRows = 32, kMergeBlocks = 2 * kGradHalves * kGradTileKeys / kMergeRows;
@@ -702,15 +718,18 @@ template <int D, int KMI>
 hipError_t launch(const GradArgs& a, const lazy_backward_info_t& i, hipStream_t stream) {
   constexpr bool IL = interleaved_of(KMI);
   prepare_rows<D, IL><<<i.num_blocks + kAngleBlocks<D>, 256, 0, stream>>>(a, i.num_blocks);
-  if (i.num_tiles) grad_kv<D, KMI, D == 64 ? 3 : 2><<<i.num_tiles * a.hkv, 256, 0, stream>>>(a);
-  if (i.num_row_items) {
+  const int tiles = i.num_tiles * a.hkv, items = i.num_row_items * a.hkv;
+  const bool together = i.row_blocks == 1 && grads_together(D, tiles, items);
+  if (together) grad_all<D, KMI><<<tiles + items, 256, 0, stream>>>(a, tiles);
+  if (tiles && !together) grad_kv<D, KMI, D == 64 ? 3 : 2><<<tiles, 256, 0, stream>>>(a);
+  if (items && !together) {
     if constexpr (D == 128) {
       if (i.row_blocks == 2)
-        grad_q<D, KMI, 8, 2><<<i.num_row_items * a.hkv, 512, 0, stream>>>(a);
+        grad_q<D, KMI, 8, 2><<<items, 512, 0, stream>>>(a);
       else
-        grad_q<D, KMI, 4, 1><<<i.num_row_items * a.hkv, 256, 0, stream>>>(a);
+        grad_q<D, KMI, 4, 1><<<items, 256, 0, stream>>>(a);
     } else {
-      grad_q<D, KMI, 4, 2><<<i.num_row_items * a.hkv, 256, 0, stream>>>(a);
+      grad_q<D, KMI, 4, 2><<<items, 256, 0, stream>>>(a);
     }
   }
   const int merges = i.num_merges * a.hkv * kMergeBlocks;

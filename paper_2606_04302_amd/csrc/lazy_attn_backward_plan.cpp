@@ -281,8 +281,19 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
     for (int i = chunk_start[r]; i < chunk_start[r + 1]; ++i)
       key_tiles[r] += lazy::ceil_div(chunks[i].len, kGradTileKeys);
   }
-  const int row_blocks = d == 128 && 4 * rows2 <= 5 * rows1 ? 2 : 1, bm = 128 * row_blocks;
-  const std::vector<int32_t> splits_of = row_splits(key_tiles, q_start, batch, G, hkv, d, row_blocks);
+  int row_blocks = d == 128 && 4 * rows2 <= 5 * rows1 ? 2 : 1;
+  std::vector<int32_t> splits_of = row_splits(key_tiles, q_start, batch, G, hkv, d, row_blocks);
+  if (row_blocks == 2) {  // little work: 128 rows too, so that one launch takes both kinds of items
+    const std::vector<int32_t> other = row_splits(key_tiles, q_start, batch, G, hkv, d, 1);
+    int64_t items = 0;
+    for (int r = 0; r < batch; ++r)
+      items += lazy::ceil_div((int64_t)(q_start[r + 1] - q_start[r]) * G, 128) * other[r];
+    if (lazy::grads_together(d, (int64_t)out_tiles.size() * hkv, items * hkv)) {
+      row_blocks = 1;
+      splits_of = other;
+    }
+  }
+  const int bm = 128 * row_blocks;
   std::vector<GradRowItem> rows;
   std::vector<GradBlock> blocks;
   std::vector<int64_t> row_cost;

@@ -518,3 +518,32 @@ def test_memory_allocated_for_another_stream(gpu):
         assert torch.equal(dk.reshape(-1)[ck], want[1].reshape(-1)[ck])
         assert torch.equal(dv.reshape(-1)[cv], want[2].reshape(-1)[cv])
         assert not dk.reshape(-1)[~(ck | cv)].any()
+
+
+# Work beyond what one launch takes for all three gradients: 128-row and 256-row items of head_dim 128, and head_dim 64.
+LARGE = {
+    "d128, 128 rows": (lambda: shared(46, 32, 32, 128, [1030, 700, 517], [20, 33], reqs=2), {}),
+    "d128, 128 rows, interleaved local": (lambda: shared(47, 32, 32, 128, [1030, 700, 517], [20, 33], reqs=2),
+                                          dict(rope_style=ops.ROPE_INTERLEAVED, key_positions=ops.KEYS_LOCAL)),
+    "d128, 128 rows, alibi": (lambda: shared(48, 32, 32, 128, [1030, 700, 517], [20, 33], reqs=2),
+                              dict(rope_style=ops.ALIBI)),
+    "d128, 256 rows": (lambda: shared(49, 64, 16, 128, [1030, 700, 517, 2000], [128, 60], reqs=2), {}),
+    "d128, 256 rows, interleaved": (lambda: shared(50, 64, 16, 128, [1030, 700, 517, 2000], [128, 60], reqs=2),
+                                    dict(rope_style=ops.ROPE_INTERLEAVED)),
+    "d64": (lambda: shared(51, 64, 64, 64, [1030, 700, 517, 500], [20, 33], reqs=2), {}),
+    "d64, interleaved local": (lambda: shared(52, 64, 64, 64, [1030, 700, 517, 500], [20, 33], reqs=2),
+                               dict(rope_style=ops.ROPE_INTERLEAVED, key_positions=ops.KEYS_LOCAL)),
+    "d64, alibi": (lambda: shared(53, 64, 64, 64, [1030, 700, 517, 500], [20, 33], reqs=2), dict(rope_style=ops.ALIBI)),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", LARGE)
+def test_gradients_in_separate_launches(gpu, name):
+    make, ckw = LARGE[name]
+    w = make()
+    info = make_plan(w, **ckw)[1].info
+    tiles, items = info.num_tiles * w.num_kv_heads, info.num_row_items * w.num_kv_heads
+    assert tiles > 1280 if w.head_dim == 64 else tiles + items > 512
+    assert info.row_blocks == (2 if "256 rows" in name else 1)
+    check(w, ckw, name)
