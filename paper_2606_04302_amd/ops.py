@@ -192,7 +192,8 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        # The pointer alone: torch.cuda.current_stream() builds an object around it, 2 us a call.
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
@@ -414,35 +415,38 @@ def prefill_backward(cfg: Config, q, q_start, q_pos0, k_pool, v_pool, chunks, ch
     _chunks(chunks)
     _need(q.dim() == 3 and q.shape[1] == cfg.num_q_heads and q.shape[2] == cfg.head_dim, "q must be [T, Hq, D]")
     _need(out.shape == q.shape and dout.shape == q.shape, "out and dout must have the shape of q")
-    for t, name in ((lse, "lse"), (dlse, "dlse")):
-        if t is None and name == "dlse":
-            continue
-        _dev(t, torch.float32, name)
-        _need(t.shape == q.shape[:2], f"{name} must be [T, Hq]")
+    _dev(lse, torch.float32, "lse")
+    _need(lse.shape == q.shape[:2], "lse must be [T, Hq]")
+    if dlse is not None:
+        _dev(dlse, torch.float32, "dlse")
+        _need(dlse.shape == lse.shape, "dlse must be [T, Hq]")
     batch = q_start.numel() - 1
     _need(chunk_start.numel() == batch + 1 and q_pos0.numel() == batch, "table sizes disagree with the batch")
     _need(isinstance(plan.data, torch.Tensor), "the plan must be on the device (upload_backward_plan)")
     _dev(plan.data, torch.uint8, "plan")
     _need(plan.data.numel() == plan.info.plan_bytes, "the plan's array does not belong to its record")
-    with _allocating_for(stream):
-        if dq is None:
-            dq = torch.empty_like(q)
-        if dk_pool is None:
-            dk_pool = torch.zeros_like(k_pool)
-            if dv_pool is None and v_pool.data_ptr() == k_pool.data_ptr() and v_pool.shape == k_pool.shape:
-                dv_pool = dk_pool
-        if dv_pool is None:
-            dv_pool = torch.zeros_like(v_pool)
+    if dq is None or dk_pool is None or dv_pool is None:
+        with _allocating_for(stream):
+            if dq is None:
+                dq = torch.empty_like(q)
+            if dk_pool is None:
+                dk_pool = torch.zeros_like(k_pool)
+                if dv_pool is None and v_pool.data_ptr() == k_pool.data_ptr() and v_pool.shape == k_pool.shape:
+                    dv_pool = dk_pool
+            if dv_pool is None:
+                dv_pool = torch.zeros_like(v_pool)
     for t, like, name in ((dq, q, "dq"), (dk_pool, k_pool, "dk_pool"), (dv_pool, v_pool, "dv_pool")):
         _dev(t, torch.bfloat16, name)
-        _need(t.shape == like.shape, f"{name} must have the shape of what it is the gradient of")
-    nbytes = backward_workspace_size(cfg, plan)
-    workspace = _workspace(nbytes, q.device, workspace, stream)
+        if t.shape != like.shape:
+            raise ValueError(f"{name} must have the shape of what it is the gradient of")
     p = cfg.c()
+    p, info = ctypes.byref(p), ctypes.byref(plan.info)
+    nbytes = lib().lazy_attn_backward_workspace_size(p, info)
+    workspace = _workspace(nbytes, q.device, workspace, stream)
     _check(lib().lazy_attn_prefill_backward(
-        ctypes.byref(p), q.data_ptr(), q_start.data_ptr(), q_pos0.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+        p, q.data_ptr(), q_start.data_ptr(), q_pos0.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
         chunks.data_ptr(), chunk_start.data_ptr(), batch, q.shape[0], out.data_ptr(), lse.data_ptr(), dout.data_ptr(),
-        _ptr(dlse), plan.data.data_ptr(), ctypes.byref(plan.info), dq.data_ptr(), dk_pool.data_ptr(),
+        _ptr(dlse), plan.data.data_ptr(), info, dq.data_ptr(), dk_pool.data_ptr(),
         dv_pool.data_ptr(), _ptr(workspace), nbytes, _stream(stream)), "lazy_attn_prefill_backward")
     return dq, dk_pool, dv_pool
 
@@ -485,11 +489,13 @@ def prefill_key_weights(cfg: Config, q, q_start, q_pos0, k_pool, chunks, chunk_s
     batch = q_start.numel() - 1
     _dev(q_start, torch.int32, "q_start")
     _weight_args(cfg, q, q_pos0, k_pool, chunks, chunk_start, key_start, batch, lse, weights, weights_in)
-    nbytes = prefill_key_weights_workspace_size(cfg, batch, q.shape[0], max_q_len, max_kv_len, weights.numel())
-    workspace = _workspace(nbytes, q.device, workspace, stream)
     p = cfg.c()
+    p = ctypes.byref(p)
+    nbytes = lib().lazy_attn_prefill_key_weights_workspace_size(p, batch, q.shape[0], max_q_len, max_kv_len,
+                                                                weights.numel())
+    workspace = _workspace(nbytes, q.device, workspace, stream)
     _check(lib().lazy_attn_prefill_key_weights(
-        ctypes.byref(p), q.data_ptr(), q_start.data_ptr(), q_pos0.data_ptr(), k_pool.data_ptr(), chunks.data_ptr(),
+        p, q.data_ptr(), q_start.data_ptr(), q_pos0.data_ptr(), k_pool.data_ptr(), chunks.data_ptr(),
         chunk_start.data_ptr(), key_start.data_ptr(), batch, q.shape[0], max_q_len, max_kv_len, weights.numel(),
         lse.data_ptr(), _ptr(weights_in), float(decay), weights.data_ptr(), _ptr(workspace), nbytes, _stream(stream)),
         "lazy_attn_prefill_key_weights")
@@ -501,11 +507,12 @@ def decode_key_weights(cfg: Config, q, q_pos, k_pool, chunks, chunk_start, key_s
     """lazy_attn_decode_key_weights: the weights that one new token per request gives, as prefill_key_weights."""
     batch = q.shape[0]
     _weight_args(cfg, q, q_pos, k_pool, chunks, chunk_start, key_start, batch, lse, weights, weights_in)
-    nbytes = decode_key_weights_workspace_size(cfg, batch, max_kv_len)
-    workspace = _workspace(nbytes, q.device, workspace, stream)
     p = cfg.c()
+    p = ctypes.byref(p)
+    nbytes = lib().lazy_attn_decode_key_weights_workspace_size(p, batch, max_kv_len)
+    workspace = _workspace(nbytes, q.device, workspace, stream)
     _check(lib().lazy_attn_decode_key_weights(
-        ctypes.byref(p), q.data_ptr(), q_pos.data_ptr(), k_pool.data_ptr(), chunks.data_ptr(), chunk_start.data_ptr(),
+        p, q.data_ptr(), q_pos.data_ptr(), k_pool.data_ptr(), chunks.data_ptr(), chunk_start.data_ptr(),
         key_start.data_ptr(), batch, max_kv_len, lse.data_ptr(), _ptr(weights_in), float(decay), weights.data_ptr(),
         _ptr(workspace), nbytes, _stream(stream)), "lazy_attn_decode_key_weights")
     return weights
