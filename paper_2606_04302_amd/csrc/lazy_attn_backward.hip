@@ -26,7 +26,8 @@ namespace {
 constexpr int kMaxBlockTokens = 16;
 
 // Queries rotated, scaled and packed by KV head; row constants.  One workgroup a block of tokens, D / 16 threads a row;
-// workgroups past the last block write the table of angles.
+// workgroups past the last block write the table of angles.  Bound by memory: 5350 tokens of 32 heads of 64 19 us for 110
+// MB (5.8 TB/s, part of it from the caches).
 template <int D, bool IL>
 __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
   __shared__ float2 cs[kMaxBlockTokens][D / 2];
@@ -88,6 +89,11 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
 // read by rows for the first two products and transposed for the last two; the next 32 are copied to the other buffer
 // during the products.  -lse and -delta are the accumulators' initial values.  dK is kept in the rotated frame of the use
 // at hand and turned on when the next use has another position.
+//
+// Two waves a SIMD (three at D = 64) hide each other's latencies.  Bound by the products and by what stands between them in a wave
+// (exponentials, masks, conversions).  16 ragged requests, 1.23 TFLOP of five products: 1.17 ms for four (840 TFLOP/s,
+// 69% of the large library product's rate); 8 requests of 64 rows a chunk 157 us, where a tile has 8 to 32 steps and its
+// loads, rotations and results are a third.  One wave of 64 keys with V in registers spilled 150 of them (350 us there).
 template <int D, int KMI>
 __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   constexpr int KM = keys_of(KMI);
@@ -521,7 +527,10 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
 }
 
 // Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q and dO in
-// registers; K (rotated) and V pass through LDS, K read by rows and transposed.
+// registers; K (rotated) and V pass through LDS, K read by rows and transposed.  Eight waves share a tile's loads and
+// rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same ragged requests 1.03
+// ms for three products (720 TFLOP/s), the 64-row questions 85 us.  Two row blocks a wave spilled 150 registers (six times
+// as long).
 template <int D, int KMI, int NW, int NBUF>
 __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
   constexpr int KM = keys_of(KMI), NT = NW * 64;
@@ -646,7 +655,8 @@ constexpr int kMergeRows = 32, kMergeBlocks = 2 * kGradHalves * kGradTileKeys / 
 
 // Partial results added up in their order, two kinds of workgroups in one launch.  The first `blocks`: partial query
 // gradients of a block of tokens, turned back from the rows' positions, scaled, rounded.  The others: 32 rows of the key
-// or value gradients of a tile whose uses were cut into parts.  D / 16 threads a row.
+// or value gradients of a tile whose uses were cut into parts.  D / 16 threads a row.  Bound by memory (21 us for 5350
+// tokens of 32 heads of 64 in one split each, 66 MB).
 template <int D, bool IL>
 __global__ __launch_bounds__(256) void finish(GradArgs a, int blocks) {
   constexpr int TPR = D / 16;

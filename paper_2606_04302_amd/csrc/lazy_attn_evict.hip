@@ -3,8 +3,9 @@
 //
 // Key weights are sums that later calls go on with and that ranks are taken of, so their scores are formed more exactly
 // than an attention output needs: rotated queries and keys are each kept as two bf16 parts (2^-16 instead of 2^-8), and a
-// score is the sum of three products, first x first and the two mixed ones.  With one part each, sums over 8 to 32 heads
-// were 1e-4 to 5e-4 off (2-norm), now about 1e-6.  ALiBi rotates nothing: one part is exact.
+// score is the sum of three products, first x first and the two mixed ones; single tokens with few heads to a key take
+// products of 32 bits instead.  With one part each, sums over 8 to 32 heads were 1e-4 to 5e-4 off (2-norm), now 2e-8 to
+// 4e-7.  ALiBi rotates nothing: one part is exact.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -107,7 +108,10 @@ __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks)
 // Weights of a prompt: workgroup (key split and row split, KV head, request), two 64-key tiles at a time, 32 keys a wave,
 // whose rotated parts stay in registers while the rows of the request pass through LDS, 32 at a time, copied to the other
 // of two buffers during the products.  S = Q K^T has a key in every lane and 32 rows in registers and lane halves, so a
-// key's sum never leaves its lane.
+// key's sum never leaves its lane.  Bound by the three products: 4 requests of 256 rows and 33K keys 750 us, 828 GFLOP at
+// 1.10 PFLOP/s (the large library product: 1.22); 8 of 64 rows and 5.3K keys 84 us (0.79), where a tile's loads and
+// rotation serve 8 steps only.  Four tiles a workgroup: with 6, 8 or 12 the latter took 92, 84 and 109 us, the former the
+// same to 10% more.
 constexpr int kStepRows = 32;
 template <int D, int KMI>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) void weigh_prompt(WeightArgs a) {
@@ -684,7 +688,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
 // 0.2 us) and by LDS atomics on the same address (weights of a few octaves share their top bits).  So every pass does the
 // least for a score: no bounds (the tail is filled up with the lowest score, which is never picked before a key), the
 // first digit counted while the scores arrive, protected keys marked afterwards, passes that few scores concern skip
-// whole waves, and every bin has two counters, one for every other lane (one counter: 3.5 us more).
+// whole waves, and every bin has two counters, one for every other lane (one counter: 3.5 us more).  33068 keys 22 us;
+// 260 thousand in 16 slices 34 us in four launches, each 8 to 10 us of chained LDS passes and a sum over the slices'
+// counts (slices of 8192 keys: 4% longer, and 44% for eight such requests).
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kBins = 2048;
 constexpr int kSlice = 16384, kMostResident = 35840;
@@ -963,7 +969,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_slices(SelectArgs a) {
 }
 
 // Gather of kept keys: workgroup (64 kept keys, KV head, request).  The records that hold them are found by prefix sums
-// over the request's table, 256 records at a time.
+// over the request's table, 256 records at a time.  Bound by memory: 64 requests, 2048 of 16.4K keys each, 255 us for 1.08
+// GB (4.2 TB/s; a large copy 4.7).
 constexpr int kGather = 64;
 template <int D, int TURN, bool LOCAL, bool IL>
 __global__ __launch_bounds__(256) void gather_keys(CompactArgs a) {
