@@ -689,8 +689,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
 // least for a score: no bounds (the tail is filled up with the lowest score, which is never picked before a key), the
 // first digit counted while the scores arrive, protected keys marked afterwards, passes that few scores concern skip
 // whole waves, and every bin has two counters, one for every other lane (one counter: 3.5 us more).  33068 keys 22 us;
-// 260 thousand in 16 slices 34 us in four launches, each 8 to 10 us of chained LDS passes and a sum over the slices'
-// counts (slices of 8192 keys: 4% longer, and 44% for eight such requests).
+// 260 thousand in 16 slices 31 us in four launches, of which each chains loads, LDS passes and a sum over the slices'
+// counts (slices of 8192 keys: 16% longer, and 65% for eight such requests).
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kBins = 2048;
 constexpr int kSlice = 16384, kMostResident = 35840;
@@ -909,7 +909,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_slices(SelectArgs a) {
   __shared__ int before_s[2];
   const int r = blockIdx.y, w = blockIdx.x, tid = threadIdx.x;
   const int k0 = a.key_start[r], room = a.key_start[r + 1] - k0;
-  const int n = min(a.key_count ? max(0, min(a.key_count[r], room)) : room, (int)min((int64_t)a.slices * kSlice, (int64_t)INT32_MAX));
+  const int most = (int)min((int64_t)a.slices * kSlice, (int64_t)INT32_MAX);
+  const int n = min(a.key_count ? max(0, min(a.key_count[r], room)) : room, most);
   const int o0 = a.kept_start[r], b = a.kept_start[r + 1] - o0;
   if (b >= n || b <= 0) {
     if (PASS == 3) trivial_selection(a, n, b, o0);
@@ -919,8 +920,20 @@ __global__ __launch_bounds__(kSelectThreads) void select_slices(SelectArgs a) {
   const int used = (n - 1) / kSlice + 1;
   if (w >= used) return;
   const int j0 = w * kSlice, count = min(kSlice, n - j0);
-  const int filled = load_scores<PASS == 0>(sm, a.weights + k0, j0, count, n, a.sink, a.recent);
+  const float* const scores = a.weights + k0 + j0;
   SliceWork& own = all[w];
+  // Passes 1 and 2 look at every score once: in registers, loaded while the counts are added up.
+  constexpr bool ONCE = PASS == 1 || PASS == 2;
+  constexpr int PER = kSlice / kSelectThreads;
+  float x[PER];
+  int filled = 0;
+  if constexpr (ONCE) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) x[u] = scores[min(u * kSelectThreads + tid, count - 1)];
+    clear_counts(sm);
+  } else {
+    filled = load_scores<PASS == 0>(sm, a.weights + k0, j0, count, n, a.sink, a.recent);
+  }
   uint32_t prefix = 0;
   int need = b;
   if constexpr (PASS > 0) {  // the digit counted last, from every slice's counts
@@ -931,17 +944,18 @@ __global__ __launch_bounds__(kSelectThreads) void select_slices(SelectArgs a) {
     }
     int c[2] = {0, 0}, earlier[2] = {0, 0};
     const int b1 = kBins - 1 - 2 * tid;
-    for (int v0 = 0; v0 < used; v0 += 8) {
-      int2 x[8];
+    constexpr int B = 16;
+    for (int v0 = 0; v0 < used; v0 += B) {
+      int2 y[B];
 #pragma unroll
-      for (int v = 0; v < 8; ++v)
-        x[v] = *reinterpret_cast<const int2*>(&all[min(v0 + v, used - 1)].hist[PASS - 1][b1 - 1]);
+      for (int v = 0; v < B; ++v)
+        y[v] = *reinterpret_cast<const int2*>(&all[min(v0 + v, used - 1)].hist[PASS - 1][b1 - 1]);
 #pragma unroll
-      for (int v = 0; v < 8; ++v) {
-        c[0] += v0 + v < used ? x[v].y : 0;
-        c[1] += v0 + v < used ? x[v].x : 0;
-        earlier[0] += v0 + v < w ? x[v].y : 0;
-        earlier[1] += v0 + v < w ? x[v].x : 0;
+      for (int v = 0; v < B; ++v) {
+        c[0] += v0 + v < used ? y[v].y : 0;
+        c[1] += v0 + v < used ? y[v].x : 0;
+        earlier[0] += v0 + v < w ? y[v].y : 0;
+        earlier[1] += v0 + v < w ? y[v].x : 0;
       }
     }
     find_digit(sm, c, need);
@@ -960,7 +974,15 @@ __global__ __launch_bounds__(kSelectThreads) void select_slices(SelectArgs a) {
         own.need = need;
         own.above = before_s[0];
       }
-      count_digits(sm, filled, prefix, PASS);
+      const uint32_t width = PASS == 1 ? 1u << 21 : 1u << 10;
+      const int head = a.sink - j0, tail = n - a.recent - j0;
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        const int i = u * kSelectThreads + tid;
+        const uint32_t d = (i < head || i >= tail ? 0xffffffffu : score_of(x[u])) - prefix;
+        if (i < count && d < width) atomicAdd(&sm.hist[2 * (d >> (PASS == 1 ? 10 : 0)) + (tid & 1)], 1);
+      }
+      __syncthreads();
     }
     *reinterpret_cast<int2*>(&own.hist[PASS][2 * tid]) = own_bins(sm, tid);
   } else {
