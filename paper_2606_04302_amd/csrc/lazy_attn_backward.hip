@@ -91,8 +91,8 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
 // at hand and turned on when the next use has another position.
 //
 // Two waves a SIMD (three at D = 64) hide each other's latencies.  Bound by the products and by what stands between them in a wave
-// (exponentials, masks, conversions).  16 ragged requests, 1.23 TFLOP of five products: 1.17 ms for four (840 TFLOP/s,
-// 69% of the large library product's rate); 8 requests of 64 rows a chunk 157 us, where a tile has 8 to 32 steps and its
+// (exponentials, masks, conversions).  16 ragged requests, 1.23 TFLOP of five products: 1.04 ms for four (950 TFLOP/s,
+// 78% of the large library product's rate); 8 requests of 64 rows a chunk 148 us, where a tile has 8 to 32 steps and its
 // loads, rotations and results are a third.  One wave of 64 keys with V in registers spilled 150 of them (350 us there).
 template <int D, int KMI>
 __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
@@ -528,8 +528,8 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
 
 // Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q and dO in
 // registers; K (rotated) and V pass through LDS, K read by rows and transposed.  Eight waves share a tile's loads and
-// rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same ragged requests 1.03
-// ms for three products (720 TFLOP/s), the 64-row questions 85 us.  Two row blocks a wave spilled 150 registers (six times
+// rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same ragged requests 0.90
+// ms for three products (820 TFLOP/s), the 64-row questions 82 us.  Two row blocks a wave spilled 150 registers (six times
 // as long).
 template <int D, int KMI, int NW, int NBUF>
 __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
