@@ -91,7 +91,7 @@ struct GradPlanLayout {
 
 // Where the backward pass keeps its intermediate results (bytes into the workspace).
 struct GradWorkLayout {
-  size_t q, dout, info, angles, dq, parts, bytes;
+  size_t q, dout, info, dq, parts, bytes;
   GradWorkLayout(int hq, int hkv, int d, const lazy_backward_info_t& i) {
     const size_t rows = (size_t)i.total_q * (size_t)hq;
     size_t at = 0;
@@ -103,7 +103,6 @@ struct GradWorkLayout {
     q = put(rows * d * sizeof(uint16_t));                                        // rotated, scaled queries
     dout = put(rows * d * sizeof(uint16_t));                                     // packed like the queries
     info = put(rows * 2 * sizeof(float));                                        // -lse log2 e of each row, then -delta
-    angles = put((size_t)kGradTileKeys * d * sizeof(float));                     // rotations of positions 0 .. 63
     dq = put((size_t)i.row_slots * rows * d * sizeof(float));                    // partial query gradients
     // partial key and value gradients
     parts = put((size_t)i.num_parts * hkv * 2 * kGradHalves * kGradTileKeys * d * sizeof(float));

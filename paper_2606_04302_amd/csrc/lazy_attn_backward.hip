@@ -25,16 +25,11 @@ namespace {
 
 constexpr int kMaxBlockTokens = 16;
 
-// Queries rotated, scaled and packed by KV head; row constants.  One workgroup a block of tokens, D / 16 threads a row;
-// workgroups past the last block write the table of angles.  Bound by memory: 5350 tokens of 32 heads of 64 19 us for 110
+// Queries rotated, scaled and packed by KV head; row constants.  One workgroup a block of tokens, D / 16 threads a row.  Bound by memory: 5350 tokens of 32 heads of 64 19 us for 110
 // MB (5.8 TB/s, part of it from the caches).
 template <int D, bool IL>
-__global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
+__global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
   __shared__ float2 cs[kMaxBlockTokens][D / 2];
-  if ((int)blockIdx.x >= blocks) {
-    if (a.rotate_k) angle_rows<D>(a, blockIdx.x - blocks);
-    return;
-  }
   const GradBlock b = a.blocks[blockIdx.x];
   if (a.rotate_q) {
     for (int e = threadIdx.x; e < b.tokens * (D / 2); e += 256)
@@ -91,8 +86,8 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a, int blocks) {
 // at hand and turned on when the next use has another position.
 //
 // Two waves a SIMD (three at D = 64) hide each other's latencies.  Bound by the products and by what stands between them in a wave
-// (exponentials, masks, conversions).  16 ragged requests, 1.23 TFLOP of five products: 1.04 ms for four (950 TFLOP/s,
-// 78% of the large library product's rate); 8 requests of 64 rows a chunk 148 us, where a tile has 8 to 32 steps and its
+// (exponentials, masks, conversions).  16 ragged requests, 1.23 TFLOP of five products: 1.02 ms for four (970 TFLOP/s,
+// 79% of the large library product's rate); 8 requests of 64 rows a chunk 138 us, where a tile has 8 to 32 steps and its
 // loads, rotations and results are a third.  One wave of 64 keys with V in registers spilled 150 of them (350 us there).
 template <int D, int KMI>
 __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
@@ -110,7 +105,12 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   __shared__ uint16_t tv[4][32 * D] __attribute__((aligned(16)));  // a wave's V operands, then its results
   __shared__ int rpos_all[4][kGradRows] __attribute__((aligned(16)));
   __shared__ float rslope_all[4][kGradRows] __attribute__((aligned(16)));
-  __shared__ float2 turn_all[4][D / 2] __attribute__((aligned(16)));
+  // A key's angle is that of its block of eight keys, a table of each wave's, and that of its place in the block, a table
+  // of the workgroup's (rows four banks apart).  Loaded from memory, in the operands' layout, they kept the CU's address
+  // units busy for 4096 cycles a use, and again at the end (64 rows a chunk: 148 us instead of 138).
+  constexpr int RLD = D / 2 + 2;
+  __shared__ float2 turn_all[4][LOCAL ? RLD : 4 * RLD] __attribute__((aligned(16)));
+  __shared__ float2 place[KM == kKeysNope ? 8 * RLD : 2] __attribute__((aligned(16)));
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h2 = lane >> 5, g = id % a.hkv;
   const int hf = wave >> 1, k32 = 32 * (wave & 1), key = k32 + (lane & 31);
   const GradTile* const tile = a.tiles + id / a.hkv;
@@ -121,7 +121,21 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   float* const rslope = rslope_all[wave];
   float2* const turn = turn_all[wave];
   const double rev = ROT ? revolutions(a, lane % (D / 2)) : 0.0;
-  const float2* angles = reinterpret_cast<const float2*>(a.ws_angles);
+  const auto block_angles = [&](int pos, int step) {  // of pos, pos + step, ..: one for local-position keys
+    const int l = again(lane);
+#pragma unroll
+    for (int e = 0; e < (LOCAL ? D / 2 : 2 * D); e += 64)
+      if (!LOCAL || l < D / 2)
+        turn[(e + l) / (D / 2) * RLD + l % (D / 2)] = rope_cs(pos + (e + l) / (D / 2) * step, rev);
+    wait_reads();
+  };
+  const float2* const own_turn = turn + (LOCAL ? 0 : (lane & 31) / 8 * RLD);
+  const float2* const own_place = place + (LOCAL ? 0 : (lane & 7) * RLD);
+  if (KM == kKeysNope) {
+    static_assert(256 % (D / 2) == 0, "a thread's entries share one pair");
+    for (int e = threadIdx.x; e < 8 * (D / 2); e += 256) place[e / (D / 2) * RLD + e % (D / 2)] = rope_cs(e / (D / 2), rev);
+    __syncthreads();
+  }
   const int own_key = min(key, t.keys - 1);  // lanes past the last key repeat it; their columns are not stored
 
   u32x4 kf[D / 16];
@@ -130,9 +144,12 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = f32x16{};
   const uint16_t* krow = a.k_pool + t.k_off + ((int64_t)g * t.kst + own_key) * D;
   if (active) {
-    const uint16_t* v = a.v_pool + t.v_off + ((int64_t)g * t.vst + own_key) * D + 8 * h2;
+    const uint16_t* v = a.v_pool + t.v_off + (int64_t)g * t.vst * D;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) copy_async(v + 16 * s, tv[wave] + 512 * s);
+    for (int i = 0; i < 32 * C / 64; ++i) {
+      const int row = (64 * i + lane) / C, chunk = (64 * i + lane) % C ^ swizzle<D>(row);
+      copy_async(v + min(k32 + row, t.keys - 1) * D + 8 * chunk, tv[wave] + 512 * i);
+    }
   }
   const uint16_t* qbase = a.ws_q + (int64_t)g * a.rows * D;
   const uint16_t* dbase = a.ws_do + (int64_t)g * a.rows * D;
@@ -166,7 +183,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
       if (ROT) {
         if (!first && here != frame) {
           if (l < D / 2) turn[l] = rope_cs(here - frame, rev);
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          wait_reads();
 #pragma unroll
           for (int db = 0; db < D / 64; ++db)
 #pragma unroll
@@ -178,14 +195,12 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
               dk[db + D / 64][i] = y2;
               if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          wait_reads();
         }
-        if (l < D / 2) turn[l] = rope_cs(here, rev);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        block_angles(LOCAL ? here : here + k32, 8);
       }
-      rotate_keys<D, KM, IL>(kf, l >> 5, turn, [&](int t) {
-        return *reinterpret_cast<const f32x4*>(angles + (k32 + (l & 31)) * (D / 2) + t);
-      });
+      rotate_keys<D, KM, IL>(kf, l >> 5, own_turn,
+                             [&](int t) { return *reinterpret_cast<const f32x4*>(own_place + t); });
       frame = here;
       first = false;
     }
@@ -196,15 +211,13 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
         rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + seg.pos_shift : INT32_MAX;
         if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      wait_reads();
     }
 
     const TileOperands<D> op(again(lane));
     // Operands are read one step ahead of their products, and the scheduler is fenced at every step: the reads in flight
     // hide their latency without taking more registers than there are.
-    const auto value = [&](int k) {
-      return as_bf16x8(*reinterpret_cast<const u32x4*>(tv[wave] + 512 * k + 8 * lane));
-    };
+    const auto value = [&](int k) { return op.row(tv[wave], 0, k); };
     f32x16 s, dp;
     bf16x8 fq[2], fd[2], fv[2];
     fq[0] = op.row(tq, 0, 0);
@@ -315,25 +328,24 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   if (!active) return;
 
   // q carries scale * log2 e, dk wants scale: a factor of ln 2.  Turned back to the frame in which the key is stored.
-  if (ROT && lane < D / 2) turn[lane] = rope_cs(-frame, rev);
-  wait_copies();
+  if (ROT) block_angles(LOCAL ? -frame : -(frame + k32), -8);
 #pragma unroll
   for (int db = 0; db < D / 64; ++db)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float x1 = dk[db][i] * kLn2, x2 = dk[db + D / 64][i] * kLn2;
-      if (ROT) {
-        const int pair = 32 * db + 8 * (i >> 2) + 4 * h2 + (i & 3);
-        float2 cs = make_float2(1.f, 0.f);
-        if (!LOCAL) {
-          cs = angles[key * (D / 2) + pair];
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const int pair = 32 * db + 8 * q4 + 4 * h2;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 4 * q4 + e;
+        float x1 = dk[db][i] * kLn2, x2 = dk[db + D / 64][i] * kLn2;
+        if (ROT) {
+          float2 cs = LOCAL ? make_float2(1.f, 0.f) : own_place[pair + e];
           cs.y = -cs.y;
+          rotate_pair(x1, x2, own_turn[pair + e], cs, x1, x2);
         }
-        rotate_pair(x1, x2, turn[pair], cs, x1, x2);
+        dk[db][i] = x1;
+        dk[db + D / 64][i] = x2;
       }
-      dk[db][i] = x1;
-      dk[db + D / 64][i] = x2;
-      if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
     }
   if (part >= 0) {
     float* out = a.ws_parts + ((((int64_t)part * a.hkv + g) * kGradHalves + hf) * 2 * kGradTileKeys + key) * D;
@@ -369,7 +381,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
           *reinterpret_cast<u32x4*>(stage + tile_at<D>(lane & 31, col / 4)) = w;
         }
       }
-    wait_copies();
+    wait_reads();
     uint16_t* out = which ? a.dk_pool + t.k_off + ((int64_t)g * t.kst + k32) * D
                           : a.dv_pool + t.v_off + ((int64_t)g * t.vst + k32) * D;
 #pragma unroll
@@ -379,7 +391,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
         *reinterpret_cast<u32x4*>(out + row * D + 8 * chunk) =
             *reinterpret_cast<const u32x4*>(stage + tile_at<D>(row, chunk));
     }
-    wait_copies();
+    wait_reads();
   }
 }
 template <int D, int KMI, int WPE>
@@ -727,7 +739,7 @@ __global__ __launch_bounds__(256) void finish(GradArgs a, int blocks) {
 template <int D, int KMI>
 hipError_t launch(const GradArgs& a, const lazy_backward_info_t& i, hipStream_t stream) {
   constexpr bool IL = interleaved_of(KMI);
-  prepare_rows<D, IL><<<i.num_blocks + kAngleBlocks<D>, 256, 0, stream>>>(a, i.num_blocks);
+  if (i.num_blocks) prepare_rows<D, IL><<<i.num_blocks, 256, 0, stream>>>(a);
   const int tiles = i.num_tiles * a.hkv, items = i.num_row_items * a.hkv;
   const bool together = i.row_blocks == 1 && grads_together(D, tiles, items);
   if (together) grad_all<D, KMI><<<tiles + items, 256, 0, stream>>>(a, tiles);

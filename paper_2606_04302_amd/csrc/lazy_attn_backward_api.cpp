@@ -55,7 +55,6 @@ extern "C" int lazy_attn_prefill_backward(const lazy_attn_params_t* p, const voi
   a.dv_pool = static_cast<uint16_t*>(dv_pool);
   a.ws_q = reinterpret_cast<uint16_t*>(work + ws.q);
   a.ws_do = reinterpret_cast<uint16_t*>(work + ws.dout);
-  a.ws_angles = reinterpret_cast<float*>(work + ws.angles);
   a.ws_info = reinterpret_cast<float*>(work + ws.info);
   a.ws_dq = reinterpret_cast<float*>(work + ws.dq);
   a.ws_parts = reinterpret_cast<float*>(work + ws.parts);
@@ -67,7 +66,6 @@ extern "C" int lazy_attn_prefill_backward(const lazy_attn_params_t* p, const voi
   a.group_magic = a.group == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
   a.causal = p->causal;
   a.rotate_q = !p->q_prerotated && p->rope_style != LAZY_ALIBI;
-  a.rotate_k = p->rope_style != LAZY_ALIBI;
   lazy::rope_revolutions(p, a.rev);
   a.scale_log2 = lazy::scale_log2(p);
   const hipError_t err =

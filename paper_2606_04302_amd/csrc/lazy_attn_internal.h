@@ -97,7 +97,6 @@ struct GradArgs {
   uint16_t* ws_q;              // [hkv][rows][D] rotated queries times scale * log2 e, pairs in half-split order
   uint16_t* ws_do;             // [hkv][rows][D] dout
   float* ws_info;              // [2][hkv][rows] -lse log2 e, then -delta
-  float* ws_angles;            // [64][D/2] (cos, sin) of positions 0 .. 63
   float* ws_dq;                // [row_slots][hkv][rows][D]
   float* ws_parts;             // [num_parts][hkv][dk, dv][64][D]
   const float* inv_freq;       // [D/2] or null; ALiBi: [hq] slopes or null
@@ -108,7 +107,6 @@ struct GradArgs {
   uint32_t group_magic;        // ceil(2^32 / group), 0 for group 1
   int32_t causal;
   int32_t rotate_q;            // 0: queries arrive rotated, or nothing is (ALiBi)
-  int32_t rotate_k;            // 0: ALiBi
   float scale_log2;
   double rev[64];              // rotations per position of each pair, in revolutions (unused with inv_freq)
 };
