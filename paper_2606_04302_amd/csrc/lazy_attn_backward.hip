@@ -89,6 +89,14 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
 // (exponentials, masks, conversions).  16 ragged requests, 1.23 TFLOP of five products: 1.02 ms for four (970 TFLOP/s,
 // 79% of the large library product's rate); 8 requests of 64 rows a chunk 138 us, where a tile has 8 to 32 steps and its
 // loads, rotations and results are a third.  One wave of 64 keys with V in registers spilled 150 of them (350 us there).
+// A use as a wave's half of the tile sees it, and a step over it.
+struct Use {
+  int row_begin, row_end, pos_shift, full_from, pos, record_pos, key_begin, key_end;
+};
+struct Step {
+  Use use;
+  int row0;
+};
 template <int D, int KMI>
 __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   constexpr int KM = keys_of(KMI);
@@ -113,8 +121,11 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   __shared__ float2 place[KM == kKeysNope ? 8 * RLD : 2] __attribute__((aligned(16)));
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h2 = lane >> 5, g = id % a.hkv;
   const int hf = wave >> 1, k32 = 32 * (wave & 1), key = k32 + (lane & 31);
-  const GradTile* const tile = a.tiles + id / a.hkv;
-  const GradHalf t = tile->half[hf];
+  const cptr<GradTile> tile = as_const(a.tiles) + id / a.hkv;
+  const struct {
+    int64_t k_off, v_off;
+    int kst, vst, keys;
+  } t = {tile->half[hf].k_off, tile->half[hf].v_off, tile->half[hf].kst, tile->half[hf].vst, tile->half[hf].keys};
   const int seg_begin = tile->seg_begin, seg_end = tile->seg_end, part = tile->part;
   const bool active = k32 < t.keys;  // a wave without keys only helps to copy
   int* const rpos = rpos_all[wave];
@@ -157,8 +168,14 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   int frame = 0;  // position by which dk is rotated (NoPE: that of the half's key 0)
   bool first = true;
 
-  const auto fetch = [&](int si, int row0, uint16_t* tq, uint16_t* td, float* in) {
-    const int most = a.segs[si].row_end - 1 - row0;  // rows past the use's end repeat its last one
+  const auto load_use = [&](int i) {
+    const cptr<GradSeg> u = as_const(a.segs) + i;
+    const cptr<GradSeg::Half> h = &u->half[hf];
+    return Use{u->row_begin, u->row_end, u->pos_shift, u->full_from, h->pos, h->record_pos, h->key_begin, h->key_end};
+  };
+
+  const auto fetch = [&](const Step& step, uint16_t* tq, uint16_t* td, float* in) {
+    const int row0 = step.row0, most = step.use.row_end - 1 - row0;  // rows past the use's end repeat its last one
     const uint16_t* q = qbase + (int64_t)row0 * D;
     const uint16_t* d = dbase + (int64_t)row0 * D;
     const int e0 = again(threadIdx.x);
@@ -173,12 +190,12 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
       copy_async4(ibase + (lane & 32 ? a.hkv * a.rows : 0) + row0 + min(lane & 31, most), in);
   };
 
-  const auto compute = [&](int si, int row0, const uint16_t* tq, const uint16_t* td, const float* in) {
-    const GradSeg& seg = a.segs[si];
-    const int rows = min(kGradRows, seg.row_end - row0), pos = seg.half[hf].pos;
+  const auto compute = [&](const Step& step, const uint16_t* tq, const uint16_t* td, const float* in) {
+    const Use& seg = step.use;
+    const int row0 = step.row0, rows = min(kGradRows, seg.row_end - row0), pos = seg.pos;
     if (row0 == seg.row_begin) {  // a new use: its keys, and dk turned on to its frame
       const int l = again(lane);
-      const int here = LOCAL ? seg.half[hf].record_pos : pos;
+      const int here = LOCAL ? seg.record_pos : pos;
       load_keys<D, IL>(krow, l >> 5, kf);
       if (ROT) {
         if (!first && here != frame) {
@@ -208,7 +225,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
     if (ALIBI || masked) {
       if (lane < kGradRows) {
         const int src = row0 + lane, tok = token_of(src, a.group_magic);
-        rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + seg.pos_shift : INT32_MAX;
+        rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + seg.pos_shift : INT32_MAX - 1;
         if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
       }
       wait_reads();
@@ -259,14 +276,19 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = fast_exp2(s[i]);
     if (masked) {
-      const bool used = key >= seg.half[hf].key_begin && key < seg.half[hf].key_end;
-      const int p = a.causal ? pos + key : 0;
+      // Keys that the use does not have lie past every row.
+      const bool used = key >= seg.key_begin && key < seg.key_end;
+      const int p = !used ? INT32_MAX : a.causal ? pos + key : 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
-        const bool ok = used && p <= rpos[row];
-        s[i] = ok ? s[i] : 0.f;
-        dp[i] = ok ? dp[i] : 0.f;
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int4 last = *reinterpret_cast<const int4*>(rpos + 8 * q4 + 4 * h2);
+        const int at[4] = {last.x, last.y, last.z, last.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool ok = p <= at[e];
+          s[4 * q4 + e] = ok ? s[4 * q4 + e] : 0.f;
+          dp[4 * q4 + e] = ok ? dp[4 * q4 + e] : 0.f;
+        }
       }
     }
     __builtin_amdgcn_s_setprio(1);
@@ -293,35 +315,36 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
     }
     __builtin_amdgcn_s_setprio(0);
   };
-  const auto advance = [&](int& si, int& row0) {  // to the next step; false at the end
-    row0 += kGradRows;
-    if (row0 < a.segs[si].row_end) return true;
-    if (++si >= seg_end) return false;
-    row0 = a.segs[si].row_begin;
-    return true;
-  };
-
   if (seg_begin < seg_end) {
-    int si = seg_begin, row0 = a.segs[seg_begin].row_begin;
-    fetch(si, row0, tq0, td0, in0);
+    int si = seg_begin;
+    Step now{load_use(si), 0}, next;
+    now.row0 = now.use.row_begin;
+    Use ahead = load_use(min(si + 1, seg_end - 1));
+    const auto advance = [&] {  // next: the step after now; false at the end
+      next = now;
+      next.row0 += kGradRows;
+      if (next.row0 < now.use.row_end) return true;
+      if (++si >= seg_end) return false;
+      next = {ahead, ahead.row_begin};
+      ahead = load_use(min(si + 1, seg_end - 1));
+      return true;
+    };
+    fetch(now, tq0, td0, in0);
     while (true) {
-      int nsi = si, nrow0 = row0;
-      bool more = advance(nsi, nrow0);
+      bool more = advance();
       wait_copies();
       __syncthreads();
-      if (more) fetch(nsi, nrow0, tq1, td1, in1);
-      if (active) compute(si, row0, tq0, td0, in0);
+      if (more) fetch(next, tq1, td1, in1);
+      if (active) compute(now, tq0, td0, in0);
       if (!more) break;
-      si = nsi;
-      row0 = nrow0;
-      more = advance(nsi, nrow0);
+      now = next;
+      more = advance();
       wait_copies();
       __syncthreads();
-      if (more) fetch(nsi, nrow0, tq0, td0, in0);
-      if (active) compute(si, row0, tq1, td1, in1);
+      if (more) fetch(next, tq0, td0, in0);
+      if (active) compute(now, tq1, td1, in1);
       if (!more) break;
-      si = nsi;
-      row0 = nrow0;
+      now = next;
     }
   }
   wait_copies();
@@ -512,11 +535,9 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
 #pragma unroll
     for (int i = 0; i < 16; ++i) dp[i] *= fast_exp2(s[i]);
     if (masked) {
+      const int last = (causal ? min(nvalid - 1, qpos - b0) : nvalid - 1) - 32 * kb - 4 * h2;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int kk = 32 * kb + 8 * (i >> 2) + 4 * h2 + (i & 3);
-        dp[i] = kk < nvalid && (!causal || b0 + kk <= qpos) ? dp[i] : 0.f;
-      }
+      for (int i = 0; i < 16; ++i) dp[i] = 8 * (i >> 2) + (i & 3) <= last ? dp[i] : 0.f;
     }
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
