@@ -443,7 +443,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
     split = at / (int)gridDim.y;
     r = at - split * (int)gridDim.y;
   }
-  const int qpos = a.q_pos0[r], room = a.key_start[r + 1] - a.key_start[r];
+  // Loaded once: the compiler cannot know that the weights do not lie over them.
+  const int qpos = uniform(a.q_pos0[r]), k0 = uniform(a.key_start[r]), room = uniform(a.key_start[r + 1]) - k0;
   const int c0 = a.chunk_start[r], c1 = a.chunk_start[r + 1];
   if (ROT && tid < D / 2) {
     qcs[tid] = rope_cs(a.rotate_q ? qpos : 0, revolutions(a, tid));
@@ -531,7 +532,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
       const auto begin = [&] {
         const int key = it.j0 + 16 * sub + col, at = it.base + key;
         sum = old = 0.f;
-        if (prior && key < it.cur.len && at < room) old = prior[a.key_start[r] + at];
+        if (prior && key < it.cur.len && at < room) old = prior[k0 + at];
         if (ROT) {
           float2* const base = base_all[wave];
           if (lane < D / 2) base[lane] = rope_cs(LOCAL ? it.cur.pos : it.cur.pos + it.j0 + 16 * sub, own_rev);
@@ -564,7 +565,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
         }
         if (a.causal && it.cur.pos + key > qpos) sum = 0.f;
         if ((HS == 1 || wave == 0) && kq == 0 && key < it.cur.len && at < room)
-          a.weights[a.key_start[r] + at] = prior ? fmaf(fade, old, sum) : sum;
+          a.weights[k0 + at] = prior ? fmaf(fade, old, sum) : sum;
         it.next();
       };
       const auto consume = [&] {
