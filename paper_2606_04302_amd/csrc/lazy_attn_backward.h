@@ -103,7 +103,7 @@ struct GradWorkLayout {
     q = put(rows * d * sizeof(uint16_t));                                        // rotated, scaled queries
     dout = put(rows * d * sizeof(uint16_t));                                     // packed like the queries
     info = put(rows * 2 * sizeof(float));                                        // -lse log2 e of each row, then -delta
-    dq = put((size_t)i.row_slots * rows * d * sizeof(float));                    // partial query gradients
+    dq = put((size_t)(i.row_slots > 1 ? i.row_slots : 0) * rows * d * sizeof(float));  // partial query gradients
     // partial key and value gradients
     parts = put((size_t)i.num_parts * hkv * 2 * kGradHalves * kGradTileKeys * d * sizeof(float));
     bytes = at;

@@ -567,7 +567,7 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
 template <int D, int KMI, int NW, int NBUF>
 __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
   constexpr int KM = keys_of(KMI), NT = NW * 64;
-  constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal;
+  constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
   using S = TileLayout<D>;
   __shared__ GradQSmem<D, NBUF> sm;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), h2 = lane >> 5, g = id % a.hkv;
@@ -661,6 +661,58 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
     }
     have = have_next;
   }
+  if (item.splits == 1) {  // whole sums: turned back, scaled, rounded and written here, in whole rows through LDS
+    __syncthreads();
+    constexpr int C = D / 8;
+    static_assert(sizeof(sm.k) + sizeof(sm.v) >= NW * 32 * D * sizeof(uint16_t));
+    uint16_t* const stage = &sm.k[0][0] + wave * 32 * D;
+    const float scale = a.scale_log2 * kLn2;
+    const int first = qs * a.group + min(item.row0 + 32 * wave, nrows - 1), tok0 = uniform(token_of(first, a.group_magic));
+    if (ROT && a.rotate_q) {
+      float2* const turn = reinterpret_cast<float2*>(stage);
+      if (lane < D / 2) turn[lane] = rope_cs(-(tok0 + shift), sm.freq[lane]);
+      wait_reads();
+      const float* const place = sm.csd + (tok - tok0) * S::CSD_LD;  // 32 rows have at most 32 tokens
+#pragma unroll
+      for (int db = 0; db < D / 64; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int pair = 32 * db + 8 * (i >> 2) + 4 * h2 + (i & 3);
+          float2 cs = *reinterpret_cast<const float2*>(place + cs_idx<D>(pair));
+          cs.y = -cs.y;
+          float y1, y2;
+          rotate_pair(dq[db][i], dq[db + D / 64][i], turn[pair], cs, y1, y2);
+          dq[db][i] = y1;
+          dq[db + D / 64][i] = y2;
+        }
+      wait_reads();
+    }
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int col = 32 * db + 8 * q4 + 4 * h2;
+        const auto at = [&](int d, int e) { return dq[d][4 * q4 + e] * scale; };
+        if (!IL)
+          *reinterpret_cast<u32x2*>(stage + tile_at<D>(lane & 31, col / 8) + col % 8) =
+              u32x2{pack2(at(db, 0), at(db, 1)), pack2(at(db, 2), at(db, 3))};
+        else if (db < D / 64)
+          *reinterpret_cast<u32x4*>(stage + tile_at<D>(lane & 31, col / 4)) =
+              u32x4{pack2(at(db, 0), at(db + D / 64, 0)), pack2(at(db, 1), at(db + D / 64, 1)),
+                    pack2(at(db, 2), at(db + D / 64, 2)), pack2(at(db, 3), at(db + D / 64, 3))};
+      }
+    wait_reads();
+#pragma unroll
+    for (int i = 0; i < 32 * C / 64; ++i) {
+      const int row = (64 * i + lane) / C, chunk = (64 * i + lane) % C, at = item.row0 + 32 * wave + row;
+      if (at < nrows) {
+        const int to = qs * a.group + at, token = token_of(to, a.group_magic);
+        *reinterpret_cast<u32x4*>(a.dq + ((int64_t)token * a.hq + g * a.group + to - token * a.group) * D + 8 * chunk) =
+            *reinterpret_cast<const u32x4*>(stage + tile_at<D>(row, chunk));
+      }
+    }
+    return;
+  }
   if (pr >= nrows) return;
   float* out = a.ws_dq + (((int64_t)item.split * a.hkv + g) * a.rows + src) * D;
 #pragma unroll
@@ -736,6 +788,7 @@ __global__ __launch_bounds__(256) void finish(GradArgs a, int blocks) {
   }
   __shared__ float2 cs[kMaxBlockTokens][D / 2];
   const GradBlock b = a.blocks[blockIdx.x];
+  if (b.splits == 1) return;  // written with its sums
   if (a.rotate_q) {
     for (int e = threadIdx.x; e < b.tokens * (D / 2); e += 256)
       cs[e / (D / 2)][e % (D / 2)] = rope_cs(-(b.t0 + e / (D / 2) + b.pos_shift), revolutions(a, e % (D / 2)));
@@ -775,8 +828,8 @@ hipError_t launch(const GradArgs& a, const lazy_backward_info_t& i, hipStream_t 
       grad_q<D, KMI, 4, 2><<<items, 256, 0, stream>>>(a);
     }
   }
-  const int merges = i.num_merges * a.hkv * kMergeBlocks;
-  if (i.num_blocks + merges) finish<D, IL><<<i.num_blocks + merges, 256, 0, stream>>>(a, i.num_blocks);
+  const int merges = i.num_merges * a.hkv * kMergeBlocks, blocks = i.row_slots > 1 ? i.num_blocks : 0;
+  if (blocks + merges) finish<D, IL><<<blocks + merges, 256, 0, stream>>>(a, blocks);
   return hipGetLastError();
 }
 

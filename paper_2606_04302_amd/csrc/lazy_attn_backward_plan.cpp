@@ -50,10 +50,12 @@ int64_t steps_of(const GradSeg& s) { return (s.row_end - s.row_begin + kGradRows
 // Key splits of every request's row tiles.  A candidate lets no work item have more than a given number of key tiles; the
 // one with the least estimated time is taken: the makespan of the items, longest first, on the workgroups that the chip
 // holds, where an item costs its tiles and kItemTiles more (its prologue and its result), plus the partial results'
-// way to memory and back.  A tile of 256 rows takes a workgroup 3.7 us at head_dim 128.
+// way to memory and back and kFinishUs for the launch that adds them up (a request in one split writes its gradient by
+// itself; with 0 in its place 32 heads of 64 over 1088 keys took 29.3 us instead of 24.4, of 128 over 2112 keys 47.5
+// instead of 42.9).  A tile of 256 rows takes a workgroup 3.7 us at head_dim 128.
 // More splits are taken for a gain of 3% only (16 ragged requests of 17K keys: 1792 items on an estimate 2% below that of
 // 464 took as long, and their partial results 26 us more).
-constexpr double kItemTiles = 3, kTileUs = 3.7, kBytesPerUs = 4.5e6, kClose = 0.97;
+constexpr double kItemTiles = 3, kTileUs = 3.7, kBytesPerUs = 4.5e6, kFinishUs = 15, kClose = 0.97;
 std::vector<int32_t> row_splits(const std::vector<int64_t>& key_tiles, const int32_t* q_start, int batch, int G, int hkv,
                                 int d, int row_blocks) {
   const int slots = lazy::kNumCUs * (row_blocks == 2 ? 1 : d == 64 ? 3 : 2);
@@ -76,7 +78,7 @@ std::vector<int32_t> row_splits(const std::vector<int64_t>& key_tiles, const int
       if (rows == 0) continue;
       const int64_t n = lazy::ceil_div(rows, bm) * hkv * trial[r];
       items.emplace_back((double)key_tiles[r] / trial[r] + kItemTiles, n);
-      bytes += 8.0 * rows * hkv * d * trial[r];
+      if (trial[r] > 1) bytes += 8.0 * rows * hkv * d * trial[r];
       count += n;
     }
     std::sort(items.begin(), items.end(), [](const auto& a, const auto& b) { return a.first > b.first; });
@@ -94,7 +96,7 @@ std::vector<int32_t> row_splits(const std::vector<int64_t>& key_tiles, const int
       for (const auto& it : items) span += it.first * (double)it.second / slots;
       span += items.front().first / 2;
     }
-    const double cost = span * tile_us + bytes / kBytesPerUs;
+    const double cost = span * tile_us + bytes / kBytesPerUs + (bytes > 0 ? kFinishUs : 0.0);
     if (least < 0 || cost < kClose * least) {
       least = cost;
       best = trial;
