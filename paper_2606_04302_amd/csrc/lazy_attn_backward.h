@@ -13,9 +13,9 @@ constexpr int kGradHalves = 2;     // halves of a tile: 64 keys each, wherever t
 constexpr int kGradRows = 32;      // packed query rows (token * G + head in group) of one step over a tile
 // Do `tiles` and `items` workgroups (row items of 128 rows) share one launch?  It fills the chip with one kind's
 // workgroups while the other kind's last ones run, but holds both kinds' LDS and registers: a workgroup a CU at head_dim
-// 128, two instead of three at 64.  us apart / together, tiles + items.  128: 18 + 34 40.4 / 31.6, 136 + 272 64.2 / 51.8,
-// 264 + 272 71.5 / 71.0, 392 + 400 77.2 (half as many items, of 256 rows) / 92.4.  64: 136 + 272 47.7 / 38.3, 792 + 768
-// 137 / 106, 864 + 1256 290 / 269, 1176 + 624 89 / 86.5, 1816 + 768 156 / 162, 5020 + 2228 1093 / 1178.
+// 128, two instead of three at 64.  us apart / together, tiles + items.  128: 18 + 34 35.4 / 26.6, 136 + 176 53.5 (half as
+// many items, of 256 rows) / 43.3, 264 + 272 59.3 / 66.2, 392 + 320 65.6 / 74.6.  64: 136 + 272 39.0 / 29.9, 792 + 768
+// 115 / 101, 864 + 1256 249 / 235, 1176 + 624 83 / 77, 1816 + 768 137 / 142, 5020 + 2228 1086 / 1096.
 constexpr bool grads_together(int d, int64_t tiles, int64_t items) {
   return tiles > 0 && items > 0 && (d == 64 ? tiles <= 1280 : tiles + items <= 512);
 }

@@ -1,9 +1,10 @@
 // Backward pass of the prefill attention for gfx950: gradients of the queries and of the stored keys and values.
 //
-// Four launches, three where there is little work (grads_together).  (1) prepare_rows: queries rotated to their positions, times scale * log2 e, in bf16 and packed by KV
-// head (row = token * G + head in group), dO packed alike, and two numbers a row, -lse log2 e and -delta.  (2) grad_kv: dk
-// and dv, one tile of the store at a time.  (3) grad_q: partial dq, one row tile and key split at a time.  (4) finish:
-// partial dq summed, turned back and rounded, and the same for tiles whose uses were cut into parts.
+// Two to four launches.  (1) prepare_rows: queries rotated to their positions, times scale * log2 e, in bf16 and packed by
+// KV head (row = token * G + head in group), dO packed alike, and two numbers a row, -lse log2 e and -delta.  (2) grad_kv:
+// dk and dv, one tile of the store at a time.  (3) grad_q: dq, one row tile and key split at a time.  (4) finish: partial
+// dq of requests in several key splits summed, turned back and rounded, and the same for tiles whose uses were cut into
+// parts; only where there are any.  Where there is little work (2) and (3) are one launch, grad_all (grads_together).
 // The probabilities are recomputed in (2) and in (3): seven products of the two kernels against five if dq were summed
 // over key tiles with atomics, whose order would change results from call to call.
 //
@@ -25,8 +26,8 @@ namespace {
 
 constexpr int kMaxBlockTokens = 16;
 
-// Queries rotated, scaled and packed by KV head; row constants.  One workgroup a block of tokens, D / 16 threads a row.  Bound by memory: 5350 tokens of 32 heads of 64 19 us for 110
-// MB (5.8 TB/s, part of it from the caches).
+// Queries rotated, scaled and packed by KV head; row constants.  One workgroup a block of tokens, D / 16 threads a row.
+// Bound by memory: 5350 tokens of 32 heads of 64 19 us for 110 MB (5.8 TB/s, part of it from the caches).
 template <int D, bool IL>
 __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
   __shared__ float2 cs[kMaxBlockTokens][D / 2];
@@ -85,10 +86,12 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
 // during the products.  -lse and -delta are the accumulators' initial values.  dK is kept in the rotated frame of the use
 // at hand and turned on when the next use has another position.
 //
-// Two waves a SIMD (three at D = 64) hide each other's latencies.  Bound by the products and by what stands between them in a wave
-// (exponentials, masks, conversions).  16 ragged requests, 1.23 TFLOP of five products: 1.02 ms for four (970 TFLOP/s,
-// 79% of the large library product's rate); 8 requests of 64 rows a chunk 138 us, where a tile has 8 to 32 steps and its
-// loads, rotations and results are a third.  One wave of 64 keys with V in registers spilled 150 of them (350 us there).
+// Two waves a SIMD (three at D = 64) hide each other's latencies.  Bound by the products and by what stands between them
+// in a wave (exponentials, masks, conversions).  16 ragged requests, 1.23 TFLOP of five products: 0.98 ms for four (1000
+// TFLOP/s, 82% of the large library product's rate); 8 requests of 64 rows a chunk 129 us, where a tile has 8 to 24 steps
+// and its loads, rotations and results are a third.  One wave of 64 keys with V in registers spilled 150 of them (350 us
+// there); copies from rows that lie in the caches gain 2 to 6%, V operands in registers at D = 64 1%.
+
 // A use as a wave's half of the tile sees it, and a step over it.
 struct Use {
   int row_begin, row_end, pos_shift, full_from, pos, record_pos, key_begin, key_end;
@@ -561,9 +564,9 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
 
 // Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q and dO in
 // registers; K (rotated) and V pass through LDS, K read by rows and transposed.  Eight waves share a tile's loads and
-// rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same ragged requests 0.90
-// ms for three products (820 TFLOP/s), the 64-row questions 82 us.  Two row blocks a wave spilled 150 registers (six times
-// as long).
+// rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same ragged requests 0.89
+// ms for three products (830 TFLOP/s), the 64-row questions 82 us.  Two row blocks a wave spilled 150 registers (six times
+// as long).  A request in one key split has its whole sums here: they are turned back and written at once.
 template <int D, int KMI, int NW, int NBUF>
 __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
   constexpr int KM = keys_of(KMI), NT = NW * 64;
@@ -667,7 +670,8 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
     static_assert(sizeof(sm.k) + sizeof(sm.v) >= NW * 32 * D * sizeof(uint16_t));
     uint16_t* const stage = &sm.k[0][0] + wave * 32 * D;
     const float scale = a.scale_log2 * kLn2;
-    const int first = qs * a.group + min(item.row0 + 32 * wave, nrows - 1), tok0 = uniform(token_of(first, a.group_magic));
+    const int first = qs * a.group + min(item.row0 + 32 * wave, nrows - 1);
+    const int tok0 = uniform(token_of(first, a.group_magic));
     if (ROT && a.rotate_q) {
       float2* const turn = reinterpret_cast<float2*>(stage);
       if (lane < D / 2) turn[lane] = rope_cs(-(tok0 + shift), sm.freq[lane]);
@@ -728,7 +732,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 }
 // Both in one launch, the first `tiles` workgroups for keys and values.
 template <int D, int KMI>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, D == 64 ? 2 : 1))) void grad_all(GradArgs a, int tiles) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, D == 64 ? 2 : 1)))
+void grad_all(GradArgs a, int tiles) {
   if ((int)blockIdx.x < tiles)
     key_gradients<D, KMI>(a, blockIdx.x);
   else
@@ -740,8 +745,8 @@ constexpr int kMergeRows = 32, kMergeBlocks = 2 * kGradHalves * kGradTileKeys / 
 
 // Partial results added up in their order, two kinds of workgroups in one launch.  The first `blocks`: partial query
 // gradients of a block of tokens, turned back from the rows' positions, scaled, rounded.  The others: 32 rows of the key
-// or value gradients of a tile whose uses were cut into parts.  D / 16 threads a row.  Bound by memory (21 us for 5350
-// tokens of 32 heads of 64 in one split each, 66 MB).
+// or value gradients of a tile whose uses were cut into parts.  D / 16 threads a row.  Bound by memory (12 us for 512 tokens
+// of 32 heads of 128 in four splits, 38 MB).
 template <int D, bool IL>
 __global__ __launch_bounds__(256) void finish(GradArgs a, int blocks) {
   constexpr int TPR = D / 16;
