@@ -703,6 +703,12 @@ __device__ __forceinline__ uint32_t with_digit(uint32_t prefix, int digit, int p
   return prefix | (uint32_t)digit << (pass == 0 ? 21 : pass == 1 ? 10 : 0);
 }
 
+// x is in its register here: a load is not moved to a conditional use behind it, one of several in flight not put off.
+template <class T>
+__device__ __forceinline__ void loaded(T& x) {
+  asm volatile("" : "+v"(x));
+}
+
 template <int CAP>
 struct SelectSmem {
   uint32_t score[CAP] __attribute__((aligned(16)));
@@ -725,13 +731,15 @@ template <bool COUNT, int CAP>
 __device__ __forceinline__ int load_scores(SelectSmem<CAP>& sm, const float* w, int j0, int count, int n, int sink,
                                            int recent) {
   static_assert(CAP % kSelectThreads == 0);
-  constexpr int U = 8;
+  constexpr int U = 12;  // loads a thread has in flight
   const int tid = threadIdx.x, filled = (count + kSelectThreads - 1) & ~(kSelectThreads - 1);
   if (COUNT) clear_counts(sm);
   for (int base = 0; base < filled; base += U * kSelectThreads) {
     float x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) x[u] = w[j0 + min(base + u * kSelectThreads + tid, count - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) loaded(x[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (base + u * kSelectThreads >= filled) break;
@@ -816,6 +824,8 @@ __device__ __forceinline__ void write_kept(SelectSmem<CAP>& sm, int j0, int fill
 #pragma unroll
     for (int e = 0; e < kBatch; ++e) s[e] = mine[min(i + 64 * e, per - 64)];
 #pragma unroll
+    for (int e = 0; e < kBatch; ++e) loaded(s[e]);
+#pragma unroll
     for (int e = 0; e < kBatch; ++e) {
       if (i + 64 * e >= per) break;
       na += __builtin_popcountll(__ballot(s[e] > threshold));
@@ -838,6 +848,8 @@ __device__ __forceinline__ void write_kept(SelectSmem<CAP>& sm, int j0, int fill
     uint32_t s[kBatch];
 #pragma unroll
     for (int e = 0; e < kBatch; ++e) s[e] = mine[min(i + 64 * e, per - 64)];
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) loaded(s[e]);
 #pragma unroll
     for (int e = 0; e < kBatch; ++e) {
       if (i + 64 * e >= per) break;
