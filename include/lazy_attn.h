@@ -289,9 +289,9 @@ LAZY_API size_t lazy_attn_backward_workspace_size(const lazy_attn_params_t* para
  *            same pointer).  Every key of every record is overwritten, with zeros where no query
  *            sees it; everything else is left as it was.
  *   workspace  at least lazy_attn_backward_workspace_size(...) bytes, 16-byte aligned.
- * Gradients are rounded to bf16 once, from fp32 sums; q (rotated, times the scale) and the keys are rounded to bf16
- * for the matrix cores as in the forward pass, and so are P and dS.  With q_prerotated dq is the gradient of q as
- * given.  num_splits and cache_hint have no effect.
+ * Gradients are rounded to bf16 once, from fp32 sums; rotated queries and keys, P and dS keep 16 bits or more for the
+ * matrix cores (the forward pass's keep 8).  With q_prerotated dq is the gradient of q as given.  num_splits and cache_hint
+ * have no effect.
  */
 LAZY_API int lazy_attn_prefill_backward(const lazy_attn_params_t* params, const void* q, const int32_t* q_start,
                                         const int32_t* q_pos0, const void* k_pool, const void* v_pool,

@@ -10,6 +10,11 @@ each stored key summing over every use.  With the gradients come first-order bou
 makes which rounds rotated queries, rotated keys, P and dS to bf16 (relative error at most u = 2^-8 each), sums in
 fp32 and rounds the result once:  a score is off by at most E_ij = 2 u scale sum_d |q'_id k'_jd|, so P by the factor
 1 + E_ij, and every term of a sum by its own relative errors.
+
+``operand`` asks for the bounds of an evaluation that keeps those operands more exactly, to a relative error of
+``operand``: each as the sum of two bf16 numbers has 2^-17 (half a step of a half step), and products of two second parts
+are left out, 2^-18; 2^-15 leaves as much again for fp32 sums over some hundred steps of 16 (2^-24 each).  Scores, biases
+and their differences from the log-sum-exps are then bounded in fp32 too: 2^-22 (four roundings) of their magnitudes.
 """
 from __future__ import annotations
 
@@ -38,11 +43,12 @@ def _pair_sum(b, pairing):
 
 def lazy_backward(q, q_start, q_pos0, pool_k, pool_v, chunks, chunk_start, hq, hkv, d, base, causal, out, lse, dout,
                   dlse=None, pairing="half", key_positions="nope", inv_freq=None, softmax_scale=0.0,
-                  q_prerotated=False):
+                  q_prerotated=False, operand=None):
     """Returns (dq, dk_pool, dv_pool) and their error bounds (same shapes); pools are flat fp64 arrays."""
     G = hq // hkv
     scale = softmax_scale or 1.0 / math.sqrt(d)
     alibi = pairing == "alibi"
+    u = U if operand is None else operand
     theta = None if alibi else O.rope_frequencies(d, base, inv_freq)
     slopes = None
     if alibi:
@@ -74,7 +80,10 @@ def lazy_backward(q, q_start, q_pos0, pool_k, pool_v, chunks, chunk_start, hq, h
             L = lse[a:b, h]
             with np.errstate(invalid="ignore", over="ignore"):
                 P = np.where(hidden | np.isneginf(L)[:, None], 0.0, np.exp(s - L[:, None]))
-            E = 2 * U * scale * np.abs(Q[h]) @ np.abs(K[g]).T
+            E = 2 * u * scale * np.abs(Q[h]) @ np.abs(K[g]).T
+            if operand is not None:
+                bias = slopes[h] * np.abs(kpos[None, :] - qpos[:, None]) if alibi else 0.0
+                E = E + 2.0 ** -22 * (np.abs(s) + np.where(np.isneginf(L), 0.0, np.abs(L))[:, None] + bias)
             delta = (dout[a:b, h] * out[a:b, h]).sum(-1)
             if dlse is not None:
                 delta = delta - np.asarray(dlse, np.float64)[a:b, h]
@@ -84,11 +93,11 @@ def lazy_backward(q, q_start, q_pos0, pool_k, pool_v, chunks, chunk_start, hq, h
             fine = 2.0 ** -16 * P * (np.abs(dout[a:b, h]) @ np.abs(V[g]).T +
                                      (np.abs(dout[a:b, h] * out[a:b, h])).sum(-1)[:, None])
             GV[g] += P.T @ dout[a:b, h]
-            BV[g] += (P * (E + U)).T @ np.abs(dout[a:b, h])
+            BV[g] += (P * (E + u)).T @ np.abs(dout[a:b, h])
             GK[g] += scale * dS.T @ Q[h]
-            BK[g] += scale * (np.abs(dS) * (E + 2 * U) + fine).T @ np.abs(Q[h])
+            BK[g] += scale * (np.abs(dS) * (E + 2 * u) + fine).T @ np.abs(Q[h])
             gq = scale * dS @ K[g]
-            gb = scale * (np.abs(dS) * (E + 2 * U) + fine) @ np.abs(K[g])
+            gb = scale * (np.abs(dS) * (E + 2 * u) + fine) @ np.abs(K[g])
             if not alibi and not q_prerotated:
                 gq, gb = _turn_back(gq, qpos, theta, pairing), _pair_sum(gb, pairing)
             dq[a:b, h] = gq

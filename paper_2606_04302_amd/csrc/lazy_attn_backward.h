@@ -89,10 +89,13 @@ struct GradPlanLayout {
   }
 };
 
+// Rotated queries are the sum of two bf16 numbers; ALiBi rotates nothing, one is exact.
+inline int query_parts(const lazy_attn_params_t* p) { return p->rope_style == LAZY_ALIBI ? 1 : 2; }
+
 // Where the backward pass keeps its intermediate results (bytes into the workspace).
 struct GradWorkLayout {
   size_t q, dout, info, dq, parts, bytes;
-  GradWorkLayout(int hq, int hkv, int d, const lazy_backward_info_t& i) {
+  GradWorkLayout(int hq, int hkv, int d, int query_parts, const lazy_backward_info_t& i) {
     const size_t rows = (size_t)i.total_q * (size_t)hq;
     size_t at = 0;
     const auto put = [&at](size_t bytes) {
@@ -100,9 +103,9 @@ struct GradWorkLayout {
       at += (bytes + 255) & ~(size_t)255;
       return here;
     };
-    q = put(rows * d * sizeof(uint16_t));                                        // rotated, scaled queries
+    q = put(query_parts * rows * d * sizeof(uint16_t));                          // rotated queries
     dout = put(rows * d * sizeof(uint16_t));                                     // packed like the queries
-    info = put(rows * 2 * sizeof(float));                                        // -lse log2 e of each row, then -delta
+    info = put(rows * 2 * sizeof(float));                                        // -lse of each row, then -delta
     dq = put((size_t)(i.row_slots > 1 ? i.row_slots : 0) * rows * d * sizeof(float));  // partial query gradients
     // partial key and value gradients
     parts = put((size_t)i.num_parts * hkv * 2 * kGradHalves * kGradTileKeys * d * sizeof(float));

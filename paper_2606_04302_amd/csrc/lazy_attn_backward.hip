@@ -1,12 +1,20 @@
 // Backward pass of the prefill attention for gfx950: gradients of the queries and of the stored keys and values.
 //
-// Two to four launches.  (1) prepare_rows: queries rotated to their positions, times scale * log2 e, in bf16 and packed by
-// KV head (row = token * G + head in group), dO packed alike, and two numbers a row, -lse log2 e and -delta.  (2) grad_kv:
-// dk and dv, one tile of the store at a time.  (3) grad_q: dq, one row tile and key split at a time.  (4) finish: partial
-// dq of requests in several key splits summed, turned back and rounded, and the same for tiles whose uses were cut into
-// parts; only where there are any.  Where there is little work (2) and (3) are one launch, grad_all (grads_together).
-// The probabilities are recomputed in (2) and in (3): seven products of the two kernels against five if dq were summed
-// over key tiles with atomics, whose order would change results from call to call.
+// Two to four launches.  (1) prepare_rows: queries rotated to their positions and packed by KV head (row = token * G +
+// head in group), dO packed alike, and two numbers a row, -lse log2 e and -delta.  (2) grad_kv: dk and dv, one tile of the
+// store at a time.  (3) grad_q: dq, one row tile and key split at a time.  (4) finish: partial dq of requests in several key
+// splits summed, turned back and rounded, and the same for tiles whose uses were cut into parts; only where there are any.
+// Where there is little work (2) and (3) are one launch, grad_all (grads_together).  The probabilities are recomputed in (2)
+// and in (3): seven products of the two kernels against five if dq were summed over key tiles with atomics, whose order
+// would change results from call to call.
+//
+// Precision: rotated queries and keys, P and dS are each the sum of two bf16 numbers (split8, 2^-17), and a product of two
+// of them is three products, first x first and the two mixed ones; V, dO and ALiBi's queries and keys are exact as they are.
+// One part each, 2^-9 a term, is no error of 2^-9: where a handful of keys holds nearly all of a row's weight, elements of
+// a gradient are far smaller than their terms and far above the tensor's root mean square (3 rows over 28000 ALiBi keys:
+// elements wrong by 0.84 of the larger of themselves and that mean; scores of standard deviation 4: 0.1 to 1.4, and 1% in
+// the 2-norm).  Two parts leave the rounding of the result (0.0039, 0.0017 in the 2-norm) and make sixteen of seven products:
+// 16 ragged requests 3.9 ms instead of 1.85, 8 requests with 64 rows a chunk 0.40 instead of 0.21.
 //
 // Rotations: scores are products of keys and queries rotated to their absolute positions, as in the forward pass.  In
 // every tile in LDS and in every operand the head dimension is in half-split order, so that the pair (t, t + D/2) of a
@@ -26,8 +34,8 @@ namespace {
 
 constexpr int kMaxBlockTokens = 16;
 
-// Queries rotated, scaled and packed by KV head; row constants.  One workgroup a block of tokens, D / 16 threads a row.
-// Bound by memory: 5350 tokens of 32 heads of 64 19 us for 110 MB (5.8 TB/s, part of it from the caches).
+// Queries rotated, in two parts, packed by KV head; row constants.  One workgroup a block of tokens, D / 16 threads a row.
+// Bound by memory: 5015 tokens of 32 heads of 64 22 us for 123 MB (5.6 TB/s, part of it from the caches).
 template <int D, bool IL>
 __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
   __shared__ float2 cs[kMaxBlockTokens][D / 2];
@@ -54,10 +62,15 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
       yl[e] = element(lo, e);
       yh[e] = element(hi, e);
       if (a.rotate_q) rotate_by(element(lo, e), element(hi, e), cs[tok][t0 + e], yl[e], yh[e]);
-      yl[e] *= a.scale_log2;
-      yh[e] *= a.scale_log2;
     }
-    store_pairs<D, false>(a.ws_q + dst * D, t0, yl, yh);
+    u32x4 rest;
+    uint16_t* const second = a.ws_q + (a.hkv * a.rows + dst) * D;
+    split8(yl, lo, rest);
+    if (a.parts > 1) *reinterpret_cast<u32x4*>(second + t0) = rest;
+    split8(yh, hi, rest);
+    if (a.parts > 1) *reinterpret_cast<u32x4*>(second + D / 2 + t0) = rest;
+    *reinterpret_cast<u32x4*>(a.ws_q + dst * D + t0) = lo;
+    *reinterpret_cast<u32x4*>(a.ws_q + dst * D + D / 2 + t0) = hi;
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -72,25 +85,25 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
     for (int m = 1; m < TPR; m <<= 1) sum += __shfl_xor(sum, m, 64);
     if (t0 == 0) {
       if (a.dlse) sum -= a.dlse[src];
-      a.ws_info[dst] = dead ? -INFINITY : -lse * 1.4426950408889634f;  // exp2(0 - inf) = 0
+      a.ws_info[dst] = dead ? -INFINITY : -lse * a.lse_scale;  // exp2(0 - inf) = 0
       a.ws_info[a.hkv * a.rows + dst] = dead ? 0.f : -sum;
     }
   }
 }
 
-// Key and value gradients.  A workgroup owns a tile of two 64-key halves, each of its four waves 32 keys: K (rotated) stays
-// in registers and V in LDS, as the right-hand operands of S = Q K^T and dP = dO V^T, whose accumulators have a key in
-// every lane and 32 query rows in registers and lane halves; P and dS leave them as the right-hand operands of
-// dV^T += dO^T P and dK^T += Q^T dS without any exchange between lanes.  Q and dO come through LDS, 32 rows at a time,
-// read by rows for the first two products and transposed for the last two; the next 32 are copied to the other buffer
-// during the products.  -lse and -delta are the accumulators' initial values.  dK is kept in the rotated frame of the use
-// at hand and turned on when the next use has another position.
+// Key and value gradients.  A workgroup owns a tile of two 64-key halves, each of its four waves 32 keys: K (rotated, both
+// parts) stays in registers and V in LDS, as the right-hand operands of S = Q K^T and dP = dO V^T, whose accumulators have a
+// key in every lane and 32 query rows in registers and lane halves; P and dS leave them, in two parts, as the right-hand
+// operands of dV^T += dO^T P and dK^T += Q^T dS without any exchange between lanes.  S, dV, dP and dK follow each other, so
+// that besides K and the sums only one or two of them are in registers.  Q and dO come through LDS, 32 rows at a time, read
+// by rows for S and dP and transposed for dV and dK.  -delta is dP's initial value.  dK is kept in the rotated frame of the
+// use at hand and turned on when the next use has another position.
 //
-// Two waves a SIMD (three at D = 64) hide each other's latencies.  Bound by the products and by what stands between them
-// in a wave (exponentials, masks, conversions).  16 ragged requests, 1.23 TFLOP of five products: 0.98 ms for four (1000
-// TFLOP/s, 82% of the large library product's rate); 8 requests of 64 rows a chunk 129 us, where a tile has 8 to 24 steps
-// and its loads, rotations and results are a third.  One wave of 64 keys with V in registers spilled 150 of them (350 us
-// there); copies from rows that lie in the caches gain 2 to 6%, V operands in registers at D = 64 1%.
+// Two waves a SIMD (three at D = 64) hide each other's latencies.  At D = 64 the next 32 rows are copied to a second buffer
+// during the products; at D = 128 a second buffer would leave one workgroup a CU, and the other workgroup's products cover
+// the copies.  Bound by the products: 16 ragged requests, 2.2 TFLOP of nine products 2.1 ms (1050 TFLOP/s, 86% of the large
+// library product's rate); 8 requests of 64 rows a chunk 232 us, where a tile has 8 to 24 steps and its loads, rotations
+// and results are a third.
 
 // A use as a wave's half of the tile sees it, and a step over it.
 struct Use {
@@ -100,28 +113,38 @@ struct Step {
   Use use;
   int row0;
 };
+// 32 query rows in LDS: both parts of Q, dO, and -lse (times log2 e but for ALiBi), then -delta.
+template <int D, bool ROT>
+struct RowTiles {
+  uint16_t q[(ROT ? 2 : 1) * kGradRows * D] __attribute__((aligned(16)));
+  uint16_t d[kGradRows * D] __attribute__((aligned(16)));
+  float in[2 * kGradRows] __attribute__((aligned(16)));
+};
 template <int D, int KMI>
-__device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
+struct KeySmem {
+  static constexpr int KM = keys_of(KMI);
+  // A key's angle is that of its block of eight keys, a table of each wave's, and that of its place in the block, a table
+  // of the workgroup's (rows four banks apart).  Loaded from memory, in the operands' layout, they kept the CU's address
+  // units busy for 4096 cycles a use, and again at the end (64 rows a chunk: 148 us instead of 138).
+  static constexpr int RLD = D / 2 + 2;
+  RowTiles<D, KM != kKeysAlibi> rows;
+  uint16_t v[4][32 * D] __attribute__((aligned(16)));  // a wave's V operands, then its results
+  int rpos[4][kGradRows] __attribute__((aligned(16)));
+  float rslope[4][KM == kKeysAlibi ? kGradRows : 4] __attribute__((aligned(16)));
+  float2 turn[4][KM == kKeysAlibi ? 2 : KM == kKeysLocal ? RLD : 4 * RLD] __attribute__((aligned(16)));
+  float2 place[KM == kKeysNope ? 8 * RLD : 2] __attribute__((aligned(16)));
+};
+// `other`: a second buffer of rows, a variable of its own (the compiler then knows that copies to one do not touch reads
+// of the other), or null.
+template <int D, int KMI, bool TWO>
+__device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem<D, KMI>& sm,
+                                              RowTiles<D, keys_of(KMI) != kKeysAlibi>* other) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
   constexpr int C = D / 8;  // chunks of a row
   constexpr int COPIES = kGradRows * C / 256;
-  // Two buffers as variables of their own: the compiler then knows that copies to one do not touch reads of the other.
-  __shared__ uint16_t tq0[kGradRows * D] __attribute__((aligned(16)));
-  __shared__ uint16_t td0[kGradRows * D] __attribute__((aligned(16)));
-  __shared__ float in0[2 * kGradRows] __attribute__((aligned(16)));  // -lse log2 e, then -delta, of the rows
-  __shared__ uint16_t tq1[kGradRows * D] __attribute__((aligned(16)));
-  __shared__ uint16_t td1[kGradRows * D] __attribute__((aligned(16)));
-  __shared__ float in1[2 * kGradRows] __attribute__((aligned(16)));
-  __shared__ uint16_t tv[4][32 * D] __attribute__((aligned(16)));  // a wave's V operands, then its results
-  __shared__ int rpos_all[4][kGradRows] __attribute__((aligned(16)));
-  __shared__ float rslope_all[4][kGradRows] __attribute__((aligned(16)));
-  // A key's angle is that of its block of eight keys, a table of each wave's, and that of its place in the block, a table
-  // of the workgroup's (rows four banks apart).  Loaded from memory, in the operands' layout, they kept the CU's address
-  // units busy for 4096 cycles a use, and again at the end (64 rows a chunk: 148 us instead of 138).
-  constexpr int RLD = D / 2 + 2;
-  __shared__ float2 turn_all[4][LOCAL ? RLD : 4 * RLD] __attribute__((aligned(16)));
-  __shared__ float2 place[KM == kKeysNope ? 8 * RLD : 2] __attribute__((aligned(16)));
+  constexpr int RLD = KeySmem<D, KMI>::RLD;
+  using Tiles = RowTiles<D, ROT>;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h2 = lane >> 5, g = id % a.hkv;
   const int hf = wave >> 1, k32 = 32 * (wave & 1), key = k32 + (lane & 31);
   const cptr<GradTile> tile = as_const(a.tiles) + id / a.hkv;
@@ -131,9 +154,11 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   } t = {tile->half[hf].k_off, tile->half[hf].v_off, tile->half[hf].kst, tile->half[hf].vst, tile->half[hf].keys};
   const int seg_begin = tile->seg_begin, seg_end = tile->seg_end, part = tile->part;
   const bool active = k32 < t.keys;  // a wave without keys only helps to copy
-  int* const rpos = rpos_all[wave];
-  float* const rslope = rslope_all[wave];
-  float2* const turn = turn_all[wave];
+  int* const rpos = sm.rpos[wave];
+  float* const rslope = sm.rslope[wave];
+  float2* const turn = sm.turn[wave];
+  float2* const place = sm.place;
+  uint16_t* const tv = sm.v[wave];
   const double rev = ROT ? revolutions(a, lane % (D / 2)) : 0.0;
   const auto block_angles = [&](int pos, int step) {  // of pos, pos + step, ..: one for local-position keys
     const int l = again(lane);
@@ -152,7 +177,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   }
   const int own_key = min(key, t.keys - 1);  // lanes past the last key repeat it; their columns are not stored
 
-  u32x4 kf[D / 16];
+  u32x4 kh[D / 16], kl[D / 16];
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = f32x16{};
@@ -162,10 +187,11 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
 #pragma unroll
     for (int i = 0; i < 32 * C / 64; ++i) {
       const int row = (64 * i + lane) / C, chunk = (64 * i + lane) % C ^ swizzle<D>(row);
-      copy_async(v + min(k32 + row, t.keys - 1) * D + 8 * chunk, tv[wave] + 512 * i);
+      copy_async(v + min(k32 + row, t.keys - 1) * D + 8 * chunk, tv + 512 * i);
     }
   }
   const uint16_t* qbase = a.ws_q + (int64_t)g * a.rows * D;
+  const int64_t second = a.hkv * a.rows * D;  // from a query's first part to its second
   const uint16_t* dbase = a.ws_do + (int64_t)g * a.rows * D;
   const float* ibase = a.ws_info + (int64_t)g * a.rows;
   int frame = 0;  // position by which dk is rotated (NoPE: that of the half's key 0)
@@ -177,7 +203,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
     return Use{u->row_begin, u->row_end, u->pos_shift, u->full_from, h->pos, h->record_pos, h->key_begin, h->key_end};
   };
 
-  const auto fetch = [&](const Step& step, uint16_t* tq, uint16_t* td, float* in) {
+  const auto fetch = [&](const Step& step, Tiles& to) {
     const int row0 = step.row0, most = step.use.row_end - 1 - row0;  // rows past the use's end repeat its last one
     const uint16_t* q = qbase + (int64_t)row0 * D;
     const uint16_t* d = dbase + (int64_t)row0 * D;
@@ -186,20 +212,23 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
     for (int i = 0; i < COPIES; ++i) {
       const int row = (256 * i + e0) / C, chunk = ((256 * i + e0) % C) ^ swizzle<D>(row);
       const int off = min(row, most) * D + 8 * chunk;
-      copy_async(q + off, tq + 2048 * i + 512 * wave);
-      copy_async(d + off, td + 2048 * i + 512 * wave);
+      copy_async(q + off, to.q + 2048 * i + 512 * wave);
+      if (ROT) copy_async(q + second + off, to.q + kGradRows * D + 2048 * i + 512 * wave);
+      copy_async(d + off, to.d + 2048 * i + 512 * wave);
     }
     if (wave == 0)
-      copy_async4(ibase + (lane & 32 ? a.hkv * a.rows : 0) + row0 + min(lane & 31, most), in);
+      copy_async4(ibase + (lane & 32 ? a.hkv * a.rows : 0) + row0 + min(lane & 31, most), to.in);
   };
 
-  const auto compute = [&](const Step& step, const uint16_t* tq, const uint16_t* td, const float* in) {
+  const auto compute = [&](const Step& step, const Tiles& tiles) {
+    const uint16_t *const tq = tiles.q, *const tq2 = tiles.q + kGradRows * D, *const td = tiles.d;
+    const float* const in = tiles.in;
     const Use& seg = step.use;
     const int row0 = step.row0, rows = min(kGradRows, seg.row_end - row0), pos = seg.pos;
     if (row0 == seg.row_begin) {  // a new use: its keys, and dk turned on to its frame
       const int l = again(lane);
       const int here = LOCAL ? seg.record_pos : pos;
-      load_keys<D, IL>(krow, l >> 5, kf);
+      load_keys<D, IL>(krow, l >> 5, kh);
       if (ROT) {
         if (!first && here != frame) {
           if (l < D / 2) turn[l] = rope_cs(here - frame, rev);
@@ -219,8 +248,9 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
         }
         block_angles(LOCAL ? here : here + k32, 8);
       }
-      rotate_keys<D, KM, IL>(kf, l >> 5, own_turn,
-                             [&](int t) { return *reinterpret_cast<const f32x4*>(own_place + t); });
+      if (ROT)
+        rotate_keys_split<D, KM, IL>(kh, kl, l >> 5, own_turn,
+                                     [&](int t) { return *reinterpret_cast<const f32x4*>(own_place + t); });
       frame = here;
       first = false;
     }
@@ -229,7 +259,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
       if (lane < kGradRows) {
         const int src = row0 + lane, tok = token_of(src, a.group_magic);
         rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + seg.pos_shift : INT32_MAX - 1;
-        if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
+        if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, kLog2e);
       }
       wait_reads();
     }
@@ -237,47 +267,38 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
     const TileOperands<D> op(again(lane));
     // Operands are read one step ahead of their products, and the scheduler is fenced at every step: the reads in flight
     // hide their latency without taking more registers than there are.
-    const auto value = [&](int k) { return op.row(tv[wave], 0, k); };
-    f32x16 s, dp;
-    bf16x8 fq[2], fd[2], fv[2];
+    f32x16 s = f32x16{};
+    bf16x8 fq[2], fl[2], fd[2], fv[2];
     fq[0] = op.row(tq, 0, 0);
-    fd[0] = op.row(td, 0, 0);
-    fv[0] = value(0);
-#pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(in + 8 * q4 + 4 * h2);
-      const f32x4 y = *reinterpret_cast<const f32x4*>(in + kGradRows + 8 * q4 + 4 * h2);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[4 * q4 + e] = x[e];
-        dp[4 * q4 + e] = y[e];
-      }
-    }
+    if (ROT) fl[0] = op.row(tq2, 0, 0);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       if (k + 1 < D / 16) {
         fq[(k + 1) & 1] = op.row(tq, 0, k + 1);
-        fd[(k + 1) & 1] = op.row(td, 0, k + 1);
-        fv[(k + 1) & 1] = value(k + 1);
+        if (ROT) fl[(k + 1) & 1] = op.row(tq2, 0, k + 1);
       }
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[k & 1], as_bf16x8(kf[k]), s, 0, 0, 0);
-      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[k & 1], fv[k & 1], dp, 0, 0, 0);
+      if (ROT) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fl[k & 1], as_bf16x8(kh[k]), s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[k & 1], as_bf16x8(kl[k]), s, 0, 0, 0);
+      }
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[k & 1], as_bf16x8(kh[k]), s, 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
     fd[0] = op.column(td, 0, 0);
-    fq[0] = op.column(tq, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
-    if (ALIBI) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
-        s[i] = fmaf(rslope[row], (float)(pos + key - rpos[row]), s[i]);
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(in + 8 * q4 + 4 * h2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = 8 * q4 + 4 * h2 + e;
+        // The bias and the log-sum-exp may be large next to their difference: one rounding for both.
+        const float y = ALIBI ? fmaf(rslope[row], (float)(pos + key - rpos[row]), x[e]) * kLog2e : x[e];
+        s[4 * q4 + e] = fast_exp2(fmaf(s[4 * q4 + e], a.scale_log2, y));
       }
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = fast_exp2(s[i]);
     if (masked) {
       // Keys that the use does not have lie past every row.
       const bool used = key >= seg.key_begin && key < seg.key_end;
@@ -287,32 +308,69 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
         const int4 last = *reinterpret_cast<const int4*>(rpos + 8 * q4 + 4 * h2);
         const int at[4] = {last.x, last.y, last.z, last.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool ok = p <= at[e];
-          s[4 * q4 + e] = ok ? s[4 * q4 + e] : 0.f;
-          dp[4 * q4 + e] = ok ? dp[4 * q4 + e] : 0.f;
-        }
+        for (int e = 0; e < 4; ++e) s[4 * q4 + e] = p <= at[e] ? s[4 * q4 + e] : 0.f;
       }
     }
+    // Eight rows of x in two parts, the right-hand operands of the products over rows.
+    const auto parts = [](const f32x16& x, int k, u32x4& hi, u32x4& lo) {
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = x[8 * k + e];
+      split8(y, hi, lo);
+    };
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      float x[8], y[8];
+      u32x4 hi, lo;
+      parts(s, k, hi, lo);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = s[8 * k + e];
-        y[e] = dp[8 * k + e] * x[e];
+      for (int db = 0; db < D / 32; ++db) {
+        const int at = k * (D / 32) + db, ahead = at + 1;
+        if (ahead < 2 * (D / 32)) fd[ahead & 1] = op.column(td, 16 * (ahead / (D / 32)), ahead % (D / 32));
+        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[at & 1], as_bf16x8(lo), dv[db], 0, 0, 0);
+        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[at & 1], as_bf16x8(hi), dv[db], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      const bf16x8 pf = as_bf16x8(pack8(x)), sf = as_bf16x8(pack8(y));
+    }
+    f32x16 dp;
+    fd[0] = op.row(td, 0, 0);
+    fv[0] = op.row(tv, 0, 0);
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const f32x4 y = *reinterpret_cast<const f32x4*>(in + kGradRows + 8 * q4 + 4 * h2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[4 * q4 + e] = y[e];
+    }
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      if (k + 1 < D / 16) {
+        fd[(k + 1) & 1] = op.row(td, 0, k + 1);
+        fv[(k + 1) & 1] = op.row(tv, 0, k + 1);
+      }
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[k & 1], fv[k & 1], dp, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    fq[0] = op.column(tq, 0, 0);
+    if (ROT) fl[0] = op.column(tq2, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] *= dp[i];
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      u32x4 hi, lo;
+      parts(s, k, hi, lo);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
         const int at = k * (D / 32) + db, ahead = at + 1;
         if (ahead < 2 * (D / 32)) {
-          fd[ahead & 1] = op.column(td, 16 * (ahead / (D / 32)), ahead % (D / 32));
           fq[ahead & 1] = op.column(tq, 16 * (ahead / (D / 32)), ahead % (D / 32));
+          if (ROT) fl[ahead & 1] = op.column(tq2, 16 * (ahead / (D / 32)), ahead % (D / 32));
         }
-        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[at & 1], pf, dv[db], 0, 0, 0);
-        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[at & 1], sf, dk[db], 0, 0, 0);
+        if (ROT) dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fl[at & 1], as_bf16x8(hi), dk[db], 0, 0, 0);
+        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[at & 1], as_bf16x8(lo), dk[db], 0, 0, 0);
+        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[at & 1], as_bf16x8(hi), dk[db], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -332,20 +390,25 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
       ahead = load_use(min(si + 1, seg_end - 1));
       return true;
     };
-    fetch(now, tq0, td0, in0);
+    fetch(now, sm.rows);
     while (true) {
       bool more = advance();
       wait_copies();
       __syncthreads();
-      if (more) fetch(next, tq1, td1, in1);
-      if (active) compute(now, tq0, td0, in0);
+      if (TWO && more) fetch(next, *other);
+      if (active) compute(now, sm.rows);
       if (!more) break;
       now = next;
+      if (!TWO) {
+        __syncthreads();
+        fetch(now, sm.rows);
+        continue;
+      }
       more = advance();
       wait_copies();
       __syncthreads();
-      if (more) fetch(next, tq0, td0, in0);
-      if (active) compute(now, tq1, td1, in1);
+      if (more) fetch(next, sm.rows);
+      if (active) compute(now, *other);
       if (!more) break;
       now = next;
     }
@@ -353,7 +416,8 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
   wait_copies();
   if (!active) return;
 
-  // q carries scale * log2 e, dk wants scale: a factor of ln 2.  Turned back to the frame in which the key is stored.
+  // Scaled, and turned back to the frame in which the key is stored.
+  const float scale = a.scale_log2 * kLn2;
   if (ROT) block_angles(LOCAL ? -frame : -(frame + k32), -8);
 #pragma unroll
   for (int db = 0; db < D / 64; ++db)
@@ -363,7 +427,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = 4 * q4 + e;
-        float x1 = dk[db][i] * kLn2, x2 = dk[db + D / 64][i] * kLn2;
+        float x1 = dk[db][i] * scale, x2 = dk[db + D / 64][i] * scale;
         if (ROT) {
           float2 cs = LOCAL ? make_float2(1.f, 0.f) : own_place[pair + e];
           cs.y = -cs.y;
@@ -388,7 +452,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
     return;
   }
   // Through LDS, so that whole rows are written: a lane has neighbouring elements of one key, four at a time.
-  uint16_t* const stage = tv[wave];
+  uint16_t* const stage = tv;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
 #pragma unroll
@@ -422,13 +486,18 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id) {
 }
 template <int D, int KMI, int WPE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE, WPE))) void grad_kv(GradArgs a) {
-  key_gradients<D, KMI>(a, blockIdx.x);
+  __shared__ KeySmem<D, KMI> sm;
+  if constexpr (D == 64) {
+    __shared__ RowTiles<D, keys_of(KMI) != kKeysAlibi> other;
+    key_gradients<D, KMI, true>(a, blockIdx.x, sm, &other);
+  } else {
+    key_gradients<D, KMI, false>(a, blockIdx.x, sm, nullptr);
+  }
 }
 
 // Loads a 64-key tile of K and V for a workgroup of NT threads, NT / 64 a key row, rotates the keys and writes both to
-// LDS (unpadded tiles, pairs in half-split order).  The angles of the 32 rows are read from LDS for every tile: kept in
-// registers by the eight-wave kernel they cost it 27 spilled ones (16 ragged requests of 17K keys: 1457 instead of 1027
-// us).
+// LDS in two parts (unpadded tiles, pairs in half-split order).  The angles of the 32 rows are read from LDS for every
+// tile: the eight-wave kernel has no registers for them.
 template <int D, int KMI, int NT>
 struct TileLoader {
   using S = TileLayout<D>;
@@ -455,7 +524,7 @@ struct TileLoader {
 #pragma unroll
     for (int i = 0; i < VC; ++i) vr[i] = *reinterpret_cast<const u32x4*>(v + r * D + 8 * (part + TPR * i));
   }
-  __device__ void store(uint16_t* tk, uint16_t* tv, const float* cb2, const float* csd) {
+  __device__ void store(uint16_t* tk, uint16_t* tk2, uint16_t* tv, const float* cb2, const float* csd) {
     const float* cb = cb2 + (row / kAngleRows) * S::CSW;
     const float* cd = csd + (row & (kAngleRows - 1)) * S::CSD_LD;
 #pragma unroll
@@ -475,8 +544,11 @@ struct TileLoader {
                         *reinterpret_cast<const float2*>(cd + ci), yl[e], yh[e]);
           }
         }
-        lo = pack8(yl);
-        hi = pack8(yh);
+        u32x4 rest;
+        split8(yl, lo, rest);
+        *reinterpret_cast<u32x4*>(tk2 + tile_at<D>(row, t0 / 8)) = rest;
+        split8(yh, hi, rest);
+        *reinterpret_cast<u32x4*>(tk2 + tile_at<D>(row, D / 16 + t0 / 8)) = rest;
       }
       *reinterpret_cast<u32x4*>(tk + tile_at<D>(row, t0 / 8)) = lo;
       *reinterpret_cast<u32x4*>(tk + tile_at<D>(row, D / 16 + t0 / 8)) = hi;
@@ -486,10 +558,11 @@ struct TileLoader {
   }
 };
 
-template <int D, int NBUF>
+template <int D, int KMI, int NBUF>
 struct GradQSmem {
   using S = TileLayout<D>;
-  uint16_t k[NBUF][kSub * D] __attribute__((aligned(16)));
+  static constexpr bool ROT = keys_of(KMI) != kKeysAlibi;
+  uint16_t k[NBUF][(ROT ? 2 : 1) * kSub * D] __attribute__((aligned(16)));  // both parts
   uint16_t v[NBUF][kSub * D] __attribute__((aligned(16)));
   float csd[kAngleRows * S::CSD_LD] __attribute__((aligned(16)));
   float csb[2][2][S::CSW] __attribute__((aligned(16)));
@@ -500,45 +573,57 @@ struct GradQSmem {
 // every lane; dS^T leaves them as the right-hand operand of dQ^T += K^T dS^T.
 template <int D, bool ALIBI>
 __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv, int lane, const bf16x8 (&qf)[D / 16],
-                                          const bf16x8 (&df)[D / 16], f32x16 (&dq)[D / 32], float nl, float nd,
-                                          float slope, int qpos, int b0, int nvalid, int qmin, int causal) {
+                                          const bf16x8 (&ql)[D / 16], const bf16x8 (&df)[D / 16],
+                                          f32x16 (&dq)[D / 32], float scale_log2, float nl, float nd, float slope,
+                                          int qpos, int b0, int nvalid, int qmin, int causal) {
+  constexpr bool ROT = !ALIBI;
   const int h2 = lane >> 5;
   const bool masked = nvalid < kSub || (causal && b0 + kSub - 1 > qmin);
   const TileOperands<D> op(again(lane));
+  const uint16_t* const tk2 = tk + kSub * D;
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
-    f32x16 s, dp;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = nl;
-      dp[i] = nd;
-    }
+    f32x16 s = f32x16{}, dp;
     __builtin_amdgcn_s_setprio(1);
     // Operands one step ahead of their products.
-    bf16x8 fk[2] = {op.row(tk, 32 * kb, 0)}, fv[2] = {op.row(tv, 32 * kb, 0)};
+    bf16x8 fk[2], fl[2], fv[2];
+    fk[0] = op.row(tk, 32 * kb, 0);
+    if (ROT) fl[0] = op.row(tk2, 32 * kb, 0);
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       if (k + 1 < D / 16) {
         fk[(k + 1) & 1] = op.row(tk, 32 * kb, k + 1);
-        fv[(k + 1) & 1] = op.row(tv, 32 * kb, k + 1);
+        if (ROT) fl[(k + 1) & 1] = op.row(tk2, 32 * kb, k + 1);
+      }
+      if (ROT) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fl[k & 1], qf[k], s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[k & 1], ql[k], s, 0, 0, 0);
       }
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[k & 1], qf[k], s, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    fv[0] = op.row(tv, 32 * kb, 0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dp[i] = nd;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      if (k + 1 < D / 16) fv[(k + 1) & 1] = op.row(tv, 32 * kb, k + 1);
       dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[k & 1], df[k], dp, 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
     fk[0] = op.column(tk, 32 * kb, 0);
-    fk[1] = op.column(tk, 32 * kb, 1);
+    if (ROT) fl[0] = op.column(tk2, 32 * kb, 0);
     __builtin_amdgcn_sched_barrier(0);
-    if (ALIBI) {
-      const float base = slope * (float)(b0 + 32 * kb + 4 * h2 - qpos);
+    const int first = 32 * kb + 4 * h2;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = fmaf(slope, (float)(8 * (i >> 2) + (i & 3)), s[i] + base);
+    for (int i = 0; i < 16; ++i) {
+      // The bias and the log-sum-exp may be large next to their difference: one rounding for both.
+      const float y = ALIBI ? fmaf(slope, (float)(b0 - qpos + first + 8 * (i >> 2) + (i & 3)), nl) * kLog2e : nl;
+      dp[i] *= fast_exp2(fmaf(s[i], scale_log2, y));
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) dp[i] *= fast_exp2(s[i]);
     if (masked) {
-      const int last = (causal ? min(nvalid - 1, qpos - b0) : nvalid - 1) - 32 * kb - 4 * h2;
+      const int last = (causal ? min(nvalid - 1, qpos - b0) : nvalid - 1) - first;
 #pragma unroll
       for (int i = 0; i < 16; ++i) dp[i] = 8 * (i >> 2) + (i & 3) <= last ? dp[i] : 0.f;
     }
@@ -546,15 +631,20 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       float y[8];
+      u32x4 hi, lo;
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = dp[8 * k + e];
-      const bf16x8 sf = as_bf16x8(pack8(y));
+      split8(y, hi, lo);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
-        const int at = k * (D / 32) + db, ahead = at + 2;
-        dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[at & 1], sf, dq[db], 0, 0, 0);
-        if (ahead < 2 * (D / 32))
-          fk[at & 1] = op.column(tk, 32 * kb + 16 * (ahead / (D / 32)), ahead % (D / 32));
+        const int at = k * (D / 32) + db, ahead = at + 1;
+        if (ahead < 2 * (D / 32)) {
+          fk[ahead & 1] = op.column(tk, 32 * kb + 16 * (ahead / (D / 32)), ahead % (D / 32));
+          if (ROT) fl[ahead & 1] = op.column(tk2, 32 * kb + 16 * (ahead / (D / 32)), ahead % (D / 32));
+        }
+        if (ROT) dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fl[at & 1], as_bf16x8(hi), dq[db], 0, 0, 0);
+        dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[at & 1], as_bf16x8(lo), dq[db], 0, 0, 0);
+        dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[at & 1], as_bf16x8(hi), dq[db], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -562,17 +652,16 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
   }
 }
 
-// Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q and dO in
-// registers; K (rotated) and V pass through LDS, K read by rows and transposed.  Eight waves share a tile's loads and
-// rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same ragged requests 0.89
-// ms for three products (830 TFLOP/s), the 64-row questions 82 us.  Two row blocks a wave spilled 150 registers (six times
-// as long).  A request in one key split has its whole sums here: they are turned back and written at once.
+// Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q (both parts) and dO in
+// registers; K (rotated, both parts) and V pass through LDS, K read by rows and transposed.  Eight waves share a tile's loads
+// and rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same ragged requests 2.1
+// ms for seven products (820 TFLOP/s), the 64-row questions 170 us.  A request in one key split has its whole sums here: they
+// are turned back and written at once.
 template <int D, int KMI, int NW, int NBUF>
-__device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
+__device__ __forceinline__ void query_gradients(const GradArgs& a, int id, GradQSmem<D, KMI, NBUF>& sm) {
   constexpr int KM = keys_of(KMI), NT = NW * 64;
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
   using S = TileLayout<D>;
-  __shared__ GradQSmem<D, NBUF> sm;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), h2 = lane >> 5, g = id % a.hkv;
   const GradRowItem item = a.row_items[id / a.hkv];
   const int r = item.request;
@@ -581,15 +670,17 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
   const int src = qs * a.group + min(pr, nrows - 1), tok = token_of(src, a.group_magic), qpos = tok + shift;
   const uint16_t* qrow = a.ws_q + ((int64_t)g * a.rows + src) * D;
   const uint16_t* drow = a.ws_do + ((int64_t)g * a.rows + src) * D;
-  bf16x8 qf[D / 16], df[D / 16];
+  const int64_t second = a.hkv * a.rows * D;
+  bf16x8 qf[D / 16], ql[D / 16], df[D / 16];
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
     qf[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + 16 * s + 8 * h2));
+    if (ROT) ql[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + second + 16 * s + 8 * h2));
     df[s] = as_bf16x8(*reinterpret_cast<const u32x4*>(drow + 16 * s + 8 * h2));
   }
   const float* in = a.ws_info + (int64_t)g * a.rows + src;
   const float nl = pr < nrows ? in[0] : -INFINITY, nd = in[a.hkv * a.rows];
-  const float slope = ALIBI ? alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f) : 0.f;
+  const float slope = ALIBI ? alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, kLog2e) : 0.f;
   f32x16 dq[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) dq[db] = f32x16{};
@@ -626,7 +717,7 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
     have_ahead = ahead.seek(a.causal, qmax);
     if (have_ahead) base(sm.csb[1][0], ahead);
     __syncthreads();
-    ld.store(sm.k[0], sm.v[0], sm.csb[0][0], sm.csd);
+    ld.store(sm.k[0], sm.k[0] + kSub * D, sm.v[0], sm.csb[0][0], sm.csd);
     if (early && have_ahead) fetch(ahead);
     __syncthreads();
   }
@@ -640,14 +731,14 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
       it.step();
       have_next = it.seek(a.causal, qmax);
       __syncthreads();
-      ld.store(sm.k[0], sm.v[0], sm.csb[0][0], sm.csd);
+      ld.store(sm.k[0], sm.k[0] + kSub * D, sm.v[0], sm.csb[0][0], sm.csd);
       __syncthreads();
       if (have_next) fetch(it);
     } else {
       buf = parity;
       it = ahead;
       have_next = have_ahead;
-      if (early && have_next) ld.store(sm.k[parity ^ 1], sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
+      if (early && have_next) ld.store(sm.k[parity ^ 1], sm.k[parity ^ 1] + kSub * D, sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
       if (have_next) {
         if (!early) fetch(it);
         ahead.step();
@@ -655,10 +746,11 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
         if (early && have_ahead) fetch(ahead);
       }
     }
-    grad_tile<D, ALIBI>(sm.k[buf], sm.v[buf], lane, qf, df, dq, nl, nd, slope, qpos, b0, nvalid, qmin, a.causal);
+    grad_tile<D, ALIBI>(sm.k[buf], sm.v[buf], lane, qf, ql, df, dq, a.scale_log2, nl, nd, slope, qpos, b0, nvalid, qmin,
+                        a.causal);
     if (NBUF == 2) {
       if (have_ahead) base(sm.csb[parity][0], ahead);
-      if (!early && have_next) ld.store(sm.k[parity ^ 1], sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
+      if (!early && have_next) ld.store(sm.k[parity ^ 1], sm.k[parity ^ 1] + kSub * D, sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
       __syncthreads();
       parity ^= 1;
     }
@@ -728,16 +820,20 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id) {
 }
 template <int D, int KMI, int NW, int NBUF>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_q(GradArgs a) {
-  query_gradients<D, KMI, NW, NBUF>(a, blockIdx.x);
+  __shared__ GradQSmem<D, KMI, NBUF> sm;
+  query_gradients<D, KMI, NW, NBUF>(a, blockIdx.x, sm);
 }
 // Both in one launch, the first `tiles` workgroups for keys and values.
 template <int D, int KMI>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, D == 64 ? 2 : 1)))
-void grad_all(GradArgs a, int tiles) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_all(GradArgs a, int tiles) {
+  __shared__ union {
+    KeySmem<D, KMI> keys;
+    GradQSmem<D, KMI, 1> queries;
+  } sm;
   if ((int)blockIdx.x < tiles)
-    key_gradients<D, KMI>(a, blockIdx.x);
+    key_gradients<D, KMI, false>(a, blockIdx.x, sm.keys, nullptr);
   else
-    query_gradients<D, KMI, 4, 1>(a, blockIdx.x - tiles);
+    query_gradients<D, KMI, 4, 1>(a, blockIdx.x - tiles, sm.queries);
 }
 
 // Keys of a tile's parts that a workgroup sums, and workgroups a (tile, KV head).

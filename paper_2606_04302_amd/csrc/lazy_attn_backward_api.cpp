@@ -24,7 +24,7 @@ extern "C" int lazy_attn_prefill_backward(const lazy_attn_params_t* p, const voi
   if (!q_start || !q_pos0 || !chunk_start || !plan || ((uintptr_t)plan & 15u)) return LAZY_EINVAL;
   if (total_q > 0 && (!q || !out || !lse || !dout || !dq)) return LAZY_EINVAL;
   if (info->num_tiles > 0 && (!k_pool || !v_pool || !chunks || !dk_pool || !dv_pool)) return LAZY_EINVAL;
-  const lazy::GradWorkLayout ws(p->num_q_heads, p->num_kv_heads, p->head_dim, *info);
+  const lazy::GradWorkLayout ws(p->num_q_heads, p->num_kv_heads, p->head_dim, lazy::query_parts(p), *info);
   if (ws.bytes > 0 && (!workspace || workspace_bytes < ws.bytes || ((uintptr_t)workspace & 15u)))
     return LAZY_EWORKSPACE;
   // The keys and values are read again after the first gradients are written.
@@ -66,6 +66,8 @@ extern "C" int lazy_attn_prefill_backward(const lazy_attn_params_t* p, const voi
   a.group_magic = a.group == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
   a.causal = p->causal;
   a.rotate_q = !p->q_prerotated && p->rope_style != LAZY_ALIBI;
+  a.parts = lazy::query_parts(p);
+  a.lse_scale = p->rope_style == LAZY_ALIBI ? 1.f : 1.4426950408889634f;
   lazy::rope_revolutions(p, a.rev);
   a.scale_log2 = lazy::scale_log2(p);
   const hipError_t err =

@@ -375,5 +375,5 @@ extern "C" int lazy_attn_backward_plan(const lazy_attn_params_t* params, const i
 extern "C" size_t lazy_attn_backward_workspace_size(const lazy_attn_params_t* params,
                                                     const lazy_backward_info_t* info) {
   if (lazy::check_params(params) != LAZY_OK || !info) return 0;
-  return lazy::GradWorkLayout(params->num_q_heads, params->num_kv_heads, params->head_dim, *info).bytes;
+  return lazy::GradWorkLayout(params->num_q_heads, params->num_kv_heads, params->head_dim, lazy::query_parts(params), *info).bytes;
 }

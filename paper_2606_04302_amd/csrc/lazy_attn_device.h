@@ -25,6 +25,7 @@ constexpr int kThreads = 256;
 constexpr int kSub = 64;  // keys of one loader sub-tile; tile row 0 of a sub-tile is a multiple of 64 in its chunk
 constexpr int kPad = 8;   // bf16 elements of padding per LDS row
 constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.4426950408889634f;
 // The softmax reference max only moves when a tile's max exceeds it by more than this (log2 units): unnormalised
 // probabilities stay below 2^8, far inside fp32 and bf16 range, and the O accumulator is rescaled rarely.
 constexpr float kRescaleSlack = 8.0f;

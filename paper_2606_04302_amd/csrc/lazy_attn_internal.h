@@ -94,11 +94,12 @@ struct GradArgs {
   uint16_t* dq;                // [total_q][hq][D]
   uint16_t* dk_pool;
   uint16_t* dv_pool;
-  uint16_t* ws_q;              // [hkv][rows][D] rotated queries times scale * log2 e, pairs in half-split order
+  uint16_t* ws_q;              // [parts][hkv][rows][D] rotated queries as the sum of `parts` bf16 numbers, pairs in
+                               // half-split order
   uint16_t* ws_do;             // [hkv][rows][D] dout
-  float* ws_info;              // [2][hkv][rows] -lse log2 e, then -delta
+  float* ws_info;              // [2][hkv][rows] -lse * lse_scale, then -delta
   float* ws_dq;                // [row_slots][hkv][rows][D]
-  float* ws_parts;             // [num_parts][hkv][dk, dv][64][D]
+  float* ws_parts;             // [num_parts][hkv][kGradHalves][dk, dv][64][D]
   const float* inv_freq;       // [D/2] or null; ALiBi: [hq] slopes or null
   int64_t rows;
   int32_t hq;
@@ -107,6 +108,8 @@ struct GradArgs {
   uint32_t group_magic;        // ceil(2^32 / group), 0 for group 1
   int32_t causal;
   int32_t rotate_q;            // 0: queries arrive rotated, or nothing is (ALiBi)
+  int32_t parts;               // 2, or 1 with ALiBi: nothing is rotated, one part is exact
+  float lse_scale;             // log2 e, or 1 with ALiBi, whose kernels add the bias first
   float scale_log2;
   double rev[64];              // rotations per position of each pair, in revolutions (unused with inv_freq)
 };

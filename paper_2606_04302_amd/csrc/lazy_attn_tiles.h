@@ -159,19 +159,6 @@ __device__ __forceinline__ void rotate_pairs(const u32x4& a, const u32x4& b, int
     }
   }
 }
-// Rounded to bf16 (ALiBi: only interleaved pairs would be split, and it has none).
-template <int D, int KM, bool IL, class Rows>
-__device__ __forceinline__ void rotate_keys(u32x4 (&kf)[D / 16], int h2, const float2* base, Rows rows) {
-  if (KM == kKeysAlibi) return;
-#pragma unroll
-  for (int s = 0; s < D / 32; ++s) {
-    float yl[8], yh[8];
-    rotate_pairs<D, KM, IL>(kf[s], kf[s + D / 32], 16 * s + 8 * h2, base, rows, yl, yh);
-    kf[s] = pack8(yl);
-    kf[s + D / 32] = pack8(yh);
-    if (s & 1) __builtin_amdgcn_sched_barrier(0);
-  }
-}
 // As two bf16 parts.
 template <int D, int KM, bool IL, class Rows>
 __device__ __forceinline__ void rotate_keys_split(u32x4 (&kh)[D / 16], u32x4 (&kl)[D / 16], int h2, const float2* base,

@@ -1,0 +1,112 @@
+"""Gradients of concentrated attention.  Where few rows see many keys and a handful of keys hold nearly all of a row's
+weight, the elements of a gradient are much smaller than the terms they are summed from and much larger than the
+tensor's root mean square: an error of half a bf16 step in the operands of a product (queries, keys, P, dS) shows as a
+multiple of both.  Every element has to be right to half a step of its own plus what two-part operands and fp32 sums
+allow (``operand`` in ``oracle/gradient_oracle.py``).
+
+Over a tensor: a rounding to bf16 has a root mean square of at most 2^-8 / sqrt(3) = 0.00226 relative, the result's own;
+operands add 2^-15 at most.  0.0023 of the 2-norm is allowed.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import gradient_oracle as GO
+from paper_2606_04302_amd import ops
+from paper_2606_04302_amd import workloads as W
+from tests.test_backward import cover_masks, make_plan, oracle_kw, shared
+
+REL = 0.0023
+OPERAND = 2.0 ** -15
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    ops.lib()
+    torch.cuda.init()
+
+
+def louder(w, factor):
+    """The workload with its queries multiplied: sharper scores."""
+    w.q[...] = (w.q.astype(np.float32) * factor).astype(w.q.dtype)
+    return w
+
+
+def long_context(seed, hq, hkv, d, keys, rows, gap=0):
+    """Some rows and their own keys behind many keys; with a gap no keys of their own, far from the others."""
+    own = [] if gap else [(rows, keys)]
+    return W.custom(seed, hq, hkv, d, 1.0e4, [dict(chunks=[("a", keys, 0), *own], q_len=rows, q_pos0=keys + gap)])
+
+
+def gradients(w, ckw, dlse, seed=0, fill=3.0):
+    """(dq, dk, dv) on the GPU, the oracle's gradients and their bounds."""
+    cfg = ops.config_of(w, **ckw)
+    dw = ops.upload(w)
+    out, lse = ops.run_lazy(dw, cfg)
+    gen = torch.Generator("cuda").manual_seed(seed)
+    dout = torch.empty_like(dw.q).normal_(generator=gen)
+    dl = torch.empty_like(lse).normal_(generator=gen) if dlse else None
+    plan = ops.upload_backward_plan(ops.backward_plan(cfg, w.q_start, w.q_pos0, w.chunks, w.chunk_start))
+    got = [torch.full_like(t, v) for t, v in ((dw.q, float("nan")), (dw.pool, fill), (dw.pool, fill))]
+    ops.prefill_backward(cfg, dw.q, dw.q_start, dw.q_pos0, dw.pool, dw.pool, dw.chunks, dw.chunk_start, out, lse, dout,
+                         plan, dlse=dl, dq=got[0], dk_pool=got[1], dv_pool=got[2])
+    torch.cuda.synchronize()
+    f64 = lambda t: t.float().cpu().numpy().astype(np.float64)  # noqa: E731
+    ref, bound = GO.lazy_backward(w.q, w.q_start, w.q_pos0, w.pool, w.pool, w.chunks, w.chunk_start, w.num_q_heads,
+                                  w.num_kv_heads, w.head_dim, w.rope_base, w.causal, f64(out), f64(lse), f64(dout),
+                                  f64(dl) if dlse else None, operand=OPERAND, **oracle_kw(ckw))
+    return [f64(t) for t in got], ref, bound
+
+
+def check(w, ckw, tag, dlse=False, fill=3.0):
+    got, ref, bound = gradients(w, ckw, dlse, fill=fill)
+    masks = (np.ones(ref[0].shape, bool), *cover_masks(w))
+    bad = []
+    for name, x, r, b, m in zip(("dq", "dk", "dv"), got, ref, bound, masks):
+        x = x.reshape(r.shape)
+        assert name == "dq" or (x[~m] == fill).all(), f"{tag}: {name} written outside the records"
+        x, r, b = x[m], r[m], b[m]
+        assert np.isfinite(x).all(), f"{tag} {name}"
+        err = np.abs(x - r)
+        rms = np.sqrt(np.mean(r * r))
+        worst, rel = (err / b).max(), np.linalg.norm(x - r) / np.linalg.norm(r)
+        print(f"{tag} {name}: largest error {(err / np.maximum(np.abs(r), rms)).max():.5f} of max(element, rms), "
+              f"{worst:.3f} of its bound; 2-norm {rel:.5f}", flush=True)
+        if worst > 1.0 or rel > REL:
+            bad.append((name, worst, rel))
+    assert not bad, f"{tag}: {bad}"
+
+
+IL, LOCAL, ALIBI = (dict(rope_style=ops.ROPE_INTERLEAVED), dict(key_positions=ops.KEYS_LOCAL),
+                    dict(rope_style=ops.ALIBI))
+CASES = {
+    "alibi, 3 rows, 28000 keys": (lambda: long_context(60, 32, 8, 128, 28000, 3), ALIBI),
+    "alibi d64, one row": (lambda: long_context(61, 8, 1, 64, 5000, 1), ALIBI),
+    "alibi, far from its keys": (lambda: long_context(62, 8, 2, 128, 500, 4, gap=20000), ALIBI),
+    "alibi, long question": (lambda: long_context(63, 8, 2, 128, 1500, 200), ALIBI),
+    "peaked": (lambda: louder(long_context(64, 8, 2, 128, 3000, 3), 4), {}),
+    "peaked d64": (lambda: louder(long_context(65, 8, 2, 64, 3000, 3), 4), {}),
+    "peaked, interleaved": (lambda: louder(long_context(66, 4, 2, 128, 3000, 7), 4), IL),
+    "peaked, interleaved local d64": (lambda: louder(long_context(67, 4, 2, 64, 3000, 7), 4), dict(IL, **LOCAL)),
+    "peaked, local": (lambda: louder(long_context(68, 4, 2, 128, 3000, 2), 4), LOCAL),
+    "peaked, prerotated": (lambda: louder(long_context(69, 8, 2, 128, 3000, 3), 4), dict(q_prerotated=True)),
+    "peaked, shared chunks": (lambda: louder(shared(70, 8, 2, 128, [130, 64, 33, 700], [17, 40, 3]), 4), {}),
+    "peaked, shared chunks d64": (lambda: louder(shared(71, 8, 2, 64, [130, 64, 33, 700], [17, 40, 3]), 4), {}),
+    "peaked, parts": (lambda: louder(shared(72, 4, 1, 128, [64], [300, 301], reqs=5), 4), {}),
+    "peaked, separate launches": (lambda: louder(shared(73, 32, 32, 128, [1030, 700, 517], [20, 33], reqs=2), 4), {}),
+    "peaked, 256 rows": (lambda: louder(shared(74, 64, 16, 128, [1030, 700, 517, 2000], [128, 60], reqs=2), 4), {}),
+    "peaked, separate launches d64": (lambda: louder(shared(75, 64, 64, 64, [1030, 700, 517, 500], [20, 33], reqs=2),
+                                                     4), {}),
+    "flat": (lambda: shared(76, 8, 2, 128, [1300, 640, 33], [64]), {}),
+    "flat d64": (lambda: shared(77, 8, 2, 64, [1300, 640, 33], [64]), {}),
+    "flat, not causal": (lambda: shared(78, 8, 2, 128, [130, 64], [64], causal=False), IL),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", CASES)
+def test_gradients_to_half_a_step(gpu, name):
+    make, ckw = CASES[name]
+    check(make(), ckw, name, dlse="shared" in name or "far" in name)
