@@ -11,14 +11,14 @@ namespace lazy {
 constexpr int kGradTileKeys = 64;  // stored keys of half a key-gradient tile
 constexpr int kGradHalves = 2;     // halves of a tile: 64 keys each, wherever they lie
 constexpr int kGradRows = 32;      // packed query rows (token * G + head in group) of one step over a tile
-// Do `tiles` and `items` workgroups (row items of 128 rows) share one launch?  It fills the chip with one kind's
-// workgroups while the other kind's last ones run, but holds both kinds' LDS and registers: a workgroup a CU at head_dim
-// 128, two instead of three at 64.  us apart / together, tiles + items.  128: 18 + 34 35.4 / 26.6, 136 + 176 53.5 (half as
-// many items, of 256 rows) / 43.3, 264 + 272 59.3 / 66.2, 392 + 320 65.6 / 74.6.  64: 136 + 272 39.0 / 29.9, 792 + 768
-// 115 / 101, 864 + 1256 249 / 235, 1176 + 624 83 / 77, 1816 + 768 137 / 142, 5020 + 2228 1086 / 1096.
-constexpr bool grads_together(int d, int64_t tiles, int64_t items) {
-  return tiles > 0 && items > 0 && (d == 64 ? tiles <= 1280 : tiles + items <= 512);
-}
+// Most workgroups (tiles and row items of 128 rows) for which one launch takes both kinds of items, where 256 rows a
+// workgroup would do (head_dim 128 and requests that fill them; otherwise both are one launch always).  One launch fills
+// the chip with one kind's workgroups while the other kind's last ones run; two let eight waves share a tile's loads and
+// rotation.  us one launch / two, tiles + items of 128 rows: 120 + 512 77 / 94, 328 + 432 92 / 94, 408 + 512 150 / 150, 656 +
+// 448 137 / 135, 1024 + 512 228 / 220, 760 + 512 424 / 406, 816 + 1024 1288 / 1237, 1408 + 512 404 / 380, 1280 + 4096 17.8 /
+// 16.8 ms; 840 + 1336 789 / 808.  With 128 rows: 136 + 136 37 / 46, 1824 + 480 180 / 194, 2176 + 512 430 / 446.  Head_dim 64: 136
+// + 136 25 / 32, 760 + 512 208 / 200, 816 + 1024 603 / 657, 1408 + 512 193 / 193, 2056 + 496 163 / 169, 1280 + 4096 8.4 / 8.6 ms.
+constexpr int64_t kMostTogether = 1024;
 
 // Up to 64 stored keys (key 0 of KV head 0 at k_off / v_off).
 struct GradHalf {

@@ -4,8 +4,8 @@
 // head in group), dO packed alike, and two numbers a row, -lse log2 e and -delta.  (2) grad_kv: dk and dv, one tile of the
 // store at a time.  (3) grad_q: dq, one row tile and key split at a time.  (4) finish: partial dq of requests in several key
 // splits summed, turned back and rounded, and the same for tiles whose uses were cut into parts; only where there are any.
-// Where there is little work (2) and (3) are one launch, grad_all (grads_together).  The probabilities are recomputed in (2)
-// and in (3): seven products of the two kernels against five if dq were summed over key tiles with atomics, whose order
+// (2) and (3) are one launch, grad_all, unless there is much work for 256 rows a workgroup (kMostTogether).  The
+// probabilities are recomputed in (2) and in (3): seven products of the two kernels against five if dq were summed over key tiles with atomics, whose order
 // would change results from call to call.
 //
 // Precision: rotated queries and keys, P and dS are each the sum of two bf16 numbers (split8, 2^-17), and a product of two
@@ -99,9 +99,8 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
 // by rows for S and dP and transposed for dV and dK.  -delta is dP's initial value.  dK is kept in the rotated frame of the
 // use at hand and turned on when the next use has another position.
 //
-// Two waves a SIMD (three at D = 64) hide each other's latencies.  At D = 64 the next 32 rows are copied to a second buffer
-// during the products; at D = 128 a second buffer would leave one workgroup a CU, and the other workgroup's products cover
-// the copies.  Bound by the products: 16 ragged requests, 2.2 TFLOP of nine products 2.1 ms (1050 TFLOP/s, 86% of the large
+// Two waves a SIMD hide each other's latencies, and one workgroup's products the other's copies: with a second buffer for
+// the next 32 rows, head_dim 128 would leave one workgroup a CU (64 with one and three workgroups: kMostTogether).  Bound by the products: 16 ragged requests, 2.2 TFLOP of nine products 2.1 ms (1050 TFLOP/s, 86% of the large
 // library product's rate); 8 requests of 64 rows a chunk 232 us, where a tile has 8 to 24 steps and its loads, rotations
 // and results are a third.
 
@@ -134,17 +133,13 @@ struct KeySmem {
   float2 turn[4][KM == kKeysAlibi ? 2 : KM == kKeysLocal ? RLD : 4 * RLD] __attribute__((aligned(16)));
   float2 place[KM == kKeysNope ? 8 * RLD : 2] __attribute__((aligned(16)));
 };
-// `other`: a second buffer of rows, a variable of its own (the compiler then knows that copies to one do not touch reads
-// of the other), or null.
-template <int D, int KMI, bool TWO>
-__device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem<D, KMI>& sm,
-                                              RowTiles<D, keys_of(KMI) != kKeysAlibi>* other) {
+template <int D, int KMI>
+__device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem<D, KMI>& sm) {
   constexpr int KM = keys_of(KMI);
   constexpr bool ALIBI = KM == kKeysAlibi, ROT = !ALIBI, LOCAL = KM == kKeysLocal, IL = interleaved_of(KMI);
   constexpr int C = D / 8;  // chunks of a row
   constexpr int COPIES = kGradRows * C / 256;
   constexpr int RLD = KeySmem<D, KMI>::RLD;
-  using Tiles = RowTiles<D, ROT>;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h2 = lane >> 5, g = id % a.hkv;
   const int hf = wave >> 1, k32 = 32 * (wave & 1), key = k32 + (lane & 31);
   const cptr<GradTile> tile = as_const(a.tiles) + id / a.hkv;
@@ -203,7 +198,8 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem
     return Use{u->row_begin, u->row_end, u->pos_shift, u->full_from, h->pos, h->record_pos, h->key_begin, h->key_end};
   };
 
-  const auto fetch = [&](const Step& step, Tiles& to) {
+  RowTiles<D, ROT>& tiles = sm.rows;
+  const auto fetch = [&](const Step& step) {
     const int row0 = step.row0, most = step.use.row_end - 1 - row0;  // rows past the use's end repeat its last one
     const uint16_t* q = qbase + (int64_t)row0 * D;
     const uint16_t* d = dbase + (int64_t)row0 * D;
@@ -212,15 +208,15 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem
     for (int i = 0; i < COPIES; ++i) {
       const int row = (256 * i + e0) / C, chunk = ((256 * i + e0) % C) ^ swizzle<D>(row);
       const int off = min(row, most) * D + 8 * chunk;
-      copy_async(q + off, to.q + 2048 * i + 512 * wave);
-      if (ROT) copy_async(q + second + off, to.q + kGradRows * D + 2048 * i + 512 * wave);
-      copy_async(d + off, to.d + 2048 * i + 512 * wave);
+      copy_async(q + off, tiles.q + 2048 * i + 512 * wave);
+      if (ROT) copy_async(q + second + off, tiles.q + kGradRows * D + 2048 * i + 512 * wave);
+      copy_async(d + off, tiles.d + 2048 * i + 512 * wave);
     }
     if (wave == 0)
-      copy_async4(ibase + (lane & 32 ? a.hkv * a.rows : 0) + row0 + min(lane & 31, most), to.in);
+      copy_async4(ibase + (lane & 32 ? a.hkv * a.rows : 0) + row0 + min(lane & 31, most), tiles.in);
   };
 
-  const auto compute = [&](const Step& step, const Tiles& tiles) {
+  const auto compute = [&](const Step& step) {
     const uint16_t *const tq = tiles.q, *const tq2 = tiles.q + kGradRows * D, *const td = tiles.d;
     const float* const in = tiles.in;
     const Use& seg = step.use;
@@ -390,27 +386,16 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem
       ahead = load_use(min(si + 1, seg_end - 1));
       return true;
     };
-    fetch(now, sm.rows);
+    fetch(now);
     while (true) {
-      bool more = advance();
+      const bool more = advance();
       wait_copies();
       __syncthreads();
-      if (TWO && more) fetch(next, *other);
-      if (active) compute(now, sm.rows);
+      if (active) compute(now);
       if (!more) break;
       now = next;
-      if (!TWO) {
-        __syncthreads();
-        fetch(now, sm.rows);
-        continue;
-      }
-      more = advance();
-      wait_copies();
       __syncthreads();
-      if (more) fetch(next, sm.rows);
-      if (active) compute(now, *other);
-      if (!more) break;
-      now = next;
+      fetch(now);
     }
   }
   wait_copies();
@@ -484,15 +469,10 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem
     wait_reads();
   }
 }
-template <int D, int KMI, int WPE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE, WPE))) void grad_kv(GradArgs a) {
+template <int D, int KMI>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_kv(GradArgs a) {
   __shared__ KeySmem<D, KMI> sm;
-  if constexpr (D == 64) {
-    __shared__ RowTiles<D, keys_of(KMI) != kKeysAlibi> other;
-    key_gradients<D, KMI, true>(a, blockIdx.x, sm, &other);
-  } else {
-    key_gradients<D, KMI, false>(a, blockIdx.x, sm, nullptr);
-  }
+  key_gradients<D, KMI>(a, blockIdx.x, sm);
 }
 
 // Loads a 64-key tile of K and V for a workgroup of NT threads, NT / 64 a key row, rotates the keys and writes both to
@@ -831,7 +811,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     GradQSmem<D, KMI, 1> queries;
   } sm;
   if ((int)blockIdx.x < tiles)
-    key_gradients<D, KMI, false>(a, blockIdx.x, sm.keys, nullptr);
+    key_gradients<D, KMI>(a, blockIdx.x, sm.keys);
   else
     query_gradients<D, KMI, 4, 1>(a, blockIdx.x - tiles, sm.queries);
 }
@@ -916,18 +896,11 @@ hipError_t launch(const GradArgs& a, const lazy_backward_info_t& i, hipStream_t 
   constexpr bool IL = interleaved_of(KMI);
   if (i.num_blocks) prepare_rows<D, IL><<<i.num_blocks, 256, 0, stream>>>(a);
   const int tiles = i.num_tiles * a.hkv, items = i.num_row_items * a.hkv;
-  const bool together = i.row_blocks == 1 && grads_together(D, tiles, items);
-  if (together) grad_all<D, KMI><<<tiles + items, 256, 0, stream>>>(a, tiles);
-  if (tiles && !together) grad_kv<D, KMI, D == 64 ? 3 : 2><<<tiles, 256, 0, stream>>>(a);
-  if (items && !together) {
-    if constexpr (D == 128) {
-      if (i.row_blocks == 2)
-        grad_q<D, KMI, 8, 2><<<items, 512, 0, stream>>>(a);
-      else
-        grad_q<D, KMI, 4, 1><<<items, 256, 0, stream>>>(a);
-    } else {
-      grad_q<D, KMI, 4, 2><<<items, 256, 0, stream>>>(a);
-    }
+  if (i.row_blocks == 1) {
+    if (tiles + items) grad_all<D, KMI><<<tiles + items, 256, 0, stream>>>(a, tiles);
+  } else if constexpr (D == 128) {
+    if (tiles) grad_kv<D, KMI><<<tiles, 256, 0, stream>>>(a);
+    if (items) grad_q<D, KMI, 8, 2><<<items, 512, 0, stream>>>(a);
   }
   const int merges = i.num_merges * a.hkv * kMergeBlocks, blocks = i.row_slots > 1 ? i.num_blocks : 0;
   if (blocks + merges) finish<D, IL><<<blocks + merges, 256, 0, stream>>>(a, blocks);

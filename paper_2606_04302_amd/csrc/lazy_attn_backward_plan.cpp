@@ -51,14 +51,15 @@ int64_t steps_of(const GradSeg& s) { return (s.row_end - s.row_begin + kGradRows
 // one with the least estimated time is taken: the makespan of the items, longest first, on the workgroups that the chip
 // holds, where an item costs its tiles and kItemTiles more (its prologue and its result), plus the partial results'
 // way to memory and back and kFinishUs for the launch that adds them up (a request in one split writes its gradient by
-// itself; with 0 in its place 32 heads of 64 over 1088 keys took 29.3 us instead of 24.4, of 128 over 2112 keys 47.5
-// instead of 42.9).  A tile of 256 rows takes a workgroup 3.7 us at head_dim 128.
-// More splits are taken for a gain of 3% only (16 ragged requests of 17K keys: 1792 items on an estimate 2% below that of
-// 464 took as long, and their partial results 26 us more).
-constexpr double kItemTiles = 3, kTileUs = 3.7, kBytesPerUs = 4.5e6, kFinishUs = 15, kClose = 0.97;
+// itself).  A tile of 256 rows takes a workgroup 8.8 us at head_dim 128.  With 3.7 instead, which splits less, one document
+// of 1024 tokens and 32 / 8 heads took 166 us instead of 151 (head_dim 64: 87 instead of 75), 16 heads of 64 over one KV head
+// and 800 tokens 57 instead of 52; but 512 tokens 68 instead of 70 (64: 38 instead of 42), 16 / 1 heads of 128 and 1024
+// tokens 102 instead of 115.  kItemTiles of 1.5 to 3 are within 2% of each other but for one document (512 tokens: 76 with
+// 1.5, 70 with 3).  More splits are taken for a gain of 3% only.
+constexpr double kItemTiles = 3, kTileUs = 8.8, kBytesPerUs = 4.5e6, kFinishUs = 15, kClose = 0.97;
 std::vector<int32_t> row_splits(const std::vector<int64_t>& key_tiles, const int32_t* q_start, int batch, int G, int hkv,
                                 int d, int row_blocks) {
-  const int slots = lazy::kNumCUs * (row_blocks == 2 ? 1 : d == 64 ? 3 : 2);
+  const int slots = lazy::kNumCUs * (row_blocks == 2 ? 1 : 2);
   const int64_t bm = 128 * row_blocks;
   const double tile_us = kTileUs * (row_blocks / 2.0) * (d / 128.0) * (slots / (double)lazy::kNumCUs);
   const int64_t longest = batch > 0 ? *std::max_element(key_tiles.begin(), key_tiles.end()) : 0;
@@ -273,7 +274,8 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
   for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
   std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return cost[a] > cost[b]; });
 
-  // Query gradient: 256 rows a workgroup (eight waves; head_dim 128 only) where requests fill such tiles, else 128.
+  // Query gradient: 128 rows a workgroup, in one launch with the tiles, or 256 (eight waves; head_dim 128 only) in one of
+  // its own where requests fill such row tiles and there is more work than kMostTogether.
   int64_t rows1 = 0, rows2 = 0;
   std::vector<int64_t> key_tiles(batch);
   for (int r = 0; r < batch; ++r) {
@@ -283,16 +285,15 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
     for (int i = chunk_start[r]; i < chunk_start[r + 1]; ++i)
       key_tiles[r] += lazy::ceil_div(chunks[i].len, kGradTileKeys);
   }
-  int row_blocks = d == 128 && 4 * rows2 <= 5 * rows1 ? 2 : 1;
-  std::vector<int32_t> splits_of = row_splits(key_tiles, q_start, batch, G, hkv, d, row_blocks);
-  if (row_blocks == 2) {  // little work: 128 rows too, so that one launch takes both kinds of items
-    const std::vector<int32_t> other = row_splits(key_tiles, q_start, batch, G, hkv, d, 1);
+  int row_blocks = 1;
+  std::vector<int32_t> splits_of = row_splits(key_tiles, q_start, batch, G, hkv, d, 1);
+  if (d == 128 && rows1 > 0 && 4 * rows2 <= 5 * rows1) {
     int64_t items = 0;
     for (int r = 0; r < batch; ++r)
-      items += lazy::ceil_div((int64_t)(q_start[r + 1] - q_start[r]) * G, 128) * other[r];
-    if (lazy::grads_together(d, (int64_t)out_tiles.size() * hkv, items * hkv)) {
-      row_blocks = 1;
-      splits_of = other;
+      items += lazy::ceil_div((int64_t)(q_start[r + 1] - q_start[r]) * G, 128) * splits_of[r];
+    if (((int64_t)out_tiles.size() + items) * hkv > lazy::kMostTogether) {
+      row_blocks = 2;
+      splits_of = row_splits(key_tiles, q_start, batch, G, hkv, d, 2);
     }
   }
   const int bm = 128 * row_blocks;
@@ -318,9 +319,9 @@ int make_plan(const lazy_attn_params_t* p, const int32_t* q_start, const int32_t
   for (size_t i = 0; i < row_order.size(); ++i) row_order[i] = (int32_t)i;
   std::stable_sort(row_order.begin(), row_order.end(), [&](int32_t a, int32_t b) { return row_cost[a] > row_cost[b]; });
 
-  // Launches of 256 threads a tile and a block, 512 a row item, and eight workgroups a merged tile.
+  // Launches of 256 threads a tile, row item (512 with 256 rows) and block, and eight workgroups a merged tile.
   const size_t most = (size_t)lazy::kMaxGroups - 64;
-  if (out_tiles.size() * (size_t)hkv > most || 2 * rows.size() * (size_t)hkv > most || out_segs.size() > INT32_MAX ||
+  if ((out_tiles.size() + 2 * rows.size()) * (size_t)hkv > most || out_segs.size() > INT32_MAX ||
       blocks.size() + 8 * merges.size() * (size_t)hkv > most)
     return LAZY_EUNSUPPORTED;
   *info = {};

@@ -14,7 +14,7 @@ import torch
 from oracle import gradient_oracle as GO
 from paper_2606_04302_amd import ops
 from paper_2606_04302_amd import workloads as W
-from tests.test_backward import cover_masks, make_plan, oracle_kw, shared
+from tests.test_backward import arrays, cover_masks, make_plan, oracle_kw, shared
 
 REL = 0.0023
 OPERAND = 2.0 ** -15
@@ -95,10 +95,9 @@ CASES = {
     "peaked, shared chunks": (lambda: louder(shared(70, 8, 2, 128, [130, 64, 33, 700], [17, 40, 3]), 4), {}),
     "peaked, shared chunks d64": (lambda: louder(shared(71, 8, 2, 64, [130, 64, 33, 700], [17, 40, 3]), 4), {}),
     "peaked, parts": (lambda: louder(shared(72, 4, 1, 128, [64], [300, 301], reqs=5), 4), {}),
-    "peaked, separate launches": (lambda: louder(shared(73, 32, 32, 128, [1030, 700, 517], [20, 33], reqs=2), 4), {}),
+    "peaked, many tiles": (lambda: louder(shared(73, 32, 32, 128, [1030, 700, 517], [20, 33], reqs=2), 4), {}),
     "peaked, 256 rows": (lambda: louder(shared(74, 64, 16, 128, [1030, 700, 517, 2000], [128, 60], reqs=2), 4), {}),
-    "peaked, separate launches d64": (lambda: louder(shared(75, 64, 64, 64, [1030, 700, 517, 500], [20, 33], reqs=2),
-                                                     4), {}),
+    "peaked, many tiles d64": (lambda: louder(shared(75, 64, 64, 64, [1030, 700, 517, 500], [20, 33], reqs=2), 4), {}),
     "flat": (lambda: shared(76, 8, 2, 128, [1300, 640, 33], [64]), {}),
     "flat d64": (lambda: shared(77, 8, 2, 64, [1300, 640, 33], [64]), {}),
     "flat, not causal": (lambda: shared(78, 8, 2, 128, [130, 64], [64], causal=False), IL),
@@ -110,3 +109,45 @@ CASES = {
 def test_gradients_to_half_a_step(gpu, name):
     make, ckw = CASES[name]
     check(make(), ckw, name, dlse="shared" in name or "far" in name)
+
+
+def uneven(seed, hq, hkv, d, keys, rows):
+    """One request with many keys, others with few."""
+    return W.custom(seed, hq, hkv, d, 1.0e4, [dict(chunks=[(n, 0), (rows, n)], q_len=rows, q_pos0=n) for n in keys])
+
+
+# Plans of each kind: (workload, options, rows of a workgroup, key splits of the requests).
+PLANS = {
+    "one split and several": (lambda: uneven(80, 8, 2, 128, [4000, 50, 700], 24), {}, 128, "both"),
+    "one split and several, interleaved d64": (lambda: uneven(81, 8, 2, 64, [4000, 50, 700], 24), IL, 128, "both"),
+    "256 rows, one split": (lambda: shared(82, 64, 16, 128, [180, 60], [64], reqs=40), {}, 256, "one"),
+    "256 rows, one split, interleaved local": (lambda: shared(83, 64, 16, 128, [180, 60], [64], reqs=40),
+                                               dict(IL, **LOCAL), 256, "one"),
+    "256 rows, one split, alibi": (lambda: shared(84, 64, 16, 128, [180, 60], [64], reqs=40), ALIBI, 256, "one"),
+    "256 rows, one split and several": (lambda: uneven(85, 64, 16, 128, [6000, 50] + [300] * 10, 64), {}, 256, "both"),
+    "d64, many rows, one split": (lambda: shared(86, 32, 32, 64, [500, 130], [150], reqs=12), {}, 128, "one"),
+    "d64 document": (lambda: W.custom(87, 4, 1, 64, 1.0e4, [dict(chunks=[(3001, 0)], q_len=3001, q_pos0=0)]), {}, 128,
+                     None),
+}
+
+
+def splits_of(plan, w):
+    rows = arrays(plan)[1]
+    return {int(rows["splits"][rows["request"] == r][0]) for r in range(w.batch)}
+
+
+@pytest.mark.parametrize("name", PLANS)
+def test_plans_are_of_their_kind(name):
+    make, ckw, rows, kind = PLANS[name]
+    w = make()
+    plan = make_plan(w, **ckw)[1]
+    assert 128 * plan.info.row_blocks == rows
+    got = splits_of(plan, w)
+    assert kind is None or (got == {1} if kind == "one" else 1 in got and max(got) > 1), got
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", PLANS)
+def test_gradients_of_every_kind_of_plan(gpu, name):
+    make, ckw, _, _ = PLANS[name]
+    check(make(), ckw, name, dlse="interleaved" in name)
