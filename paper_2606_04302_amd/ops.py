@@ -262,14 +262,15 @@ def prefill(cfg: Config, q, q_start, q_pos0, k_pool, v_pool, chunks, chunk_start
     _need(chunk_start.numel() == batch + 1 and q_pos0.numel() == batch, "table sizes disagree with the batch")
     total_q = q.shape[0]
     if out is None:
-        out = torch.empty_like(q)
+        with _allocating_for(stream):
+            out = torch.empty_like(q)
     _dev(out, torch.bfloat16, "out")
     _need(out.shape == q.shape, "out must have the shape of q")
     if lse is not None:
         _dev(lse, torch.float32, "lse")
         _need(lse.shape == (total_q, cfg.num_q_heads), "lse must be [T, Hq]")
     nbytes = prefill_workspace_size(cfg, batch, total_q, max_q_len, max_kv_len)
-    workspace = _workspace(nbytes, q.device, workspace)
+    workspace = _workspace(nbytes, q.device, workspace, stream)
     p = cfg.c()
     fn = lib().lazy_plain_attn_prefill if plain else lib().lazy_attn_prefill
     _check(fn(ctypes.byref(p), q.data_ptr(), q_start.data_ptr(), q_pos0.data_ptr(), k_pool.data_ptr(),
@@ -292,13 +293,14 @@ def decode(cfg: Config, q, q_pos, k_pool, v_pool, chunks, chunk_start, max_kv_le
     batch = q.shape[0]
     _need(chunk_start.numel() == batch + 1 and q_pos.numel() == batch, "table sizes disagree with the batch")
     if out is None:
-        out = torch.empty_like(q)
+        with _allocating_for(stream):
+            out = torch.empty_like(q)
     _dev(out, torch.bfloat16, "out")
     if lse is not None:
         _dev(lse, torch.float32, "lse")
         _need(lse.shape == (batch, cfg.num_q_heads), "lse must be [B, Hq]")
     nbytes = decode_workspace_size(cfg, batch, max_kv_len)
-    workspace = _workspace(nbytes, q.device, workspace)
+    workspace = _workspace(nbytes, q.device, workspace, stream)
     p = cfg.c()
     fn = lib().lazy_plain_attn_decode if plain else lib().lazy_attn_decode
     _check(fn(ctypes.byref(p), q.data_ptr(), q_pos.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
@@ -345,7 +347,8 @@ def combine(part_o, part_lse, out=None, lse=None, stream=None):
     s, rows, d = part_o.shape
     _need(part_lse.shape == (s, rows), "part_lse must be [S, rows]")
     if out is None:
-        out = torch.empty((rows, d), dtype=torch.bfloat16, device=part_o.device)
+        with _allocating_for(stream):
+            out = torch.empty((rows, d), dtype=torch.bfloat16, device=part_o.device)
     _dev(out, torch.bfloat16, "out")
     if lse is not None:
         _dev(lse, torch.float32, "lse")
@@ -581,11 +584,13 @@ def materialize_k(cfg: Config, k_pool, chunks, max_chunk_len: int, total_kv: int
     _dev(k_pool, torch.bfloat16, "k_pool")
     _chunks(chunks)
     n = chunks.numel() // 32
-    if k_out is None:
-        k_out = torch.empty(max(1, cfg.num_kv_heads * total_kv * cfg.head_dim), dtype=torch.bfloat16,
-                            device=k_pool.device)
-    if chunks_out is None:
-        chunks_out = torch.empty_like(chunks)
+    if k_out is None or chunks_out is None:
+        with _allocating_for(stream):
+            if k_out is None:
+                k_out = torch.empty(max(1, cfg.num_kv_heads * total_kv * cfg.head_dim), dtype=torch.bfloat16,
+                                    device=k_pool.device)
+            if chunks_out is None:
+                chunks_out = torch.empty_like(chunks)
     _dev(k_out, torch.bfloat16, "k_out")
     _chunks(chunks_out)
     _need(k_out.numel() >= cfg.num_kv_heads * total_kv * cfg.head_dim, "k_out too small")
@@ -729,13 +734,14 @@ def decode_shared(cfg: Config, q, q_pos, k_pool, v_pool, plan: DevicePlan, out=N
     batch = q.shape[0]
     _need(q_pos.numel() == batch and plan.slot_start.numel() == batch + 1, "table sizes disagree with the batch")
     if out is None:
-        out = torch.empty_like(q)
+        with _allocating_for(stream):
+            out = torch.empty_like(q)
     _dev(out, torch.bfloat16, "out")
     if lse is not None:
         _dev(lse, torch.float32, "lse")
         _need(lse.shape == (batch, cfg.num_q_heads), "lse must be [B, Hq]")
     nbytes = decode_shared_workspace_size(cfg, batch, plan.max_slots)
-    workspace = _workspace(nbytes, q.device, workspace)
+    workspace = _workspace(nbytes, q.device, workspace, stream)
     p = cfg.c()
     _check(lib().lazy_attn_decode_shared(ctypes.byref(p), q.data_ptr(), q_pos.data_ptr(), k_pool.data_ptr(),
                                          v_pool.data_ptr(), plan.items.data_ptr(), plan.num_items,
@@ -799,7 +805,10 @@ def run_lazy(dw: DeviceWorkload, cfg: Config | None = None, with_lse: bool = Tru
     plain_chunks (from materialize_k) the plain (no K rotation) entry points run over the materialised keys."""
     w = dw.w
     cfg = cfg or dw.cfg
-    lse = torch.empty((w.total_q, w.num_q_heads), dtype=torch.float32, device=dw.q.device) if with_lse else None
+    lse = None
+    if with_lse:
+        with _allocating_for(kw.get("stream")):
+            lse = torch.empty((w.total_q, w.num_q_heads), dtype=torch.float32, device=dw.q.device)
     plain = plain_k is not None
     kp = plain_k if plain else dw.pool
     ch = plain_chunks if plain else dw.chunks
@@ -816,5 +825,5 @@ def run_materialized(dw: DeviceWorkload, cfg: Config | None = None, **kw):
     cfg = cfg or dw.cfg
     total_kv = int(w.chunks["len"].astype(np.int64).sum())
     k_out, ch_out = materialize_k(cfg, dw.pool, dw.chunks, int(w.chunks["len"].max()) if len(w.chunks) else 0,
-                                  total_kv)
+                                  total_kv, stream=kw.get("stream"))
     return run_lazy(dw, cfg, plain_k=k_out, plain_chunks=ch_out, **kw), (k_out, ch_out)
