@@ -192,8 +192,12 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        # The pointer alone: torch.cuda.current_stream() builds an object around it, 2 us a call.
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        # The pointer alone: torch.cuda.current_stream() builds an object around it, 2 us a call.  These two functions are
+        # no public ones: a torch without them, or with others of their names, takes the public way.
+        try:
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        except (AttributeError, TypeError):
+            return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 

@@ -83,6 +83,32 @@ def test_memory_is_allocated_for_the_stream_of_the_call(monkeypatch, name):
     assert library.streams and set(library.streams) == {stream}
 
 
+@pytest.mark.parametrize("missing", ["_cuda_getCurrentRawStream", "_cuda_getDevice"])
+@pytest.mark.parametrize("how", ["gone", "another"])
+def test_current_stream_without_the_functions_that_are_not_public(monkeypatch, missing, how):
+    class Public:
+        cuda_stream = 0xC0FFEE
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Public)
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.setattr(torch._C, name, lambda *a: 0, raising=False)
+    assert ops._stream(None) == 0
+    if how == "gone":
+        monkeypatch.delattr(torch._C, missing)
+    else:
+        monkeypatch.setattr(torch._C, missing, lambda one, two, three: 0)
+    assert ops._stream(None) == 0xC0FFEE
+    assert ops._stream(5) == 5 and ops._stream(Public) == 0xC0FFEE
+
+
+@pytest.mark.gpu
+def test_the_current_streams_pointer_is_the_public_one(gpu):
+    side = torch.cuda.Stream()
+    assert ops._stream(None) == torch.cuda.current_stream().cuda_stream
+    with torch.cuda.stream(side):
+        assert ops._stream(None) == side.cuda_stream
+
+
 @pytest.mark.gpu
 def test_forward_calls_on_another_stream_keep_their_memory(gpu):
     """Split decode and prefill on a stream that is still busy, while the current stream allocates and fills memory of
