@@ -285,8 +285,8 @@ LAZY_API size_t lazy_attn_backward_workspace_size(const lazy_attn_params_t* para
  *   dlse     [total_q][Hq] fp32, gradient by lse (a loss over merged partial results depends on it), or NULL
  *   dq       [total_q][Hq][D] bf16, fully overwritten
  *   dk_pool, dv_pool  bf16 bases laid out like k_pool and v_pool (they may be the same pointer, provided that no
- *            record's keys are another's values; they are not k_pool's or v_pool's own memory: LAZY_EINVAL if the
- *            same pointer).  Every key of every record is overwritten, with zeros where no query
+ *            record's keys are another's values; they share no memory with k_pool or v_pool: LAZY_EINVAL if the
+ *            same pointer; the sizes are not known here, other overlaps are the caller's to avoid).  Every key of every record is overwritten, with zeros where no query
  *            sees it; everything else is left as it was.
  *   workspace  at least lazy_attn_backward_workspace_size(...) bytes, 16-byte aligned.
  * Gradients are rounded to bf16 once, from fp32 sums; rotated queries and keys, P and dS keep 16 bits or more for the

@@ -214,6 +214,12 @@ def _dev(t, dtype, name):
     _need(t.is_contiguous(), f"{name} must be contiguous")
 
 
+def _apart(a, b):
+    """Do two contiguous tensors share no memory?"""
+    pa, pb = a.data_ptr(), b.data_ptr()
+    return pa + a.numel() * a.element_size() <= pb or pb + b.numel() * b.element_size() <= pa
+
+
 def _chunks(t):
     _need(t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.numel() % 32 == 0,
           "chunks must be a contiguous device uint8 tensor of 32-byte lazy_chunk_t records")
@@ -446,6 +452,9 @@ def prefill_backward(cfg: Config, q, q_start, q_pos0, k_pool, v_pool, chunks, ch
         _dev(t, torch.bfloat16, name)
         if t.shape != like.shape:
             raise ValueError(f"{name} must have the shape of what it is the gradient of")
+    # Keys and values are read again after the first gradients are written.
+    for t, name in ((dk_pool, "dk_pool"), (dv_pool, "dv_pool")):
+        _need(_apart(t, k_pool) and _apart(t, v_pool), f"{name} must not overlap k_pool or v_pool")
     p = cfg.c()
     p, info = ctypes.byref(p), ctypes.byref(plan.info)
     nbytes = lib().lazy_attn_backward_workspace_size(p, info)

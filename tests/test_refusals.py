@@ -1,0 +1,60 @@
+"""Calls that the binding refuses before anything is launched (host tensors and a stand-in library that succeeds)."""
+import pytest
+import torch
+
+from paper_2606_04302_amd import ops
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The names of the library's functions that were called; type and device checks are off."""
+    names = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                names.append(name)
+                return 64 if name.endswith("_size") else 0
+            return call
+
+    library = Library()
+    monkeypatch.setattr(ops, "lib", lambda: library)
+    monkeypatch.setattr(ops, "_dev", lambda *a: None)
+    monkeypatch.setattr(ops, "_chunks", lambda *a: None)
+    return names
+
+
+def bf16(*shape):
+    return torch.zeros(*shape, dtype=torch.bfloat16)
+
+
+def i32(*v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("which", ["dk_pool", "dv_pool"])
+@pytest.mark.parametrize("of", ["k_pool", "v_pool"])
+@pytest.mark.parametrize("shift", [-1, 0, 1, 999, 1000])
+def test_gradient_pools_may_not_overlap_the_pools(calls, which, of, shift):
+    """Not in part either: a view of the pool's memory, shifted.  Memory that only touches is fine."""
+    store = bf16(4000)
+    pools = dict(k_pool=store[1000:2000], v_pool=bf16(1000))
+    if of == "v_pool":
+        pools = dict(k_pool=pools["v_pool"], v_pool=pools["k_pool"])
+    grads = dict(dk_pool=bf16(1000), dv_pool=bf16(1000))
+    grads[which] = store[1000 + shift:2000 + shift]
+    q, lse = bf16(3, 2, 64), torch.zeros(3, 2)
+    plan = ops.BackwardPlan(torch.zeros(0, dtype=torch.uint8), ops.BackwardInfo())
+
+    def call():
+        ops.prefill_backward(ops.Config(2, 1, 64, 1e4), q, i32(0, 3), i32(0), pools["k_pool"], pools["v_pool"],
+                             torch.zeros(32, dtype=torch.uint8), i32(0, 1), q, lse, q, plan, **grads, stream=0,
+                             workspace=torch.zeros(64, dtype=torch.uint8))
+
+    if shift == 1000:
+        call()
+        assert calls[-1] == "lazy_attn_prefill_backward"
+    else:
+        with pytest.raises(ValueError, match=which):
+            call()
+        assert "lazy_attn_prefill_backward" not in calls
