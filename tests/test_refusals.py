@@ -48,7 +48,7 @@ def test_gradient_pools_may_not_overlap_the_pools(calls, which, of, shift):
 
     def call():
         ops.prefill_backward(ops.Config(2, 1, 64, 1e4), q, i32(0, 3), i32(0), pools["k_pool"], pools["v_pool"],
-                             torch.zeros(32, dtype=torch.uint8), i32(0, 1), q, lse, q, plan, **grads, stream=0,
+                             torch.zeros(32, dtype=torch.uint8), i32(0, 1), q, lse, q, plan, dq=q, **grads, stream=0,
                              workspace=torch.zeros(64, dtype=torch.uint8))
 
     if shift == 1000:
