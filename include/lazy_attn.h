@@ -310,13 +310,14 @@ LAZY_API int lazy_attn_prefill_backward(const lazy_attn_params_t* params, const 
  * Key weights.  Key j of request r (j counts the keys of its table in table order) has its number at
  * key_start[r] + j of an fp32 array; key_start [batch+1] int32 device, non-decreasing from 0, gives every request room
  * for key_start[r+1] - key_start[r] keys, which may be more than it has (a growing tail): what lies behind a request's
- * last key is neither read nor written, and keys without room are passed over.
+ * last key is neither read nor written, and keys without room are passed over.  key_start is trusted like the other tables:
+ * key_start[batch] is at most the arrays' size.
  *     weights_j = decay * weights_in_j + sum over the request's query tokens and all query heads of exp(s - lse)
  * with s the scaled score of the attention entry points (0 for hidden keys and for rows with lse = -inf, whatever
  * q holds there).  q, q_start,
  * q_pos0 (q_pos) and lse are what the attention call had and wrote; any rows of a prompt may be given, say its last
  * ones, as long as q_pos0 is the position of the first of them.
- *   weights_in  fp32 running sums, or NULL (then decay has no effect); may be the same array as weights
+ *   weights_in  fp32 running sums, or NULL (then decay has no effect); the same array as weights, or apart from it
  *   decay       finite, what the running sums are multiplied by (1: plain accumulation)
  *   num_keys    size of the weights arrays, key_start[batch] (the prefill form sizes its workspace by it)
  *   workspace   device scratch of at least ..._workspace_size(...) bytes, 16-byte aligned (may be NULL if 0)
@@ -368,7 +369,7 @@ LAZY_API size_t lazy_cache_select_workspace_size(int32_t batch, int32_t max_kv_l
  *      and lazy_plain_attn_decode.  LAZY_EUNSUPPORTED with LAZY_ALIBI.
  * max_kept bounds the requests' kept counts (LAZY_EUNSUPPORTED from 2^24 on).  weights_out (with weights and key_start
  * as above; all three or none) receives the kept keys' weights at kept_start[r] + i (0 for entries that name no key, or
- * one without room in weights).  k_out and v_out may lie in the pools' own memory (or be the same pointer) as long as no
+ * one without room in weights); it shares no memory with weights (LAZY_EINVAL if the same pointer).  k_out and v_out may lie in the pools' own memory (or be the same pointer) as long as no
  * new record overlaps another or what a table reads.
  */
 LAZY_API int lazy_cache_compact(const lazy_attn_params_t* params, const void* k_pool, const void* v_pool,

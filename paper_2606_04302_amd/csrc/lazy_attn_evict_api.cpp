@@ -178,6 +178,7 @@ int lazy_cache_compact(const lazy_attn_params_t* p, const void* k_pool, const vo
   if (rotate && p->rope_style == LAZY_ALIBI) return LAZY_EUNSUPPORTED;
   const int some = (key_start != nullptr) + (weights != nullptr) + (weights_out != nullptr);
   if (some != 0 && some != 3) return LAZY_EINVAL;
+  if (some == 3 && weights_out == weights) return LAZY_EINVAL;  // other workgroups still read what one writes
   if (batch == 0 || max_kept == 0) return LAZY_OK;
   if (!k_pool || !v_pool || !chunks || !chunk_start || !kept || !kept_start || !dst || !k_out || !v_out)
     return LAZY_EINVAL;

@@ -495,6 +495,8 @@ def _weight_args(cfg, q, q_pos, k_pool, chunks, chunk_start, key_start, batch, l
     if weights_in is not None:
         _dev(weights_in, torch.float32, "weights_in")
         _need(weights_in.shape == weights.shape, "weights_in must have the shape of weights")
+        _need(weights_in.data_ptr() == weights.data_ptr() or _apart(weights_in, weights),
+              "weights_in must be weights or share no memory with it")
 
 
 def prefill_key_weights(cfg: Config, q, q_start, q_pos0, k_pool, chunks, chunk_start, key_start, max_q_len: int,
@@ -581,6 +583,8 @@ def cache_compact(cfg: Config, k_pool, v_pool, chunks, chunk_start, kept, kept_s
         if t is not None:
             _dev(t, torch.float32, name)
     _need(weights_out is None or weights_out.numel() >= kept.numel(), "weights_out must have an entry a kept key")
+    _need(weights is None or weights_out is None or _apart(weights, weights_out),
+          "weights_out must not overlap weights")
     if kept.numel() == 0:
         return k_out, v_out
     p = cfg.c()

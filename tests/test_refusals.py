@@ -1,4 +1,6 @@
 """Calls that the binding refuses before anything is launched (host tensors and a stand-in library that succeeds)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -58,3 +60,49 @@ def test_gradient_pools_may_not_overlap_the_pools(calls, which, of, shift):
         with pytest.raises(ValueError, match=which):
             call()
         assert "lazy_attn_prefill_backward" not in calls
+
+
+@pytest.mark.parametrize("shift", [-3, 0, 4, 7, 8])
+def test_compacted_weights_may_not_overlap_the_weights(calls, shift):
+    """Kept keys move to lower places: one workgroup would overwrite weights that another has yet to read."""
+    w = torch.zeros(24)
+    weights, out = w[8:16], w[8 + shift:8 + shift + 8]
+    if shift == -3:
+        out = w[1:9]  # its last entry is the first weight
+
+    def call():
+        ops.cache_compact(ops.Config(2, 1, 64, 1e4), bf16(512), bf16(512), torch.zeros(32, dtype=torch.uint8), i32(0, 1),
+                          i32(0, 3), i32(0, 2), 2, torch.zeros(32, dtype=torch.uint8), bf16(512), bf16(512),
+                          key_start=i32(0, 8), weights=weights, weights_out=out, stream=0)
+
+    if shift == 8:
+        call()
+        assert calls == ["lazy_cache_compact"]
+    else:
+        with pytest.raises(ValueError, match="weights_out"):
+            call()
+        assert not calls
+
+
+def test_compaction_in_place_is_refused_by_the_library():
+    p, one = ops.Config(4, 2, 64, 1e4).c(), 4096  # addresses that are never read
+    args = [one] * 4 + [1, one, one, 10, one, 0, one, one]
+    assert ops.lib().lazy_cache_compact(ctypes.byref(p), *args, one, one, one, None) == ops.LAZY_EINVAL
+
+
+@pytest.mark.parametrize("shift", [0, 3, 8])
+def test_running_weights_are_the_weights_or_apart(calls, shift):
+    w = torch.zeros(24)
+    q, lse = bf16(1, 2, 64), torch.zeros(1, 2)
+
+    def call():
+        ops.decode_key_weights(ops.Config(2, 1, 64, 1e4), q, i32(7), bf16(512), torch.zeros(32, dtype=torch.uint8),
+                               i32(0, 1), i32(0, 8), 8, lse, w[8:16], weights_in=w[8 + shift:16 + shift], stream=0,
+                               workspace=torch.zeros(64, dtype=torch.uint8))
+
+    if shift == 3:
+        with pytest.raises(ValueError, match="weights_in"):
+            call()
+    else:
+        call()
+        assert calls[-1] == "lazy_attn_decode_key_weights"
