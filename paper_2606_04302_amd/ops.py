@@ -243,7 +243,9 @@ def _workspace(nbytes, device, workspace, stream=None):
         return None
     if workspace is None or workspace.numel() < nbytes:
         with _allocating_for(stream):
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    _need(workspace.device == device and workspace.is_contiguous(),
+          f"workspace must be a contiguous tensor on {device}")
     return workspace
 
 

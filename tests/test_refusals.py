@@ -106,3 +106,19 @@ def test_running_weights_are_the_weights_or_apart(calls, shift):
     else:
         call()
         assert calls[-1] == "lazy_attn_decode_key_weights"
+
+
+def test_workspaces_that_the_kernels_cannot_write_are_refused(calls):
+    """A tensor elsewhere, or one whose bytes do not lie together."""
+    here, other = torch.device("cpu"), torch.zeros(64, dtype=torch.uint8, device="meta")
+    fine = torch.zeros(64, dtype=torch.uint8)
+    assert ops._workspace(64, here, fine) is fine
+    assert ops._workspace(0, here, other) is None
+    assert ops._workspace(65, here, fine).numel() == 65
+    for bad in (other, torch.zeros(128, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            ops._workspace(64, here, bad)
+    with pytest.raises(ValueError, match="workspace"):
+        ops.decode(ops.Config(2, 1, 64, 1e4), bf16(1, 2, 64), i32(7), bf16(512), bf16(512),
+                   torch.zeros(32, dtype=torch.uint8), i32(0, 1), 8, out=bf16(1, 2, 64), workspace=other, stream=0)
+    assert "lazy_attn_decode" not in calls
