@@ -49,13 +49,13 @@ struct KeyIter : TileIter<kSub> {
 
 constexpr int kPrepTokens = 2;
 
-// Queries rotated, in two parts, packed by KV head, and -lse log2 e of each row; workgroups past the last block write the
-// table of angles.
+// Queries rotated, in two parts, packed by KV head, and -lse log2 e of each row; workgroups past the last block (NoPE keys
+// only) write the table of angles.
 template <int D, bool IL>
 __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks) {
   __shared__ float2 cs[kPrepTokens][D / 2];
   if ((int)blockIdx.x >= blocks) {
-    if (a.rotate_k) angle_rows<D>(a, blockIdx.x - blocks);
+    angle_rows<D>(a, blockIdx.x - blocks);
     return;
   }
   const int first = blockIdx.x * kPrepTokens, tokens = min(kPrepTokens, a.total_q - first);
@@ -1082,8 +1082,8 @@ __global__ __launch_bounds__(256) void gather_keys(CompactArgs a) {
 
 template <int D, int KMI>
 hipError_t prompt_mode(const WeightArgs& a, int max_kv_len, hipStream_t s) {
-  const int blocks = (a.total_q + kPrepTokens - 1) / kPrepTokens;
-  prepare_queries<D, interleaved_of(KMI)><<<blocks + kAngleBlocks<D>, 256, 0, s>>>(a, blocks);
+  const int blocks = (a.total_q + kPrepTokens - 1) / kPrepTokens, more = keys_of(KMI) == kKeysNope ? kAngleBlocks<D> : 0;
+  if (blocks + more) prepare_queries<D, interleaved_of(KMI)><<<blocks + more, 256, 0, s>>>(a, blocks);
   weigh_prompt<D, KMI><<<dim3(a.splits * a.row_splits, a.hkv, a.batch), 256, 0, s>>>(a);
   sum_weights<<<dim3(ceil_div(max_kv_len, 256), a.batch), 256, 0, s>>>(a);
   return hipGetLastError();

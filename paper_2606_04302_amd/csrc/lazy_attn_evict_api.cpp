@@ -11,7 +11,7 @@ namespace {
 
 using lazy::ceil_div, lazy::check_params, lazy::kMaxGroups, lazy::kNumCUs;
 
-constexpr int kTileKeys = 64;
+constexpr int kTileKeys = 64, kAngleRows = 32;
 constexpr int64_t kSortBytes = 512 << 10;
 
 int status(hipError_t e) { return e == hipSuccess ? LAZY_OK : LAZY_EHIP; }
@@ -37,7 +37,8 @@ PromptSizes prompt_sizes(const lazy_attn_params_t* p, int32_t batch, int32_t tot
   };
   z.q = put((size_t)rows * p->head_dim * sizeof(uint16_t) * (p->rope_style == LAZY_ALIBI ? 1 : 2));
   z.nlse = put((size_t)rows * sizeof(float));
-  z.angles = put((size_t)kTileKeys * p->head_dim * sizeof(float));
+  const bool block_angles = p->key_positions == LAZY_KEYS_NOPE && p->rope_style != LAZY_ALIBI;
+  z.angles = put((block_angles ? (size_t)kAngleRows : 0) * p->head_dim * sizeof(float));
   z.part = put((size_t)z.row_splits * p->num_kv_heads * (size_t)num_keys * sizeof(float));
   return z;
 }

@@ -119,10 +119,10 @@ __device__ __forceinline__ double revolutions(const Args& a, int t) {
   return a.inv_freq ? (double)a.inv_freq[t] * kInvTwoPi : a.rev[t];
 }
 
-// Angles of positions 0 .. 63, which a tile's keys add to the position of its key 0: (cos, sin) of [64][D/2] pairs by
-// kAngleBlocks workgroups of 256.
+// Angles of positions 0 .. 31, which a 32-key block's keys add to the position of its first: (cos, sin) of [32][D/2] pairs
+// by kAngleBlocks workgroups of 256.
 template <int D>
-constexpr int kAngleBlocks = 64 * (D / 2) / 256;
+constexpr int kAngleBlocks = kAngleRows * (D / 2) / 256;
 template <int D, class Args>
 __device__ __forceinline__ void angle_rows(const Args& a, int block) {
   const int e = block * 256 + threadIdx.x;

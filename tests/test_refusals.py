@@ -122,3 +122,15 @@ def test_workspaces_that_the_kernels_cannot_write_are_refused(calls):
         ops.decode(ops.Config(2, 1, 64, 1e4), bf16(1, 2, 64), i32(7), bf16(512), bf16(512),
                    torch.zeros(32, dtype=torch.uint8), i32(0, 1), 8, out=bf16(1, 2, 64), workspace=other, stream=0)
     assert "lazy_attn_decode" not in calls
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_weights_reserve_angles_where_they_are_read(d):
+    """A table of 32 positions' (cos, sin), and only for keys that are stored without positions."""
+    def size(**kw):
+        return ops.prefill_key_weights_workspace_size(ops.Config(4, 2, d, 1e4, **kw), 2, 6, 3, 100, 200)
+
+    for style in (ops.ROPE_HALF, ops.ROPE_INTERLEAVED):
+        assert size(rope_style=style) - size(rope_style=style, key_positions=ops.KEYS_LOCAL) == 32 * (d // 2) * 8
+    # ALiBi keeps one part of the queries, too: 6 tokens of 4 heads
+    assert size(key_positions=ops.KEYS_LOCAL) - size(rope_style=ops.ALIBI) == 6 * 4 * d * 2
