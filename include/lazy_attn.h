@@ -369,8 +369,8 @@ LAZY_API size_t lazy_cache_select_workspace_size(int32_t batch, int32_t max_kv_l
  *      and lazy_plain_attn_decode.  LAZY_EUNSUPPORTED with LAZY_ALIBI.
  * max_kept bounds the requests' kept counts (LAZY_EUNSUPPORTED from 2^24 on).  weights_out (with weights and key_start
  * as above; all three or none) receives the kept keys' weights at kept_start[r] + i (0 for entries that name no key, or
- * one without room in weights); it shares no memory with weights (LAZY_EINVAL if the same pointer).  k_out and v_out may lie in the pools' own memory (or be the same pointer) as long as no
- * new record overlaps another or what a table reads.
+ * one without room in weights); it shares no memory with weights (LAZY_EINVAL if the same pointer).  k_out and v_out may
+ * lie in the pools' own memory (or be the same pointer) as long as no new record overlaps another or what a table reads.
  */
 LAZY_API int lazy_cache_compact(const lazy_attn_params_t* params, const void* k_pool, const void* v_pool,
                                 const lazy_chunk_t* chunks, const int32_t* chunk_start, int32_t batch,
