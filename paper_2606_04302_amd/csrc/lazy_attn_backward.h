@@ -12,12 +12,13 @@ constexpr int kGradTileKeys = 64;  // stored keys of half a key-gradient tile
 constexpr int kGradHalves = 2;     // halves of a tile: 64 keys each, wherever they lie
 constexpr int kGradRows = 32;      // packed query rows (token * G + head in group) of one step over a tile
 // Most workgroups (tiles and row items of 128 rows) for which one launch takes both kinds of items, where 256 rows a
-// workgroup would do (head_dim 128 and requests that fill them; otherwise both are one launch always).  One launch fills
-// the chip with one kind's workgroups while the other kind's last ones run; two let eight waves share a tile's loads and
-// rotation.  us one launch / two, tiles + items of 128 rows: 120 + 512 77 / 94, 328 + 432 92 / 94, 408 + 512 150 / 150, 656 +
-// 448 137 / 135, 1024 + 512 228 / 220, 760 + 512 424 / 406, 816 + 1024 1288 / 1237, 1408 + 512 404 / 380, 1280 + 4096 17.8 /
-// 16.8 ms; 840 + 1336 789 / 808.  With 128 rows: 136 + 136 37 / 46, 1824 + 480 180 / 194, 2176 + 512 430 / 446.  Head_dim 64: 136
-// + 136 25 / 32, 760 + 512 208 / 200, 816 + 1024 603 / 657, 1408 + 512 193 / 193, 2056 + 496 163 / 169, 1280 + 4096 8.4 / 8.6 ms.
+// workgroup would do (head_dim 128 and requests that fill them; otherwise both are one launch always).  One launch
+// fills the chip with one kind's workgroups while the other kind's last ones run; two let eight waves share a tile's
+// loads and rotation.  us one launch / two, tiles + items of 128 rows: 120 + 512 77 / 94, 328 + 432 92 / 94, 408 + 512
+// 150 / 150, 656 + 448 137 / 135, 1024 + 512 228 / 220, 760 + 512 424 / 406, 816 + 1024 1288 / 1237, 1408 + 512 404 /
+// 380, 1280 + 4096 17.8 / 16.8 ms; 840 + 1336 789 / 808.  With 128 rows: 136 + 136 37 / 46, 1824 + 480 180 / 194, 2176
+// + 512 430 / 446.  Head_dim 64: 136 + 136 25 / 32, 760 + 512 208 / 200, 816 + 1024 603 / 657, 1408 + 512 193 / 193,
+// 2056 + 496 163 / 169, 1280 + 4096 8.4 / 8.6 ms.
 constexpr int64_t kMostTogether = 1024;
 
 // Up to 64 stored keys (key 0 of KV head 0 at k_off / v_off).

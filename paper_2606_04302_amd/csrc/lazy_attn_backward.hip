@@ -1,20 +1,21 @@
 // Backward pass of the prefill attention for gfx950: gradients of the queries and of the stored keys and values.
 //
 // Two to four launches.  (1) prepare_rows: queries rotated to their positions and packed by KV head (row = token * G +
-// head in group), dO packed alike, and two numbers a row, -lse log2 e and -delta.  (2) grad_kv: dk and dv, one tile of the
-// store at a time.  (3) grad_q: dq, one row tile and key split at a time.  (4) finish: partial dq of requests in several key
-// splits summed, turned back and rounded, and the same for tiles whose uses were cut into parts; only where there are any.
-// (2) and (3) are one launch, grad_all, unless there is much work for 256 rows a workgroup (kMostTogether).  The
-// probabilities are recomputed in (2) and in (3): seven products of the two kernels against five if dq were summed over key tiles with atomics, whose order
-// would change results from call to call.
+// head in group), dO packed alike, and two numbers a row, -lse log2 e and -delta.  (2) grad_kv: dk and dv, one tile of
+// the store at a time.  (3) grad_q: dq, one row tile and key split at a time.  (4) finish: partial dq of requests in
+// several key splits summed, turned back and rounded, and the same for tiles whose uses were cut into parts; only where
+// there are any. (2) and (3) are one launch, grad_all, unless there is much work for 256 rows a workgroup
+// (kMostTogether).  The probabilities are recomputed in (2) and in (3): seven products of the two kernels against five
+// if dq were summed over key tiles with atomics, whose order would change results from call to call.
 //
-// Precision: rotated queries and keys, P and dS are each the sum of two bf16 numbers (split8, 2^-17), and a product of two
-// of them is three products, first x first and the two mixed ones; V, dO and ALiBi's queries and keys are exact as they are.
-// One part each, 2^-9 a term, is no error of 2^-9: where a handful of keys holds nearly all of a row's weight, elements of
-// a gradient are far smaller than their terms and far above the tensor's root mean square (3 rows over 28000 ALiBi keys:
-// elements wrong by 0.84 of the larger of themselves and that mean; scores of standard deviation 4: 0.1 to 1.4, and 1% in
-// the 2-norm).  Two parts leave the rounding of the result (0.0039, 0.0017 in the 2-norm) and make sixteen of seven products:
-// 16 ragged requests 3.9 ms instead of 1.85, 8 requests with 64 rows a chunk 0.40 instead of 0.21.
+// Precision: rotated queries and keys, P and dS are each the sum of two bf16 numbers (split8, 2^-17), and a product of
+// two of them is three products, first x first and the two mixed ones; V, dO and ALiBi's queries and keys are exact as
+// they are. One part each, 2^-9 a term, is no error of 2^-9: where a handful of keys holds nearly all of a row's
+// weight, elements of a gradient are far smaller than their terms and far above the tensor's root mean square (3 rows
+// over 28000 ALiBi keys: elements wrong by 0.84 of the larger of themselves and that mean; scores of standard deviation
+// 4: 0.1 to 1.4, and 1% in the 2-norm).  Two parts leave the rounding of the result (0.0039, 0.0017 in the 2-norm) and
+// make sixteen of seven products: 16 ragged requests 3.9 ms instead of 1.85, 8 requests with 64 rows a chunk 0.40
+// instead of 0.21.
 //
 // Rotations: scores are products of keys and queries rotated to their absolute positions, as in the forward pass.  In
 // every tile in LDS and in every operand the head dimension is in half-split order, so that the pair (t, t + D/2) of a
@@ -91,18 +92,19 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
   }
 }
 
-// Key and value gradients.  A workgroup owns a tile of two 64-key halves, each of its four waves 32 keys: K (rotated, both
-// parts) stays in registers and V in LDS, as the right-hand operands of S = Q K^T and dP = dO V^T, whose accumulators have a
-// key in every lane and 32 query rows in registers and lane halves; P and dS leave them, in two parts, as the right-hand
-// operands of dV^T += dO^T P and dK^T += Q^T dS without any exchange between lanes.  S, dV, dP and dK follow each other, so
-// that besides K and the sums only one or two of them are in registers.  Q and dO come through LDS, 32 rows at a time, read
-// by rows for S and dP and transposed for dV and dK.  -delta is dP's initial value.  dK is kept in the rotated frame of the
-// use at hand and turned on when the next use has another position.
+// Key and value gradients.  A workgroup owns a tile of two 64-key halves, each of its four waves 32 keys: K (rotated,
+// both parts) stays in registers and V in LDS, as the right-hand operands of S = Q K^T and dP = dO V^T, whose
+// accumulators have a key in every lane and 32 query rows in registers and lane halves; P and dS leave them, in two
+// parts, as the right-hand operands of dV^T += dO^T P and dK^T += Q^T dS without any exchange between lanes.  S, dV, dP
+// and dK follow each other, so that besides K and the sums only one or two of them are in registers.  Q and dO come
+// through LDS, 32 rows at a time, read by rows for S and dP and transposed for dV and dK.  -delta is dP's initial
+// value.  dK is kept in the rotated frame of the use at hand and turned on when the next use has another position.
 //
-// Two waves a SIMD hide each other's latencies, and one workgroup's products the other's copies: with a second buffer for
-// the next 32 rows, head_dim 128 would leave one workgroup a CU (64 with one and three workgroups: kMostTogether).  Bound by the products: 16 ragged requests, 2.2 TFLOP of nine products 2.1 ms (1050 TFLOP/s, 86% of the large
-// library product's rate); 8 requests of 64 rows a chunk 232 us, where a tile has 8 to 24 steps and its loads, rotations
-// and results are a third.
+// Two waves a SIMD hide each other's latencies, and one workgroup's products the other's copies: with a second buffer
+// for the next 32 rows, head_dim 128 would leave one workgroup a CU (64 with one and three workgroups: kMostTogether).
+// Bound by the products: 16 ragged requests, 2.2 TFLOP of nine products 2.1 ms (1050 TFLOP/s, 86% of the large library
+// product's rate); 8 requests of 64 rows a chunk 232 us, where a tile has 8 to 24 steps and its loads, rotations and
+// results are a third.
 
 // A use as a wave's half of the tile sees it, and a step over it.
 struct Use {
@@ -255,7 +257,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem
       if (lane < kGradRows) {
         const int src = row0 + lane, tok = token_of(src, a.group_magic);
         rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + seg.pos_shift : INT32_MAX - 1;
-        if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, kLog2e);
+        if (ALIBI) rslope[lane] = natural_slope(a, g * a.group + src - tok * a.group);
       }
       wait_reads();
     }
@@ -290,8 +292,7 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int row = 8 * q4 + 4 * h2 + e;
-        // The bias and the log-sum-exp may be large next to their difference: one rounding for both.
-        const float y = ALIBI ? fmaf(rslope[row], (float)(pos + key - rpos[row]), x[e]) * kLog2e : x[e];
+        const float y = ALIBI ? biased(rslope[row], pos + key - rpos[row], x[e]) : x[e];
         s[4 * q4 + e] = fast_exp2(fmaf(s[4 * q4 + e], a.scale_log2, y));
       }
     }
@@ -598,8 +599,7 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
     const int first = 32 * kb + 4 * h2;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      // The bias and the log-sum-exp may be large next to their difference: one rounding for both.
-      const float y = ALIBI ? fmaf(slope, (float)(b0 - qpos + first + 8 * (i >> 2) + (i & 3)), nl) * kLog2e : nl;
+      const float y = ALIBI ? biased(slope, b0 - qpos + first + 8 * (i >> 2) + (i & 3), nl) : nl;
       dp[i] *= fast_exp2(fmaf(s[i], scale_log2, y));
     }
     if (masked) {
@@ -632,11 +632,11 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
   }
 }
 
-// Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q (both parts) and dO in
-// registers; K (rotated, both parts) and V pass through LDS, K read by rows and transposed.  Eight waves share a tile's loads
-// and rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same ragged requests 2.1
-// ms for seven products (820 TFLOP/s), the 64-row questions 170 us.  A request in one key split has its whole sums here: they
-// are turned back and written at once.
+// Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q (both parts) and
+// dO in registers; K (rotated, both parts) and V pass through LDS, K read by rows and transposed.  Eight waves share a
+// tile's loads and rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same
+// ragged requests 2.1 ms for seven products (820 TFLOP/s), the 64-row questions 170 us.  A request in one key split has
+// its whole sums here: they are turned back and written at once.
 template <int D, int KMI, int NW, int NBUF>
 __device__ __forceinline__ void query_gradients(const GradArgs& a, int id, GradQSmem<D, KMI, NBUF>& sm) {
   constexpr int KM = keys_of(KMI), NT = NW * 64;
@@ -660,7 +660,7 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id, GradQ
   }
   const float* in = a.ws_info + (int64_t)g * a.rows + src;
   const float nl = pr < nrows ? in[0] : -INFINITY, nd = in[a.hkv * a.rows];
-  const float slope = ALIBI ? alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, kLog2e) : 0.f;
+  const float slope = ALIBI ? natural_slope(a, g * a.group + src - tok * a.group) : 0.f;
   f32x16 dq[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) dq[db] = f32x16{};
@@ -718,7 +718,8 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id, GradQ
       buf = parity;
       it = ahead;
       have_next = have_ahead;
-      if (early && have_next) ld.store(sm.k[parity ^ 1], sm.k[parity ^ 1] + kSub * D, sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
+      if (early && have_next)
+        ld.store(sm.k[parity ^ 1], sm.k[parity ^ 1] + kSub * D, sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
       if (have_next) {
         if (!early) fetch(it);
         ahead.step();
@@ -730,7 +731,8 @@ __device__ __forceinline__ void query_gradients(const GradArgs& a, int id, GradQ
                         a.causal);
     if (NBUF == 2) {
       if (have_ahead) base(sm.csb[parity][0], ahead);
-      if (!early && have_next) ld.store(sm.k[parity ^ 1], sm.k[parity ^ 1] + kSub * D, sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
+      if (!early && have_next)
+        ld.store(sm.k[parity ^ 1], sm.k[parity ^ 1] + kSub * D, sm.v[parity ^ 1], sm.csb[parity ^ 1][0], sm.csd);
       __syncthreads();
       parity ^= 1;
     }
@@ -820,9 +822,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 constexpr int kMergeRows = 32, kMergeBlocks = 2 * kGradHalves * kGradTileKeys / kMergeRows;
 
 // Partial results added up in their order, two kinds of workgroups in one launch.  The first `blocks`: partial query
-// gradients of a block of tokens, turned back from the rows' positions, scaled, rounded.  The others: 32 rows of the key
-// or value gradients of a tile whose uses were cut into parts.  D / 16 threads a row.  Bound by memory (12 us for 512 tokens
-// of 32 heads of 128 in four splits, 38 MB).
+// gradients of a block of tokens, turned back from the rows' positions, scaled, rounded.  The others: 32 rows of the
+// key or value gradients of a tile whose uses were cut into parts.  D / 16 threads a row.  Bound by memory (12 us for
+// 512 tokens of 32 heads of 128 in four splits, 38 MB).
 template <int D, bool IL>
 __global__ __launch_bounds__(256) void finish(GradArgs a, int blocks) {
   constexpr int TPR = D / 16;

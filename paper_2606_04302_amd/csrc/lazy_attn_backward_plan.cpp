@@ -47,15 +47,15 @@ bool blocks_overlap(const std::vector<Slab>& slabs, int hkv, int d, bool values)
 
 int64_t steps_of(const GradSeg& s) { return (s.row_end - s.row_begin + kGradRows - 1) / kGradRows; }
 
-// Key splits of every request's row tiles.  A candidate lets no work item have more than a given number of key tiles; the
-// one with the least estimated time is taken: the makespan of the items, longest first, on the workgroups that the chip
-// holds, where an item costs its tiles and kItemTiles more (its prologue and its result), plus the partial results'
-// way to memory and back and kFinishUs for the launch that adds them up (a request in one split writes its gradient by
-// itself).  A tile of 256 rows takes a workgroup 8.8 us at head_dim 128.  With 3.7 instead, which splits less, one document
-// of 1024 tokens and 32 / 8 heads took 166 us instead of 151 (head_dim 64: 87 instead of 75), 16 heads of 64 over one KV head
-// and 800 tokens 57 instead of 52; but 512 tokens 68 instead of 70 (64: 38 instead of 42), 16 / 1 heads of 128 and 1024
-// tokens 102 instead of 115.  kItemTiles of 1.5 to 3 are within 2% of each other but for one document (512 tokens: 76 with
-// 1.5, 70 with 3).  More splits are taken for a gain of 3% only.
+// Key splits of every request's row tiles.  A candidate lets no work item have more than a given number of key tiles;
+// the one with the least estimated time is taken: the makespan of the items, longest first, on the workgroups that the
+// chip holds, where an item costs its tiles and kItemTiles more (its prologue and its result), plus the partial
+// results' way to memory and back and kFinishUs for the launch that adds them up (a request in one split writes its
+// gradient by itself).  A tile of 256 rows takes a workgroup 8.8 us at head_dim 128.  With 3.7 instead, which splits
+// less, one document of 1024 tokens and 32 / 8 heads took 166 us instead of 151 (head_dim 64: 87 instead of 75), 16
+// heads of 64 over one KV head and 800 tokens 57 instead of 52; but 512 tokens 68 instead of 70 (64: 38 instead of 42),
+// 16 / 1 heads of 128 and 1024 tokens 102 instead of 115.  kItemTiles of 1.5 to 3 are within 2% of each other but for
+// one document (512 tokens: 76 with 1.5, 70 with 3).  More splits are taken for a gain of 3% only.
 constexpr double kItemTiles = 3, kTileUs = 8.8, kBytesPerUs = 4.5e6, kFinishUs = 15, kClose = 0.97;
 std::vector<int32_t> row_splits(const std::vector<int64_t>& key_tiles, const int32_t* q_start, int batch, int G, int hkv,
                                 int d, int row_blocks) {

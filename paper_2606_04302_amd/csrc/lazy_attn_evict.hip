@@ -49,10 +49,11 @@ struct KeyIter : TileIter<kSub> {
 
 constexpr int kPrepTokens = 2;
 
-// Queries rotated, in two parts, packed by KV head, and -lse log2 e of each row; workgroups past the last block (NoPE keys
+// Queries rotated, in two parts, packed by KV head, and -lse (times log2 e but for ALiBi) of each row; workgroups past the last block (NoPE keys
 // only) write the table of angles.
-template <int D, bool IL>
+template <int D, int KMI>
 __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks) {
+  constexpr bool IL = interleaved_of(KMI);
   __shared__ float2 cs[kPrepTokens][D / 2];
   if ((int)blockIdx.x >= blocks) {
     angle_rows<D>(a, blockIdx.x - blocks);
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(256) void prepare_queries(WeightArgs a, int blocks)
     }
     *reinterpret_cast<u32x4*>(a.ws_q + dst * D + t0) = lo;
     *reinterpret_cast<u32x4*>(a.ws_q + dst * D + D / 2 + t0) = hi;
-    if (t0 == 0) a.ws_nlse[dst] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
+    if (t0 == 0) a.ws_nlse[dst] = lse == -INFINITY ? -INFINITY : -lse * lse_scale(keys_of(KMI));
   }
 }
 
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
         if (lane < kStepRows) {
           const int src = row0 + lane, tok = token_of(src, a.group_magic);
           rpos[lane] = lane >= rows ? INT32_MIN : a.causal || ALIBI ? tok + shift : INT32_MAX;
-          if (ALIBI) rslope[lane] = alibi_slope(g * a.group + src - tok * a.group, a.hq, a.inv_freq, 1.f);
+          if (ALIBI) rslope[lane] = natural_slope(a, g * a.group + src - tok * a.group);
         }
         wait_reads();
       }
@@ -224,13 +225,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
       for (int q4 = 0; q4 < 4; ++q4) {
         const f32x4 x = *reinterpret_cast<const f32x4*>(nl + 8 * q4 + 4 * h2);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * q4 + e] = fmaf(s[4 * q4 + e], a.scale_log2, x[e]);
-      }
-      if (ALIBI) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int row = 8 * (i >> 2) + 4 * h2 + (i & 3);
-          s[i] = fmaf(rslope[row], (float)(b0 + key - rpos[row]), s[i]);
+        for (int e = 0; e < 4; ++e) {
+          const int row = 8 * q4 + 4 * h2 + e;
+          s[4 * q4 + e] =
+              fmaf(s[4 * q4 + e], a.scale_log2, ALIBI ? biased(rslope[row], b0 + key - rpos[row], x[e]) : x[e]);
         }
       }
       if (masked) {
@@ -497,8 +495,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
       for (int e = tid; e < ng * 16; e += 256) {  // rows past a group's end: exp2(score - inf) = 0
         const int grp = g0 + e / 16, in = (grp % per_head) * 16 + e % 16, h = (grp / per_head) * a.group + in;
         const float lse = in < a.group ? a.lse[(int64_t)r * a.hq + h] : -INFINITY;
-        nlse[e] = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
-        if (ALIBI) rslope[e] = in < a.group ? alibi_slope(h, a.hq, a.inv_freq, 1.f) : 0.f;
+        nlse[e] = lse == -INFINITY ? -INFINITY : -lse * lse_scale(KM);
+        if (ALIBI) rslope[e] = in < a.group ? natural_slope(a, h) : 0.f;
       }
       __syncthreads();
       // A wave's groups: first, first + step, ...
@@ -637,14 +635,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) voi
             s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, as_bf16x8(kh[s]), s4, 0, 0, 0);
           }
           {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(nlse + 16 * k + 4 * kq);
+            f32x4 x = *reinterpret_cast<const f32x4*>(nlse + 16 * k + 4 * kq);
+            if (ALIBI) {
+              const f32x4 sl = *reinterpret_cast<const f32x4*>(rslope + 16 * k + 4 * kq);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[e] = biased(sl[e], it.cur.pos + it.j0 + 16 * sub + col - qpos, x[e]);
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) s4[e] = fmaf(s4[e], a.scale_log2, x[e]);
-          }
-          if (ALIBI) {
-            const f32x4 sl = *reinterpret_cast<const f32x4*>(rslope + 16 * k + 4 * kq);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s4[e] = fmaf(sl[e], (float)(it.cur.pos + it.j0 + 16 * sub + col - qpos), s4[e]);
           }
           sum += (fast_exp2(s4[0]) + fast_exp2(s4[1])) + (fast_exp2(s4[2]) + fast_exp2(s4[3]));
         }
@@ -1083,7 +1081,7 @@ __global__ __launch_bounds__(256) void gather_keys(CompactArgs a) {
 template <int D, int KMI>
 hipError_t prompt_mode(const WeightArgs& a, int max_kv_len, hipStream_t s) {
   const int blocks = (a.total_q + kPrepTokens - 1) / kPrepTokens, more = keys_of(KMI) == kKeysNope ? kAngleBlocks<D> : 0;
-  if (blocks + more) prepare_queries<D, interleaved_of(KMI)><<<blocks + more, 256, 0, s>>>(a, blocks);
+  if (blocks + more) prepare_queries<D, KMI><<<blocks + more, 256, 0, s>>>(a, blocks);
   weigh_prompt<D, KMI><<<dim3(a.splits * a.row_splits, a.hkv, a.batch), 256, 0, s>>>(a);
   sum_weights<<<dim3(ceil_div(max_kv_len, 256), a.batch), 256, 0, s>>>(a);
   return hipGetLastError();

@@ -127,7 +127,7 @@ struct WeightArgs {
   const float* weights_in;    // or null
   float* weights;
   uint16_t* ws_q;             // [2][hkv][rows][D] rotated queries in two parts (ALiBi: the first only)
-  float* ws_nlse;             // [hkv][rows] -lse log2 e
+  float* ws_nlse;             // [hkv][rows] -lse log2 e (ALiBi: -lse)
   float* ws_angles;           // [32][D/2] (cos, sin) of positions 0 .. 31 (NoPE keys only)
   float* ws_part;             // [row_splits * hkv][num_keys] partial sums
   const float* inv_freq;

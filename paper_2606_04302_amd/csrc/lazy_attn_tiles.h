@@ -113,6 +113,17 @@ __device__ __forceinline__ void store_pairs(uint16_t* v, int t0, const float (&l
   }
 }
 
+// ALiBi's slopes and the log-sum-exps enter the kernels of these scores as they are, not times log2 e: bias and log-sum-exp
+// may each be far larger than their difference, which is rounded once (fmaf) and then scaled.
+constexpr float lse_scale(int km) { return km == kKeysAlibi ? 1.f : kLog2e; }
+template <class Args>
+__device__ __forceinline__ float natural_slope(const Args& a, int h) {
+  return a.inv_freq ? a.inv_freq[h] : exp2f(-8.0f * (float)(h + 1) / (float)a.hq);
+}
+__device__ __forceinline__ float biased(float slope, int distance, float nlse) {
+  return fmaf(slope, (float)distance, nlse) * kLog2e;
+}
+
 // Rotations per position of pair t, in revolutions: from the caller's table, or as the host worked them out.
 template <class Args>
 __device__ __forceinline__ double revolutions(const Args& a, int t) {

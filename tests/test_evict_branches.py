@@ -10,6 +10,7 @@ from oracle import eviction_oracle as E
 from paper_2606_04302_amd import ops
 from paper_2606_04302_amd import workloads as W
 from tests.test_backward import oracle_kw, shared
+from tests.test_backward_precision import long_context
 from tests.test_evict import check_weights, decode_of, i32, run_select
 
 SLICE, RESIDENT = 16384, 35840  # keys of a slice; most keys that one workgroup holds
@@ -192,3 +193,20 @@ def test_rotated_copies_against_lazy_materialize_k(gpu, d, ckw):
     step = np.maximum(np.abs(want), np.abs(got)) * 2.0 ** -7
     assert (np.abs(got - want) <= step + 4e-6).all()
     assert (got == want).mean() > 0.99
+
+
+FAR = {
+    "d128": lambda: long_context(117, 8, 2, 128, 500, 4, gap=20000),
+    "d64, one KV head": lambda: long_context(118, 8, 1, 64, 500, 40, gap=20000),
+    "d128, plain": lambda: long_context(119, 8, 2, 128, 17000, 4, gap=300000),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", FAR)
+@pytest.mark.parametrize("kind", ["prompt", "token"])
+def test_alibi_weights_far_from_the_keys(gpu, name, kind):
+    """Bias and log-sum-exp are far larger than their difference, the score: what the call is given decides (the slopes
+    of eight heads are powers of two, exact in fp32), so the bound is that of keys nearby."""
+    w = FAR[name]()
+    check_weights(w if kind == "prompt" else decode_of(w), ALIBI, f"{name}, {kind}")
