@@ -400,13 +400,23 @@ def backward_plan(cfg: Config, q_start: np.ndarray, q_pos0: np.ndarray, chunks: 
     _need(0 <= int(chunk_start[-1]) <= chunks.size, "chunk_start goes past the records")
     p, info = cfg.c(), BackwardInfo()
     args = (ctypes.byref(p), q_start.ctypes.data, q_pos0.ctypes.data, chunks.ctypes.data, chunk_start.ctypes.data, batch)
-    code = lib().lazy_attn_backward_plan(*args, None, 0, ctypes.byref(info))
-    if code != LAZY_EINVAL:  # EINVAL: only the size was asked for (or the arguments are bad, then again below)
-        _check(code, "lazy_attn_backward_plan")
-    data = np.zeros(int(info.plan_bytes), np.uint8)
-    _check(lib().lazy_attn_backward_plan(*args, data.ctypes.data, data.size, ctypes.byref(info)),
-           "lazy_attn_backward_plan")
-    return BackwardPlan(data, info)
+    data = np.empty(_plan_room(cfg, q_start, chunks), np.uint8)
+    code = lib().lazy_attn_backward_plan(*args, data.ctypes.data, data.size, ctypes.byref(info))
+    if code == LAZY_EINVAL and info.plan_bytes > data.size:  # rare: planned again with the room that it told
+        data = np.empty(int(info.plan_bytes), np.uint8)
+        code = lib().lazy_attn_backward_plan(*args, data.ctypes.data, data.size, ctypes.byref(info))
+    _check(code, "lazy_attn_backward_plan")
+    return BackwardPlan(data[:int(info.plan_bytes)].copy(), info)
+
+
+def _plan_room(cfg: Config, q_start, chunks) -> int:
+    """Bytes that a backward plan hardly ever exceeds (a planning takes the same time whether its size is known or not):
+    a block a token, row items in up to 32 key splits, a tile with two uses for every 64 keys of every record (64 MiB at
+    most), and 256 KiB of parts and merges."""
+    tokens, batch = int(q_start[-1]), q_start.size - 1
+    rows = tokens * (cfg.num_q_heads // max(1, cfg.num_kv_heads)) // 128 + batch
+    halves = int(chunks["len"].astype(np.int64).sum()) // 64 + 2 * chunks.size
+    return min(64 << 20, max(0, 16 * (tokens + batch) + 16 * 32 * rows + (80 + 2 * 48) * halves)) + (256 << 10)
 
 
 def upload_backward_plan(plan: BackwardPlan, device="cuda:0") -> BackwardPlan:

@@ -151,3 +151,31 @@ def test_plans_are_of_their_kind(name):
 def test_gradients_of_every_kind_of_plan(gpu, name):
     make, ckw, _, _ = PLANS[name]
     check(make(), ckw, name, dlse="interleaved" in name)
+
+
+@pytest.mark.parametrize("room", [None, 0, 100])
+@pytest.mark.parametrize("name", PLANS)
+def test_plans_are_made_once(monkeypatch, name, room):
+    """One run of the planner where the room guessed for the plan is enough, a second one where it is not; equal bytes."""
+    make, ckw, _, _ = PLANS[name]
+    w = make()
+    library, codes = ops.lib(), []
+
+    class Counting:
+        def __getattr__(self, fn):
+            real = getattr(library, fn)
+            if fn != "lazy_attn_backward_plan":
+                return real
+
+            def call(*args):
+                codes.append(real(*args))
+                return codes[-1]
+            return call
+
+    want = make_plan(w, **ckw)[1]
+    monkeypatch.setattr(ops, "lib", lambda: Counting())
+    if room is not None:
+        monkeypatch.setattr(ops, "_plan_room", lambda *a: room)
+    plan = make_plan(w, **ckw)[1]
+    assert codes == ([ops.LAZY_OK] if room is None else [ops.LAZY_EINVAL, ops.LAZY_OK])
+    assert plan.data.size == plan.info.plan_bytes and np.array_equal(plan.data, want.data)
