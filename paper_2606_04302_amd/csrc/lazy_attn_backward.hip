@@ -351,6 +351,10 @@ __device__ __forceinline__ void key_gradients(const GradArgs& a, int id, KeySmem
     fq[0] = op.column(tq, 0, 0);
     if (ROT) fl[0] = op.column(tq2, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
+    if (masked) {  // hidden pairs: 0, also where dp has overflowed
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dp[i] = s[i] > 0.f ? dp[i] : 0.f;
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] *= dp[i];
     __builtin_amdgcn_s_setprio(1);

@@ -179,3 +179,32 @@ def test_plans_are_made_once(monkeypatch, name, room):
     plan = make_plan(w, **ckw)[1]
     assert codes == ([ops.LAZY_OK] if room is None else [ops.LAZY_EINVAL, ops.LAZY_OK])
     assert plan.data.size == plan.info.plan_bytes and np.array_equal(plan.data, want.data)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,ckw", [(64, {}), (128, IL), (128, ALIBI), (128, LOCAL)])
+def test_products_of_hidden_pairs_may_overflow(gpu, d, ckw):
+    """Large finite values of keys that a row does not see, times large finite gradients, are no number: nothing of them
+    reaches a gradient."""
+    w = W.custom(90, 4, 2, d, 1.0e4, [dict(chunks=[(90, 60)], q_len=30, q_pos0=90)])  # keys 60 to 89 lie past every row
+    cfg, dw = ops.config_of(w, **ckw), ops.upload(w)
+    out, lse = ops.run_lazy(dw, cfg)
+    dout = torch.randn(w.q.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(torch.bfloat16) * 1e30
+    plan = ops.upload_backward_plan(ops.backward_plan(cfg, w.q_start, w.q_pos0, w.chunks, w.chunk_start))
+
+    def rows(pool, which):
+        at, st = int(w.chunks[0][which + "_offset"]), int(w.chunks[0][which + "_stride"])
+        return pool.view(-1)[at:at + 2 * st * d].view(2, st, d)
+
+    got = []
+    for large in (False, True):
+        pool = dw.pool.clone()
+        if large:
+            rows(pool, "v")[:, 60:90] = 3.0e38
+        got.append(ops.prefill_backward(cfg, dw.q, dw.q_start, dw.q_pos0, pool, pool.clone(), dw.chunks, dw.chunk_start,
+                                        out, lse, dout, plan, dk_pool=torch.zeros_like(pool),
+                                        dv_pool=torch.zeros_like(pool)))
+    for a, b in zip(*got):
+        assert torch.isfinite(b).all() and b.any() and torch.equal(a, b)
+    for pool, which in ((got[1][1], "k"), (got[1][2], "v")):
+        assert rows(pool, which)[:, :60].any() and not rows(pool, which)[:, 60:90].any()
