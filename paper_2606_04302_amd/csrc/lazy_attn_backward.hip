@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void prepare_rows(GradArgs a) {
 // Two waves a SIMD hide each other's latencies, and one workgroup's products the other's copies: with a second buffer
 // for the next 32 rows, head_dim 128 would leave one workgroup a CU (64 with one and three workgroups: kMostTogether).
 // Bound by the products: 16 ragged requests, 2.2 TFLOP of nine products 2.1 ms (1050 TFLOP/s, 86% of the large library
-// product's rate); 8 requests of 64 rows a chunk 232 us, where a tile has 8 to 24 steps and its loads, rotations and
+// product's rate); 8 requests of 64 rows a chunk 211 us, where a tile has 8 to 24 steps and its loads, rotations and
 // results are a third.
 
 // A use as a wave's half of the tile sees it, and a step over it.
@@ -639,7 +639,7 @@ __device__ __forceinline__ void grad_tile(const uint16_t* tk, const uint16_t* tv
 // Query gradient of 32 NW packed rows over the 64-key tiles of one key split: NW waves of 32 rows, Q (both parts) and
 // dO in registers; K (rotated, both parts) and V pass through LDS, K read by rows and transposed.  Eight waves share a
 // tile's loads and rotation where requests fill 256 rows.  Bound like grad_kv, and by the loader's rotation: the same
-// ragged requests 2.1 ms for seven products (820 TFLOP/s), the 64-row questions 170 us.  A request in one key split has
+// ragged requests 2.1 ms for seven products (820 TFLOP/s), the 64-row questions 159 us.  A request in one key split has
 // its whole sums here: they are turned back and written at once.
 template <int D, int KMI, int NW, int NBUF>
 __device__ __forceinline__ void query_gradients(const GradArgs& a, int id, GradQSmem<D, KMI, NBUF>& sm) {
