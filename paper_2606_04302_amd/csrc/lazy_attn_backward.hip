@@ -13,7 +13,7 @@
 // they are. One part each, 2^-9 a term, is no error of 2^-9: where a handful of keys holds nearly all of a row's
 // weight, elements of a gradient are far smaller than their terms and far above the tensor's root mean square (3 rows
 // over 28000 ALiBi keys: elements wrong by 0.84 of the larger of themselves and that mean; scores of standard deviation
-// 4: 0.1 to 1.4, and 1% in the 2-norm).  Two parts leave the rounding of the result (0.0039, 0.0017 in the 2-norm) and
+// 4: 0.03 to 1.4, and 1% in the 2-norm).  Two parts leave the rounding of the result (0.0039, 0.0017 in the 2-norm) and
 // make sixteen of seven products: 16 ragged requests 3.9 ms instead of 1.85, 8 requests with 64 rows a chunk 0.40
 // instead of 0.21.
 //

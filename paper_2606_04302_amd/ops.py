@@ -244,8 +244,8 @@ def _workspace(nbytes, device, workspace, stream=None):
     if workspace is None or workspace.numel() < nbytes:
         with _allocating_for(stream):
             return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    _need(workspace.device == device and workspace.is_contiguous(),
-          f"workspace must be a contiguous tensor on {device}")
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
     return workspace
 
 
@@ -466,7 +466,8 @@ def prefill_backward(cfg: Config, q, q_start, q_pos0, k_pool, v_pool, chunks, ch
             raise ValueError(f"{name} must have the shape of what it is the gradient of")
     # Keys and values are read again after the first gradients are written.
     for t, name in ((dk_pool, "dk_pool"), (dv_pool, "dv_pool")):
-        _need(_apart(t, k_pool) and _apart(t, v_pool), f"{name} must not overlap k_pool or v_pool")
+        if not (_apart(t, k_pool) and _apart(t, v_pool)):
+            raise ValueError(f"{name} must not overlap k_pool or v_pool")
     p = cfg.c()
     p, info = ctypes.byref(p), ctypes.byref(plan.info)
     nbytes = lib().lazy_attn_backward_workspace_size(p, info)

@@ -110,6 +110,32 @@ def test_the_current_streams_pointer_is_the_public_one(gpu):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("which", ["pointer 0", "default stream", "side stream"])
+def test_calls_that_allocate_take_any_stream(gpu, which):
+    """The default stream has the pointer 0."""
+    side = torch.cuda.Stream()
+    stream = {"pointer 0": 0, "default stream": torch.cuda.default_stream(), "side stream": side}[which]
+    w = W.custom(4, 8, 2, 128, 1.0e4, [dict(chunks=[(300, 0), (40, 300)], q_len=40, q_pos0=300)])
+    dw = ops.upload(w)
+    cfg = ops.config_of(w, num_splits=3)
+    plan = ops.upload_backward_plan(ops.backward_plan(cfg, w.q_start, w.q_pos0, w.chunks, w.chunk_start))
+
+    def call(s):
+        out, lse = ops.run_lazy(dw, cfg, stream=s)
+        grads = ops.prefill_backward(cfg, dw.q, dw.q_start, dw.q_pos0, dw.pool, dw.pool, dw.chunks, dw.chunk_start, out,
+                                     lse, dw.q, plan, stream=s)
+        both = ops.run_materialized(dw, cfg, stream=s)[0]
+        return (out, lse, *grads, *both)
+
+    want = call(None)
+    torch.cuda.synchronize()
+    got = call(stream)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
 def test_forward_calls_on_another_stream_keep_their_memory(gpu):
     """Split decode and prefill on a stream that is still busy, while the current stream allocates and fills memory of
     the sizes that the calls took: the same bits as on the current stream."""
